@@ -207,6 +207,95 @@ int moe_ep_forward_noalloc(const moe_ep_config *cfg, const void *tokens, const f
                            int32_t r_chunks, int32_t order, int32_t n_tokens, void *out,
                            void *stream, const char **why);
 
+/* Types of operands that come in more than one. */
+typedef enum { MOE_EP_BF16 = 0, MOE_EP_F32 = 1 } moe_ep_type;
+
+/*
+ * Routing rules (Sec. 2.1 leaves the gate's form open; moe_ep_forward by itself takes the softmax over the top_k largest scores).  A
+ * token's scores s over E experts become
+ *   p    MOE_EP_SCORE_SOFTMAX: softmax over the experts that are there; MOE_EP_SCORE_SIGMOID: 1 / (1 + exp(-s))
+ *   c    p + bias, by which experts are chosen; without a bias they are chosen by the order of s
+ *   the n_groups groups of E / n_groups consecutive experts count by the largest c of their experts (MOE_EP_GROUP_MAX) or by the sum
+ *        of the two largest (MOE_EP_GROUP_TOP2; of a group with one expert by that one; without a bias c = p); the best top_groups stay
+ *   idx  the top_k experts of those groups with the largest c, best first
+ *   w    p of the chosen experts (never the bias); renormalise: divided by their sum; times scale
+ * Equal groups and experts: the lower one first.  Choices are those of c computed in double precision; weights are fp32.
+ * An expert is not there for a token where its score is NaN, minus infinity or the lowest finite value of the scores' type, or its
+ * bias NaN or minus infinity; no expert is there for a token whose token_mask byte is 0 (padding).  Slots that no expert is left for
+ * come last and get idx -1 and w 0.  A score of plus infinity counts as the largest fp32 number.
+ */
+typedef enum { MOE_EP_SCORE_SOFTMAX = 0, MOE_EP_SCORE_SIGMOID = 1 } moe_ep_score;
+typedef enum { MOE_EP_GROUP_MAX = 0, MOE_EP_GROUP_TOP2 = 1 } moe_ep_group_score;
+typedef struct {
+    int32_t n_experts;    /* E; 1..512                                                        */
+    int32_t top_k;        /* 1..64, at most the experts of top_groups groups                  */
+    int32_t n_groups;     /* 1..64, divides n_experts; 0 = 1, no groups                       */
+    int32_t top_groups;   /* 1..n_groups (ignored without groups)                             */
+    int32_t score;        /* moe_ep_score                                                     */
+    int32_t group_score;  /* moe_ep_group_score (ignored without groups)                      */
+    int32_t renormalise;  /* 0 or 1                                                           */
+    int32_t score_type;   /* moe_ep_type of the scores                                        */
+    int32_t device;       /* HIP device ordinal                                               */
+    float scale;          /* positive                                                         */
+    int64_t score_stride; /* scores between the rows of two tokens; 0 = n_experts; up to 2^22 */
+} moe_ep_routing;
+
+/* Pure host check, usable without a GPU; returns and `why` as for moe_ep_validate_config. */
+int moe_ep_validate_routing(const moe_ep_routing *rule, const char **why);
+
+/*
+ * Experts and weights of n_tokens tokens by a rule.
+ *   scores      score_type [n_tokens, E], rows score_stride apart, aligned to their elements
+ *   bias        fp32 [E], or NULL;   token_mask  one byte per token, 0 = padding, or NULL
+ *   idx, w      int32 and fp32 [n_tokens, top_k]; neither may overlap the other or an input
+ *   stream      hipStream_t (NULL = the default stream); the call only enqueues one kernel: it allocates nothing, keeps nothing and never waits,
+ *               so it may be recorded into a HIP graph, and calls on different streams do not disturb each other
+ *   why         may be NULL; receives a string naming the first violated rule or the failed HIP call (valid until
+ *               the calling thread's next call)
+ * All pointers are GPU-addressable memory; what they point at is checked as moe_ep_forward does (MOE_EP_CHECK_POINTERS, read once).
+ * The rule's device need not be the current one, which the call leaves as it was.  n_tokens == 0 is a no-op.
+ */
+int moe_ep_route(const moe_ep_routing *rule, const void *scores, const float *bias, const uint8_t *token_mask,
+                 int32_t n_tokens, int32_t *idx, float *w, void *stream, const char **why);
+
+/*
+ * Matrix product with an epilogue: out = act(x W^T + bias) + residual.  The gate's scores are one (fp32 weights and results), a dense
+ * layer's projections and the output projection onto the residual stream others.
+ */
+typedef enum {
+    MOE_EP_ACT_NONE = 0,
+    MOE_EP_ACT_RELU = 1,
+    MOE_EP_ACT_SILU = 2,     /* z / (1 + exp(-z))                                          */
+    MOE_EP_ACT_GELU = 3,     /* z (1 + erf(z / sqrt 2)) / 2                                */
+    MOE_EP_ACT_GELU_TANH = 4 /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2          */
+} moe_ep_activation;
+typedef struct {
+    int32_t in_features;     /* K; 1..2^20                                                 */
+    int32_t out_features;    /* N; 1..2^20                                                 */
+    int32_t weight_type;     /* moe_ep_type                                                */
+    int32_t out_type;        /* moe_ep_type of out and residual                            */
+    int32_t activation;      /* moe_ep_activation                                          */
+    int32_t device;          /* HIP device ordinal                                         */
+    int64_t x_stride;        /* elements between two rows; 0 = rows without a gap; up to 2^22 */
+    int64_t weight_stride;
+    int64_t residual_stride;
+    int64_t out_stride;
+} moe_ep_linear_config;
+
+/* Pure host check, usable without a GPU; returns and `why` as for moe_ep_validate_config. */
+int moe_ep_validate_linear(const moe_ep_linear_config *cfg, const char **why);
+
+/*
+ *   x         bf16 [n_rows, K];   weight  weight_type [N, K];   bias  fp32 [N], or NULL
+ *   residual  out_type [n_rows, N], or NULL; may be `out` itself (with the same stride)
+ *   out       out_type [n_rows, N]; must not overlap anything else.  What lies between its rows is left as it is.
+ * Rows are contiguous and every pointer is aligned to its elements; no more is asked of sizes, strides and addresses.  Products are summed in fp32 (fp32
+ * weights enter with their whole mantissa and must be finite), bias, activation and residual are fp32 too, and a result is rounded once.  The same call gives the
+ * same bits.  Streams, graphs, devices, checks, `why` and n_rows == 0 as for moe_ep_route.
+ */
+int moe_ep_linear(const moe_ep_linear_config *cfg, const void *x, const void *weight, const float *bias,
+                  const void *residual, int32_t n_rows, void *out, void *stream, const char **why);
+
 /*
  * Test / inspection surface: host copies of what the last forward computed for chunk
  * `chunk` (synchronises the context's streams; after moe_ep_forward_dep chunk = i * r_2 + j for

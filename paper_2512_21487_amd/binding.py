@@ -83,6 +83,31 @@ class MoeEpConfig(ctypes.Structure):
         "max_tokens", "max_top_k", "max_chunks", "io_mode", "device")]
 
 
+BF16, F32 = 0, 1
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+GROUP_MAX, GROUP_TOP2 = 0, 1
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = 0, 1, 2, 3, 4
+
+
+class Routing(ctypes.Structure):
+    """Mirror of ``moe_ep_routing``; fields that are not named are 0, but for a scale of 1."""
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "n_experts", "top_k", "n_groups", "top_groups", "score", "group_score", "renormalise", "score_type",
+        "device")] + [("scale", ctypes.c_float), ("score_stride", ctypes.c_int64)]
+
+    def __init__(self, *args, **kw):
+        if len(args) < 10:
+            kw.setdefault("scale", 1.0)
+        super().__init__(*args, **kw)
+
+
+class LinearConfig(ctypes.Structure):
+    """Mirror of ``moe_ep_linear_config``; fields that are not named are 0."""
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "in_features", "out_features", "weight_type", "out_type", "activation", "device")] + [
+        (n, ctypes.c_int64) for n in ("x_stride", "weight_stride", "residual_stride", "out_stride")]
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -122,6 +147,15 @@ def load_library() -> ctypes.CDLL:
                                            ctypes.POINTER(ctypes.c_char_p)]
     lib.moe_ep_forward_dep.restype = ctypes.c_int
     lib.moe_ep_forward_dep.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, ctypes.c_double, i32, vp, vp]
+    whyp = ctypes.POINTER(ctypes.c_char_p)
+    lib.moe_ep_validate_routing.restype = ctypes.c_int
+    lib.moe_ep_validate_routing.argtypes = [ctypes.POINTER(Routing), whyp]
+    lib.moe_ep_route.restype = ctypes.c_int
+    lib.moe_ep_route.argtypes = [ctypes.POINTER(Routing), vp, vp, vp, i32, vp, vp, vp, whyp]
+    lib.moe_ep_validate_linear.restype = ctypes.c_int
+    lib.moe_ep_validate_linear.argtypes = [ctypes.POINTER(LinearConfig), whyp]
+    lib.moe_ep_linear.restype = ctypes.c_int
+    lib.moe_ep_linear.argtypes = [ctypes.POINTER(LinearConfig), vp, vp, vp, vp, i32, vp, vp, whyp]
     lib.moe_ep_chunk_range.restype = ctypes.c_int
     lib.moe_ep_chunk_range.argtypes = [i32, i32, i32, i32, vp, vp]
     lib.moe_ep_routed_tile_rows.restype = i32
@@ -241,6 +275,91 @@ def forward_noalloc(cfg: MoeEpConfig, tokens, gate_logits, routed_w, shared_w, t
     rc = load_library().moe_ep_forward_noalloc(ctypes.byref(cfg), _ptr(tokens), _ptr(gate_logits), _ptr(routed_w),
                                                _ptr(shared_w), top_k, r_chunks, order, n_tokens, _ptr(out), stream,
                                                ctypes.byref(why))
+    if rc != 0:
+        raise MoeEpError(rc, (why.value or b"").decode())
+    return rc
+
+
+def _check_rows(x, name: str, n_rows: int, cols: int, stride: int, size: int) -> None:
+    """Marshalling check of a torch tensor argument of rows that may lie apart: element size, at least ``n_rows`` rows of ``cols``
+    contiguous elements ``stride`` apart, on the GPU (raw addresses pass through)."""
+    if x is None or not hasattr(x, "stride"):
+        return
+    if x.element_size() != size:
+        raise ValueError(f"{name} has elements of {x.element_size()} bytes, the call reads {size}")
+    if not (x.is_cuda or x.is_pinned()):
+        raise ValueError(f"{name} must be a device tensor")
+    if x.dim() == 1 and n_rows == 1:
+        if x.shape[0] < cols or (cols > 1 and x.stride(0) != 1):
+            raise ValueError(f"{name} must be a contiguous row of {cols}")
+        return
+    if x.dim() != 2 or x.shape[0] < n_rows or x.shape[1] < cols:
+        raise ValueError(f"{name} must be at least {n_rows} rows of {cols}, got {tuple(x.shape)}")
+    if (cols > 1 and x.stride(1) != 1) or (n_rows > 1 and x.stride(0) != stride):
+        raise ValueError(f"{name} has strides {x.stride()}, the call reads rows {stride} apart")
+
+
+def _check_vector(x, name: str, n: int, size: int) -> None:
+    if x is None or not hasattr(x, "stride"):
+        return
+    if x.element_size() != size or not x.is_contiguous() or x.numel() < n:
+        raise ValueError(f"{name} must be {n} contiguous elements of {size} bytes")
+    if not (x.is_cuda or x.is_pinned()):
+        raise ValueError(f"{name} must be a device tensor")
+
+
+def validate_routing(rule: Routing) -> Tuple[int, str]:
+    why = ctypes.c_char_p()
+    rc = load_library().moe_ep_validate_routing(ctypes.byref(rule), ctypes.byref(why))
+    return rc, (why.value or b"").decode()
+
+
+def route(rule: Routing, scores, bias=None, token_mask=None, n_tokens: Optional[int] = None, idx=None, w=None,
+          stream: Optional[int] = None) -> int:
+    """moe_ep_route: ``idx`` (int32) and ``w`` (fp32), both [n_tokens, top_k], from the scores by ``rule``."""
+    if n_tokens is None:
+        n_tokens = int(scores.shape[0])
+    if stream is None:
+        import torch
+        stream = torch.cuda.current_stream().cuda_stream
+    k = rule.top_k
+    _check_rows(scores, "scores", n_tokens, rule.n_experts, rule.score_stride or rule.n_experts, 4 if rule.score_type else 2)
+    _check_vector(bias, "bias", rule.n_experts, 4)
+    _check_vector(token_mask, "token_mask", n_tokens, 1)
+    _check_vector(idx, "idx", n_tokens * k, 4)
+    _check_vector(w, "w", n_tokens * k, 4)
+    why = ctypes.c_char_p()
+    rc = load_library().moe_ep_route(ctypes.byref(rule), _ptr(scores), _ptr(bias), _ptr(token_mask), n_tokens, _ptr(idx),
+                                     _ptr(w), stream, ctypes.byref(why))
+    if rc != 0:
+        raise MoeEpError(rc, (why.value or b"").decode())
+    return rc
+
+
+def validate_linear(cfg: LinearConfig) -> Tuple[int, str]:
+    why = ctypes.c_char_p()
+    rc = load_library().moe_ep_validate_linear(ctypes.byref(cfg), ctypes.byref(why))
+    return rc, (why.value or b"").decode()
+
+
+def linear(cfg: LinearConfig, x, weight, bias=None, residual=None, out=None, n_rows: Optional[int] = None,
+           stream: Optional[int] = None) -> int:
+    """moe_ep_linear: out = act(x weight^T + bias) + residual."""
+    if n_rows is None:
+        n_rows = int(x.shape[0])
+    if stream is None:
+        import torch
+        stream = torch.cuda.current_stream().cuda_stream
+    K, N = cfg.in_features, cfg.out_features
+    size = 4 if cfg.out_type else 2
+    _check_rows(x, "x", n_rows, K, cfg.x_stride or K, 2)
+    _check_rows(weight, "weight", N, K, cfg.weight_stride or K, 4 if cfg.weight_type else 2)
+    _check_vector(bias, "bias", N, 4)
+    _check_rows(residual, "residual", n_rows, N, cfg.residual_stride or N, size)
+    _check_rows(out, "out", n_rows, N, cfg.out_stride or N, size)
+    why = ctypes.c_char_p()
+    rc = load_library().moe_ep_linear(ctypes.byref(cfg), _ptr(x), _ptr(weight), _ptr(bias), _ptr(residual), n_rows,
+                                      _ptr(out), stream, ctypes.byref(why))
     if rc != 0:
         raise MoeEpError(rc, (why.value or b"").decode())
     return rc

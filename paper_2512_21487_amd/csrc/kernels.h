@@ -212,4 +212,29 @@ bool grouped_gemm_variant_shape(int variant, int K, bool ragged, int G, int shap
 // the variant of the same tile shape that multiplies with the 16 x 16 x 32 instruction, or `variant` itself
 int grouped_gemm_variant_mfma16(int variant);
 
+// ---- routing rules (routing.hip): the public struct's fields as the kernels read them
+struct RouteArgs {
+    const void* scores; const float* bias; const uint8_t* token_mask;   // the last two may be NULL
+    int32_t* idx; float* w;
+    long long stride;                                                   // scores between two tokens' rows
+    int T, E, k, groups, top_groups;
+    bool bf16, sigmoid, group_top2, renorm;
+    float scale;
+};
+hipError_t launch_route(const RouteArgs& a, hipStream_t s);
+
+// ---- matrix product with an epilogue (linear.hip)
+enum { kActNone = 0, kActRelu, kActSilu, kActGelu, kActGeluTanh, kActCount };
+struct LinearArgs {
+    const uint16_t* x; const void* w; const float* bias; const void* residual; void* out;   // bias, residual may be NULL
+    long long ldx, ldw, ldr, ldo;
+    int R, N, K, act;
+    bool w32, out32;
+    bool rows_first;   // set by the launcher: consecutive tiles are of one column tile
+};
+hipError_t launch_linear(const LinearArgs& a, int n_cu, hipStream_t s);
+
+// What the kernels are about to read or write through a caller's pointer (moe_ep.hip): NULL where it is usable, else what is wrong
+const char* check_span(const void* p, size_t bytes, bool want_host, const void** dev_ptr);
+
 }  // namespace moe_ep

@@ -309,12 +309,14 @@ int fail(moe_ep_ctx* ctx, int code, const char* what, hipError_t e = hipSuccess)
         if (e__ != hipSuccess) return fail((ctx), MOE_EP_EHIP, #call, e__);     \
     } while (0)
 
+}  // namespace
+
 // What the kernels are about to read or write through a caller's pointer: memory the GPU can
 // address, of at least `bytes` bytes where the runtime knows the allocation's extent.  Turns a host
 // pointer or an undersized buffer into an error before a kernel faults on it.  Returns nullptr when
 // the span is usable, else what is wrong with it.  `want_host`: pinned host memory is required
 // (the link stand-ins of MOE_EP_IO_PINNED_HOST); *dev_ptr receives the address kernels use.
-const char* check_span(const void* p, size_t bytes, bool want_host, const void** dev_ptr)
+const char* moe_ep::check_span(const void* p, size_t bytes, bool want_host, const void** dev_ptr)
 {
     hipPointerAttribute_t attr;
     if (hipPointerGetAttributes(&attr, p) != hipSuccess) {
@@ -346,6 +348,8 @@ const char* check_span(const void* p, size_t bytes, bool want_host, const void**
     if (q < lo || (size_t)(lo + size - q) < bytes) return "points at an allocation smaller than the forward needs";
     return nullptr;
 }
+
+namespace {
 
 // Tile shape of a routed projection for a chunk of Tn tokens.  Row tiles are cut to fit each expert
 // (units of unit_rows rows, at most max_units per tile, equal heights), so a shape is judged by how

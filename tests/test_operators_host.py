@@ -1,0 +1,117 @@
+"""moe_ep_route, moe_ep_linear: structs, exported constants and refusals, all of them before any HIP call."""
+import ctypes
+import os
+import re
+
+import pytest
+
+import paper_2512_21487_amd as pkg
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+SIZES = {"int32_t": 4, "float": 4, "int64_t": 8}
+
+
+@pytest.mark.parametrize("struct,mirror", [("moe_ep_routing", pkg.Routing), ("moe_ep_linear_config", pkg.LinearConfig)])
+def test_structs_match_header(struct, mirror):
+    header = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "moe_ep.h")).read(), flags=re.S)
+    body = re.search(r"typedef struct \{([^}]*)\} " + struct + ";", header).group(1)
+    fields = re.findall(r"(\w+)\s+(\w+)\s*;", body)
+    assert [n for _, n in fields] == [f[0] for f in mirror._fields_]
+    assert [SIZES[t] for t, _ in fields] == [ctypes.sizeof(f[1]) for f in mirror._fields_]
+
+
+def rule(**kw):
+    return pkg.Routing(**dict(dict(n_experts=64, top_k=6, renormalise=1, score_type=pkg.F32), **kw))
+
+
+@pytest.mark.parametrize("bad,word", [
+    (dict(n_experts=0), "n_experts"), (dict(n_experts=513), "n_experts"), (dict(top_k=0), "top_k"), (dict(top_k=65), "top_k"),
+    (dict(n_experts=4, top_k=5), "top_k"), (dict(n_groups=7), "n_groups"), (dict(n_groups=-1), "n_groups"),
+    (dict(n_experts=130, n_groups=65, top_groups=1, top_k=1), "n_groups"), (dict(n_groups=8, top_groups=0), "top_groups"),
+    (dict(n_groups=8, top_groups=9), "top_groups"), (dict(n_groups=16, top_groups=1), "top_k"), (dict(score=2), "score"),
+    (dict(group_score=2), "group_score"), (dict(renormalise=2), "renormalise"), (dict(score_type=2), "score_type"),
+    (dict(score_stride=63), "score_stride"), (dict(score_stride=(1 << 22) + 1), "score_stride"), (dict(scale=0.0), "scale"),
+    (dict(scale=-1.0), "scale"), (dict(scale=float("nan")), "scale"), (dict(scale=float("inf")), "scale"), (dict(device=-1), "device")])
+def test_routing_rules_that_are_refused(bad, word):
+    rc, why = pkg.validate_routing(rule(**bad))
+    assert rc == -1 and word in why
+
+
+def test_routing_rules_that_are_taken():
+    for good in (dict(), dict(n_experts=1, top_k=1), dict(n_experts=512, top_k=64), dict(n_groups=64, top_groups=6), dict(n_groups=1),
+                 dict(n_groups=8, top_groups=8, group_score=pkg.GROUP_TOP2, score=pkg.SCORE_SIGMOID), dict(score_stride=1 << 22)):
+        assert pkg.validate_routing(rule(**good)) == (0, "ok")
+    assert rule().scale == 1.0 and pkg.Routing(n_experts=4, top_k=1, scale=2.5).scale == 2.5
+
+
+def config(**kw):
+    return pkg.LinearConfig(**dict(dict(in_features=64, out_features=32), **kw))
+
+
+@pytest.mark.parametrize("bad,word", [
+    (dict(in_features=0), "in_features"), (dict(in_features=(1 << 20) + 1), "in_features"), (dict(out_features=0), "out_features"),
+    (dict(weight_type=2), "weight_type"), (dict(out_type=-1), "out_type"), (dict(activation=5), "activation"),
+    (dict(activation=-1), "activation"), (dict(x_stride=63), "x_stride"), (dict(weight_stride=63), "weight_stride"),
+    (dict(residual_stride=31), "residual_stride"), (dict(out_stride=31), "out_stride"), (dict(x_stride=(1 << 22) + 1), "x_stride"),
+    (dict(device=-1), "device")])
+def test_products_that_are_refused(bad, word):
+    rc, why = pkg.validate_linear(config(**bad))
+    assert rc == -1 and word in why
+
+
+def test_products_that_are_taken():
+    assert pkg.validate_linear(config()) == (0, "ok")
+    assert pkg.validate_linear(config(x_stride=64, out_stride=1 << 22, weight_type=pkg.F32, out_type=pkg.F32, activation=pkg.ACT_GELU_TANH)) == (0, "ok")
+
+
+# addresses that are never read: the call is refused before
+A, B, C, D, E = (0x10000000 * i for i in range(1, 6))
+
+
+@pytest.mark.parametrize("args,word", [
+    ((None, None, None, 4, A, B), "NULL"), ((A, None, None, 4, None, B), "NULL"), ((A, None, None, 4, B, None), "NULL"),
+    ((A, None, None, -1, B, C), "n_tokens"), ((A + 2, None, None, 4, B, C), "aligned"), ((A, B + 1, None, 4, C, D), "aligned"),
+    ((A, None, None, 4, B + 2, C), "aligned"), ((A, None, None, 4, A + 64, C), "idx must not overlap scores"),
+    ((A, None, None, 4, B, B + 92), "overlap"), ((A, B, None, 4, C, B + 252), "w must not overlap bias"),
+    ((A, None, B, 4, C, B - 92), "w must not overlap token_mask")])
+def test_routing_calls_that_are_refused(args, word):
+    scores, bias, mask, n, idx, w = args
+    with pytest.raises(pkg.MoeEpError) as ei:
+        pkg.route(rule(), scores, bias, mask, n_tokens=n, idx=idx, w=w, stream=0)
+    assert ei.value.code == -1 and word in str(ei.value)
+
+
+@pytest.mark.parametrize("args,word", [
+    ((None, A, None, None, B, 4), "NULL"), ((A, None, None, None, B, 4), "NULL"), ((A, B, None, None, None, 4), "NULL"),
+    ((A, B, None, None, C, -1), "n_rows"), ((A + 1, B, None, None, C, 4), "aligned"), ((A, B + 1, None, None, C, 4), "aligned"),
+    ((A, B, C + 2, None, D, 4), "aligned"), ((A, B, None, C + 1, D, 4), "aligned"), ((A, B, None, None, C + 1, 4), "aligned"),
+    ((A, B, None, None, A, 4), "out must not overlap x"), ((A, B, None, None, B + 4094, 4), "out must not overlap weight"),
+    ((A, B, C, None, C + 126, 4), "out must not overlap bias"), ((A, B, None, C, C + 2, 4), "out must not overlap residual"),
+    ((A, B, None, C, C - 254, 4), "out must not overlap residual")])
+def test_product_calls_that_are_refused(args, word):
+    x, weight, bias, residual, out, n = args
+    with pytest.raises(pkg.MoeEpError) as ei:
+        pkg.linear(config(), x, weight, bias, residual, out=out, n_rows=n, stream=0)
+    assert ei.value.code == -1 and word in str(ei.value)
+
+
+def test_in_place_residual_with_another_stride_is_refused():
+    with pytest.raises(pkg.MoeEpError) as ei:
+        pkg.linear(config(residual_stride=40), A, B, None, C, out=C, n_rows=4, stream=0)
+    assert ei.value.code == -1 and "overlap residual" in str(ei.value)
+
+
+def test_calls_without_a_row_do_nothing():
+    assert pkg.route(rule(), None, n_tokens=0, stream=0) == 0
+    assert pkg.linear(config(), None, None, n_rows=0, stream=0) == 0
+
+
+def test_tensors_that_do_not_fit_are_refused():
+    torch = pytest.importorskip("torch")
+    x = torch.zeros((4, 64), dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="device tensor"):
+        pkg.linear(config(), x, A, out=B, stream=0)
+    with pytest.raises(ValueError, match="elements of 4 bytes"):
+        pkg.linear(config(), x.float(), A, out=B, stream=0)
+    with pytest.raises(ValueError, match="device tensor"):
+        pkg.route(rule(), torch.zeros((4, 64)), idx=A, w=B, stream=0)
