@@ -5,81 +5,170 @@
 //
 // fp32 weights are three bf16 numbers each, 8 mantissa bits at a time cut off the top (24 together: all of them), and a product is three
 // matrix instructions: as exact as fp32 multiplications at 5 times their rate.
+#include <cmath>
+#include <type_traits>
+
 #include "common.h"
 
 namespace moe_ep {
 
 namespace {
 
-// 16 bytes from an address that only the type of the elements aligns
+#define SB() __builtin_amdgcn_sched_barrier(0)
+
+// 16 or 8 bytes from an address that only the type of the elements aligns
 typedef uint32_t u32x4_any2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2_any2 __attribute__((ext_vector_type(2), aligned(2)));
 typedef float f32x4_any4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 
+// exp from the hardware's exp2: off by about a step of fp32 and by what the argument's own rounding makes of it
+__device__ __forceinline__ float exp_f(float x) { return __builtin_amdgcn_exp2f(x * 1.4426950408889634f); }
+
+// 0.5 z (1 + erf(z / sqrt 2)).  1 - erf(x) for x >= 0 is a polynomial in 1 / (1 + p x) times exp(-x^2) to 1.5e-7 (Abramowitz and Stegun,
+// Handbook of Mathematical Functions, 7.1.26), so that nothing cancels where z is negative.
+__device__ __forceinline__ float gelu_f(float z)
+{
+    const float x = fabsf(z) * 0.7071067811865476f;
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
+    const float q = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    const float h = 0.5f * z * (q * exp_f(-x * x));   // 0.5 z (1 - erf(x))
+    return z >= 0.f ? z - h : h;
+}
+
+// 0.5 z (1 + tanh(u)) = z / (1 + exp(-2u)),  u = sqrt(2 / pi) (z + 0.044715 z^3)
 __device__ __forceinline__ float gelu_tanh_f(float z)
 {
-    // 0.5 z (1 + tanh(u)) = z / (1 + exp(-2u)),  u = sqrt(2 / pi) (z + 0.044715 z^3)
     const float u = 0.7978845608028654f * (z + 0.044715f * z * z * z);
-    return z / (1.0f + expf(-2.0f * u));
+    return z * __builtin_amdgcn_rcpf(1.0f + exp_f(-2.0f * u));
 }
 
-__device__ __forceinline__ float activate(int act, float z)
+// one branch for N numbers
+template <int N, class V>
+__device__ __forceinline__ void activate(int act, V& v)
 {
     switch (act) {
-    case kActRelu: return z < 0.f ? 0.f : z;   // a NaN stays one
-    case kActSilu: return z / (1.0f + expf(-z));
-    case kActGelu: return 0.5f * z * (1.0f + erff(z * 0.7071067811865476f));
-    case kActGeluTanh: return gelu_tanh_f(z);
-    default: return z;
+    case kActRelu:
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];   // a NaN stays one
+        break;
+    case kActSilu:
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = silu_f(v[i]);
+        break;
+    case kActGelu:
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = gelu_f(v[i]);
+        break;
+    case kActGeluTanh:
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = gelu_tanh_f(v[i]);
+        break;
+    default: break;
     }
 }
 
-// four consecutive columns of a row: bias, activation, residual, rounding, store
-__device__ __forceinline__ void finish(const LinearArgs& a, int m, int n, f32x4_t v)
-{
-    const int left = a.N - n;
-    if (m >= a.R || left <= 0) return;
-    const bool whole = left >= 4;
-    if (a.bias) {
+// Epilogue of 16 rows x NB * 16 columns in registers: a lane has 4 consecutive columns of its row in every block of 16.
+template <int NB>
+struct Epilogue {
+    struct Residual { u32x4_t v[NB]; };          // bf16 ones take the first half
+    const LinearArgs& a;
+    int n, kh;                                   // the lane's column in block 0; which four of the block's 16 columns
+    bool whole;                                  // every column of the wavefront is there
+    f32x4_t bias[NB];
+
+    __device__ __forceinline__ Epilogue(const LinearArgs& args, int n0, int kh_) : a(args), n(n0 + kh_ * 4), kh(kh_), whole(n0 + NB * 16 <= args.N)
+    {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] += a.bias[n + (whole ? i : min(i, left - 1))];
-    }
-    if (a.act != kActNone) {
+        for (int b = 0; b < NB; ++b) {
+            bias[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            if (!a.bias) continue;
+            if (whole) bias[b] = *reinterpret_cast<const f32x4_any4*>(a.bias + n + b * 16);
+            else
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = activate(a.act, v[i]);
-    }
-    const size_t at = (size_t)m * a.ldo + n;
-    if (a.residual) {
-        const size_t from = (size_t)m * a.ldr + n;
-        if (a.out32) {
-            const float* r = static_cast<const float*>(a.residual) + from;
-            if (whole) v += *reinterpret_cast<const f32x4_any4*>(r);
-            else for (int i = 0; i < left; ++i) v[i] += r[i];
-        } else {
-            const uint16_t* r = static_cast<const uint16_t*>(a.residual) + from;
-            for (int i = 0; i < 4; ++i) if (i < left) v[i] += __uint_as_float((uint32_t)r[i] << 16);
+                for (int i = 0; i < 4; ++i) bias[b][i] = a.bias[min(n + b * 16 + i, a.N - 1)];
         }
     }
-    if (a.out32) {
-        float* o = static_cast<float*>(a.out) + at;
-        if (whole) *reinterpret_cast<f32x4_any4*>(o) = v;
-        else for (int i = 0; i < left; ++i) o[i] = v[i];
-    } else {
-        uint16_t* o = static_cast<uint16_t*>(a.out) + at;
-        const uint32_t p[2] = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-        for (int i = 0; i < 4; ++i) if (i < left) o[i] = (uint16_t)(p[i >> 1] >> (16 * (i & 1)));
+    __device__ __forceinline__ bool group(int b) const { return whole || n + b * 16 + 4 <= a.N; }   // all four columns in block b
+    // of a row that is there
+    __device__ __forceinline__ void fetch(int m, Residual& r) const
+    {
+        const char* const row = static_cast<const char*>(a.residual) + ((size_t)m * a.ldr + n) * (a.out32 ? 4 : 2);
+        if (a.out32) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+                if (group(b)) r.v[b] = *reinterpret_cast<const u32x4_any2*>(row + b * 64);
+        } else {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+                if (group(b)) {
+                    const u32x2_t x = *reinterpret_cast<const u32x2_any2*>(row + b * 32);
+                    r.v[b] = u32x4_t{x[0], x[1], 0, 0};
+                }
+        }
     }
-}
+    __device__ __forceinline__ void store(int m, bool there, f32x4_t v[NB], const Residual& res) const
+    {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            v[b] += bias[b];
+            activate<4>(a.act, v[b]);
+        }
+        if (a.residual) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                if (!group(b)) continue;
+                const u32x4_t r = res.v[b];
+                v[b] += a.out32 ? __builtin_bit_cast(f32x4_t, r) : f32x4_t{bf16_lo(r[0]), bf16_hi(r[0]), bf16_lo(r[1]), bf16_hi(r[1])};
+            }
+        }
+        char* const row = static_cast<char*>(a.out) + ((size_t)m * a.ldo + n) * (a.out32 ? 4 : 2);
+        if (whole && !a.out32) {
+            // two neighbouring blocks exchange halves: 8 columns of one of them a lane, 64 bytes of a row a store
+            char* const at = row + ((kh & 1) * 16 + (kh >> 1) * 8 - kh * 4) * 2;
+#pragma unroll
+            for (int b = 0; b + 1 < NB; b += 2) {
+                const f32x4_t u = v[b], w = v[b + 1];
+                const auto s0 = __builtin_amdgcn_permlane16_swap(pack_bf16x2(u[0], u[1]), pack_bf16x2(w[0], w[1]), false, false);
+                const auto s1 = __builtin_amdgcn_permlane16_swap(pack_bf16x2(u[2], u[3]), pack_bf16x2(w[2], w[3]), false, false);
+                if (there) *reinterpret_cast<u32x4_any2*>(at + b * 32) = u32x4_t{s0[0], s1[0], s0[1], s1[1]};
+            }
+        }
+        if (!there) return;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            if (whole && !a.out32 && !(NB % 2 && b == NB - 1)) continue;
+            if (!group(b)) continue;
+            if (a.out32) *reinterpret_cast<f32x4_any4*>(row + b * 64) = v[b];
+            else *reinterpret_cast<u32x2_any2*>(row + b * 32) = u32x2_t{pack_bf16x2(v[b][0], v[b][1]), pack_bf16x2(v[b][2], v[b][3])};
+        }
+        if (whole || a.N % 4 == 0) return;
+        // the last columns, fewer than four, of whichever block they are in
+        const int left = a.N - n, last = left >> 4;
+        if (left < 0 || (left & 15) > 3 || last >= NB) return;
+        f32x4_t u = v[0];
+#pragma unroll
+        for (int b = 1; b < NB; ++b) u = last == b ? v[b] : u;
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            if (i >= (left & 15)) continue;
+            const size_t from = (size_t)m * a.ldr + n + last * 16 + i;
+            float x = u[i];
+            if (a.out32) reinterpret_cast<float*>(row)[last * 16 + i] = a.residual ? x + static_cast<const float*>(a.residual)[from] : x;
+            else reinterpret_cast<uint16_t*>(row)[last * 16 + i] = (uint16_t)pack_bf16x2(a.residual ? x + bf16_lo(static_cast<const uint16_t*>(a.residual)[from]) : x, 0.f);
+        }
+    }
+};
 
-// 8 elements of a row from element k on, zeros from the row's end on; p: element k
-__device__ __forceinline__ bf16x8_t load8(const uint16_t* p, int left)
+// 8 elements of a row, the `left` first of which are there, and zeros; p: the first
+__device__ __forceinline__ u32x4_t load8(const uint16_t* p, int left)
 {
-    if (left >= 8) return __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_any2*>(p));
-    uint32_t v[4] = {0, 0, 0, 0};
-    for (int i = 0; i < 8; ++i) if (i < left) v[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
-    const u32x4_t u = {v[0], v[1], v[2], v[3]};
-    return __builtin_bit_cast(bf16x8_t, u);
+    if (left >= 8) return *reinterpret_cast<const u32x4_any2*>(p);
+    u32x4_t v = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 7; ++i) if (i < left) v[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
+    return v;
 }
 struct f32x8_t { f32x4_t lo, hi; };
 __device__ __forceinline__ f32x8_t load8(const float* p, int left)
@@ -94,6 +183,97 @@ __device__ __forceinline__ f32x8_t load8(const float* p, int left)
     }
     return v;
 }
+
+// 16 bytes of a row, the `left` first elements of which are there, and zeros
+template <int N, class T>
+__device__ __forceinline__ u32x4_t load_part(const T* p, int left)
+{
+    u32x4_t v = {0, 0, 0, 0};
+    if (left >= N) return *reinterpret_cast<const u32x4_any2*>(p);
+#pragma unroll
+    for (int i = 0; i < N - 1; ++i) {
+        if (i >= left) continue;
+        if constexpr (N == 8) v[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
+        else v[i] = __float_as_uint(p[i]);
+    }
+    return v;
+}
+
+// ---- a few rows: no matrix instruction is full
+
+// A workgroup has C columns and up to RB rows: its threads take 8 elements of the reduction in turn, which reads the weights in whole
+// 4 or 8 KB, and their sums are added up through the wavefronts and LDS.
+template <int RB, int C, bool W32>
+__global__ __launch_bounds__(256) void linear_rows_kernel(LinearArgs a)
+{
+    __shared__ float s_sum[4][C * RB];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int nt = (a.N + C - 1) / C, n0 = (int)(blockIdx.x % nt) * C, m0 = (int)(blockIdx.x / nt) * RB;
+    float acc[C][RB];
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int r = 0; r < RB; ++r) acc[c][r] = 0.f;
+    typedef typename std::conditional<W32, float, uint16_t>::type Weight;
+    typedef typename std::conditional<W32, f32x8_t, u32x4_t>::type Weight8;
+#pragma unroll 2
+    for (int k = tid * 8; k < a.K; k += 256 * 8) {
+        const int left = a.K - k;
+        Weight8 w[C];
+        u32x4_t x[RB];
+#pragma unroll
+        for (int c = 0; c < C; ++c) w[c] = load8(static_cast<const Weight*>(a.w) + (size_t)min(n0 + c, a.N - 1) * a.ldw + k, left);
+#pragma unroll
+        for (int r = 0; r < RB; ++r) x[r] = load8(a.x + (size_t)min(m0 + r, a.R - 1) * a.ldx + k, left);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if constexpr (W32) f[i] = i < 4 ? w[c].lo[i & 3] : w[c].hi[i & 3];
+                else f[i] = (i & 1) ? bf16_hi(w[c][i >> 1]) : bf16_lo(w[c][i >> 1]);
+            }
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[c][r] = fmaf(f[i], (i & 1) ? bf16_hi(x[r][i >> 1]) : bf16_lo(x[r][i >> 1]), acc[c][r]);
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            float v = acc[c][r];
+#pragma unroll
+            for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d, 64);
+            if (lane == 0) s_sum[wave][r * C + c] = v;
+        }
+    __syncthreads();
+    if (tid < C * RB) {
+        const int m = m0 + tid / C, n = n0 + tid % C;
+        if (m < a.R && n < a.N) {
+            float v[1] = {s_sum[0][tid] + s_sum[1][tid] + s_sum[2][tid] + s_sum[3][tid]};
+            if (a.bias) v[0] += a.bias[n];
+            activate<1>(a.act, v);
+            const size_t from = (size_t)m * a.ldr + n, to = (size_t)m * a.ldo + n;
+            if (a.residual) v[0] += a.out32 ? static_cast<const float*>(a.residual)[from] : bf16_lo(static_cast<const uint16_t*>(a.residual)[from]);
+            if (a.out32) static_cast<float*>(a.out)[to] = v[0];
+            else static_cast<uint16_t*>(a.out)[to] = (uint16_t)pack_bf16x2(v[0], 0.f);
+        }
+    }
+}
+
+template <int RB, int C>
+hipError_t launch_rows(const LinearArgs& a, hipStream_t s)
+{
+    const long long grid = (long long)((a.N + C - 1) / C) * ((a.R + RB - 1) / RB);
+    if (grid > 0x7fffffffll) return hipErrorInvalidValue;
+    if (a.w32) hipLaunchKernelGGL((linear_rows_kernel<RB, C, true>), dim3((unsigned)grid), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((linear_rows_kernel<RB, C, false>), dim3((unsigned)grid), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+// ---- some rows, weights in fp32, or operands that are not on 16 bytes
 
 // the upper halves of two words, of `a` in the low half
 __device__ __forceinline__ uint32_t upper_halves(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
@@ -111,71 +291,147 @@ __device__ __forceinline__ void split3(const f32x8_t& w, bf16x8_t part[3])
     }
 }
 
-// Few rows or few columns: both operands go from memory straight into the lanes that multiply them, and the wavefronts of a workgroup
-// take K steps of 64 in turn; their sums are added up in LDS, in the order of the wavefronts.  MB x NB blocks of 16 rows x 16 columns.
+// The wavefronts of a workgroup share a tile of MB x NB blocks of 16 rows x 16 columns and take K steps of 64 of it in turn; their sums are added up
+// in LDS, in the order of the wavefronts.  A step's rows are fetched in whole pieces of 128 or 256 bytes, at any alignment, and go through LDS of
+// the wavefront's own (16-byte chunks XOR-swizzled by the row) to the lanes that multiply them, while the next step's are on their way.  Straight into
+// those lanes, 16 rows' bytes at a time, a load took the memory path four times as long (4096 x 128 x 4096, fp32 weights: 33 us).
+template <int MB, int NB, bool W32>
+struct SplitCfg {
+    static constexpr int KS = 64, WROW = W32 ? 256 : 128;                    // bytes of a row of weights
+    static constexpr int XL = MB * 2, WL = NB * 16 * WROW / 1024;             // loads of 1 KB
+    static constexpr int X_BYTES = MB * 16 * 128, W_BYTES = NB * 16 * WROW, BYTES = X_BYTES + W_BYTES;
+    static_assert(MB * NB * 1024 <= BYTES, "the sums take the place of the operands");
+};
+
 template <int MB, int NB, int WAVES, bool W32>
 __global__ __launch_bounds__(WAVES * 64) void linear_split_kernel(LinearArgs a)
 {
-    constexpr int KS = 64;
-    __shared__ f32x4_t s_sum[WAVES][MB * NB][64];
+    using C = SplitCfg<MB, NB, W32>;
+    constexpr int KS = C::KS;
+    extern __shared__ uint4 lds4[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    char* const own = reinterpret_cast<char*>(lds4) + wave * C::BYTES;
     // tiles of one XCD (workgroup number mod 8) are consecutive ones
     const int mt = (a.R + MB * 16 - 1) / (MB * 16), nt = (a.N + NB * 16 - 1) / (NB * 16);
     const long long total = (long long)mt * nt, per = (total + 7) / 8, L = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
     if ((blockIdx.x >> 3) >= per || L >= total) return;
     const int m0 = (int)(a.rows_first ? L % mt : L / nt) * (MB * 16), n0 = (int)(a.rows_first ? L / mt : L % nt) * (NB * 16);
-    const int row = lane & 15, kq = (lane >> 4) * 8;
 
-    const uint16_t* xp[MB];
-    const char* wp[NB];
-    constexpr int WB = W32 ? 4 : 2;
+    // load i of the rows: 8 of x, or of bf16 weights, 8 lanes each; 4 of fp32 weights, 16 lanes each
+    typedef typename std::conditional<W32, float, uint16_t>::type Weight;
+    constexpr int PER = W32 ? 4 : 8;                                          // weights in 16 bytes
+    const int xr = lane >> 3, xc = lane & 7, wr = W32 ? lane >> 4 : lane >> 3, wc = W32 ? lane & 15 : lane & 7;
+    const uint16_t* const x0 = a.x + (size_t)m0 * a.ldx;
+    const Weight* const w0 = static_cast<const Weight*>(a.w) + (size_t)n0 * a.ldw;
+    // a tile's rows from its first: 64 rows of 2^22 elements are within 32 bits
+    uint32_t xo[C::XL], wo[C::WL];
 #pragma unroll
-    for (int i = 0; i < MB; ++i) xp[i] = a.x + (size_t)min(m0 + i * 16 + row, a.R - 1) * a.ldx + kq;
+    for (int i = 0; i < C::XL; ++i) xo[i] = (uint32_t)min(i * 8 + xr, a.R - 1 - m0) * (uint32_t)a.ldx + xc * 8;
 #pragma unroll
-    for (int i = 0; i < NB; ++i) wp[i] = static_cast<const char*>(a.w) + ((size_t)min(n0 + i * 16 + row, a.N - 1) * a.ldw + kq) * WB;
+    for (int i = 0; i < C::WL; ++i) wo[i] = (uint32_t)min(i * (64 / (C::WROW / 16)) + wr, a.N - 1 - n0) * (uint32_t)a.ldw + wc * PER;
+    struct Step { u32x4_t x[C::XL], w[C::WL]; } f;
+    // whole: all 64 elements are there
+    const auto load = [&](int step, bool whole) __attribute__((always_inline)) {
+        const int left = a.K - step * KS;
+#pragma unroll
+        for (int i = 0; i < C::WL; ++i) {
+            const Weight* p = w0 + step * KS + wo[i];
+            f.w[i] = whole ? *reinterpret_cast<const u32x4_any2*>(p) : load_part<PER>(p, left - wc * PER);
+        }
+#pragma unroll
+        for (int i = 0; i < C::XL; ++i) {
+            const uint16_t* p = x0 + step * KS + xo[i];
+            f.x[i] = whole ? *reinterpret_cast<const u32x4_any2*>(p) : load_part<8>(p, left - xc * 8);
+        }
+    };
+    const uint32_t xw = xr * 128, ww = C::X_BYTES + wr * C::WROW;
+    const auto to_lds = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < C::WL; ++i) {
+            const int r = i * (64 / (C::WROW / 16)) + wr, sw = W32 ? r & 15 : (r >> 1) & 7;
+            *reinterpret_cast<u32x4_t*>(own + ww + i * 1024 + (wc ^ sw) * 16) = f.w[i];
+        }
+#pragma unroll
+        for (int i = 0; i < C::XL; ++i) *reinterpret_cast<u32x4_t*>(own + xw + i * 1024 + (xc ^ (((i * 8 + xr) >> 1) & 7)) * 16) = f.x[i];
+    };
 
+    const int row = lane & 15, kh = lane >> 4, sw = (row >> 1) & 7, sw32 = row;
     f32x4_t acc[MB][NB];
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
         for (int j = 0; j < NB; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int k0 = wave * KS; k0 < a.K; k0 += WAVES * KS) {
+    const auto multiply = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int k = k0 + h * 32, left = a.K - k - kq;
-            bf16x8_t xf[MB];
+            bf16x8_t x[MB];
 #pragma unroll
-            for (int i = 0; i < MB; ++i) xf[i] = load8(xp[i] + k, left);
+            for (int i = 0; i < MB; ++i) x[i] = *reinterpret_cast<const bf16x8_t*>(own + (i * 16 + row) * 128 + ((h * 4 + kh) ^ sw) * 16);
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
+                const char* const at = own + C::X_BYTES + (j * 16 + row) * C::WROW;
                 if constexpr (W32) {
+                    f32x8_t v;
+                    v.lo = *reinterpret_cast<const f32x4_t*>(at + ((h * 8 + kh * 2) ^ sw32) * 16);
+                    v.hi = *reinterpret_cast<const f32x4_t*>(at + ((h * 8 + kh * 2 + 1) ^ sw32) * 16);
                     bf16x8_t part[3];
-                    split3(load8(reinterpret_cast<const float*>(wp[j]) + k, left), part);
+                    split3(v, part);
 #pragma unroll
                     for (int p = 0; p < 3; ++p)
 #pragma unroll
-                        for (int i = 0; i < MB; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part[p], xf[i], acc[i][j], 0, 0, 0);
+                        for (int i = 0; i < MB; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part[p], x[i], acc[i][j], 0, 0, 0);
                 } else {
-                    const bf16x8_t wf = load8(reinterpret_cast<const uint16_t*>(wp[j]) + k, left);
+                    const bf16x8_t w = *reinterpret_cast<const bf16x8_t*>(at + ((h * 4 + kh) ^ sw) * 16);
 #pragma unroll
-                    for (int i = 0; i < MB; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, xf[i], acc[i][j], 0, 0, 0);
+                    for (int i = 0; i < MB; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x[i], acc[i][j], 0, 0, 0);
                 }
             }
         }
+    };
+    const int steps = (a.K + KS - 1) / KS, whole = a.K / KS;
+    if (wave < steps) load(wave, wave < whole);
+    for (int st = wave; st < steps; st += WAVES) {
+        to_lds();
+        wavefront_lds_order();
+        if (st + WAVES < steps) load(st + WAVES, st + WAVES < whole);
+        SB();   // or the compiler moves loads behind the products
+        multiply();
+        wavefront_lds_order();
     }
+    // a wavefront's operands make room for its sums
+    f32x4_t* const sums = reinterpret_cast<f32x4_t*>(own) + lane;
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
-        for (int j = 0; j < NB; ++j) s_sum[wave][i * NB + j][lane] = acc[i][j];
+        for (int j = 0; j < NB; ++j) sums[(i * NB + j) * 64] = acc[i][j];
     __syncthreads();
-    // neighbouring threads: neighbouring columns
-    for (int q = threadIdx.x; q < MB * NB * 64; q += WAVES * 64) {
-        const int r = q / (NB * 4), c = q % (NB * 4), b = (r / 16) * NB + c / 4, l = (c & 3) * 16 + (r & 15);
-        f32x4_t v = s_sum[0][b][l];
+    // 16 rows a wavefront
+    for (int i = wave; i < MB; i += WAVES) {
+        const Epilogue<NB> e(a, n0, kh);
+        const int m = m0 + i * 16 + row;
+        typename Epilogue<NB>::Residual res;
+        if (a.residual && m < a.R) e.fetch(m, res);
+        f32x4_t v[NB];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) v += s_sum[w][b][l];
-        finish(a, m0 + r, n0 + c * 4, v);
+        for (int j = 0; j < NB; ++j) {
+            const f32x4_t* const at = reinterpret_cast<const f32x4_t*>(lds4) + (i * NB + j) * 64 + lane;
+            v[j] = at[0];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) v[j] += at[w * (C::BYTES / 16)];
+        }
+        e.store(m, m < a.R, v, res);
     }
+}
+
+template <int MB, int NB, int WAVES, bool W32>
+hipError_t launch_split_as(const LinearArgs& a, unsigned grid, hipStream_t s)
+{
+    constexpr int bytes = WAVES * SplitCfg<MB, NB, W32>::BYTES;
+    static_assert(bytes <= 160 * 1024, "LDS of a compute unit");
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&linear_split_kernel<MB, NB, WAVES, W32>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((linear_split_kernel<MB, NB, WAVES, W32>), dim3(grid), dim3(WAVES * 64), bytes, s, a);
+    return hipGetLastError();
 }
 
 template <int MB, int NB, int WAVES>
@@ -185,25 +441,35 @@ hipError_t launch_split(LinearArgs a, hipStream_t s)
     if (per * 8 > 0x7fffffffll) return hipErrorInvalidValue;
     // an XCD's tiles share the rows of the larger operand through its L2
     a.rows_first = (double)a.N * a.K * (a.w32 ? 4 : 2) > (double)a.R * a.K * 2;
-    if (a.w32) hipLaunchKernelGGL((linear_split_kernel<MB, NB, WAVES, true>), dim3((unsigned)(per * 8)), dim3(WAVES * 64), 0, s, a);
-    else hipLaunchKernelGGL((linear_split_kernel<MB, NB, WAVES, false>), dim3((unsigned)(per * 8)), dim3(WAVES * 64), 0, s, a);
-    return hipGetLastError();
+    return a.w32 ? launch_split_as<MB, NB, WAVES, true>(a, (unsigned)(per * 8), s) : launch_split_as<MB, NB, WAVES, false>(a, (unsigned)(per * 8), s);
 }
 
-#define SB() __builtin_amdgcn_sched_barrier(0)
+// ---- many rows and columns
+
+
+// 16 bytes per lane from memory to consecutive places in LDS.  Written out because the compiler cannot tell which slot a load is on its way to, and
+// makes a fragment read in the middle of a K step wait for all of them; hand_over() is what waits.
+__device__ __forceinline__ void load_to_lds(uint32_t to, const char* base, uint32_t off)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ void load_to_lds(uint32_t to, const char* src)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(src) : "memory", "m0");
+}
 
 __device__ const uint4 kZeros[4] = {};   // what a lane fetches that is beyond its row's end
 
 // Many rows and columns: tiles of BM rows x BN columns through LDS, 2 x 2 wavefronts.  A K step is 64 elements, rows of 128 bytes
-// whose 16-byte chunks are XOR-swizzled by the row, so that fragment reads meet no bank twice; global_load_lds brings them in, a ring of
-// two slots.  A workgroup takes tiles in turn; the loads run a K step ahead of the multiplications, across tiles too.
-template <int BM, int BN>
+// whose 16-byte chunks are XOR-swizzled by the row, so that fragment reads meet no bank twice; global_load_lds brings them in, into a ring of
+// SLOTS K steps.  A workgroup takes tiles in turn; the loads run ahead of the multiplications across tiles too.
+template <int BM, int BN, int SLOTS>
 struct TileCfg {
-    static constexpr int KS = 64, NW = 4, SLOTS = 2;
+    static constexpr int KS = 64, NW = 4;
     static constexpr int WTM = BM / 2, WTN = BN / 2, MB = WTM / 16, NB = WTN / 16;
     static constexpr int RX = BM / 8 / NW, RW = BN / 8 / NW, RPW = RX + RW;   // 1 KB regions (8 rows) a wavefront loads per K step
     static constexpr int SLOT_BYTES = (BM + BN) * KS * 2;
-    static constexpr int LANES = WTN / 8, SUM_BYTES = 16 * WTN * 4;           // epilogue: 8 columns a lane; a wavefront's row of blocks in fp32
+    static constexpr int SUM_BYTES = 16 * WTN * 4;                            // epilogue: a wavefront's row of blocks in fp32
     static constexpr int LDS_BYTES = SLOTS * SLOT_BYTES + NW * SUM_BYTES;
     static constexpr int M = 2 * MB * NB;                                     // MFMAs of a K step
     static constexpr int TAIL = M / 4 > MB + NB ? M / 4 : MB + NB;            // of which behind the hand-over of the next slot
@@ -218,62 +484,118 @@ struct TileCfg {
     }
 };
 
-// The results of 16 rows x 8 * LANES columns that a wavefront holds in LDS as fp32 (16-byte chunks XOR-swizzled by the row): bias, activation,
-// residual, rounding, stores of whole pieces of a row.  A lane has 8 consecutive columns n.. of every (64 / LANES)th row from m on.
-template <int LANES>
-__device__ __forceinline__ void finish_rows(const LinearArgs& a, const char* sums, int lane, int m, int n, const float bias[8])
-{
-    constexpr int ROWS = 64 / LANES;
-    const int c = lane % LANES, left = a.N - n;
-#pragma unroll 1
-    for (int r = lane / LANES; r < 16; r += ROWS) {
-        if (m + r >= a.R || left <= 0) continue;
-        const char* row = sums + r * LANES * 32;
-        const f32x4_t lo = *reinterpret_cast<const f32x4_t*>(row + ((2 * c) ^ (r & 7)) * 16);
-        const f32x4_t hi = *reinterpret_cast<const f32x4_t*>(row + ((2 * c + 1) ^ (r & 7)) * 16);
-        float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+// Epilogue of a wavefront's part of a tile, MB * 16 rows x COLS columns.  Bias and activation are applied where the sums are, a row of blocks at a
+// time; that goes through LDS (fp32, 16-byte chunks XOR-swizzled by the row), so that residual and results move in whole pieces of a row: a lane has 8
+// consecutive columns of every (64 / LANES)th row.  Straight from the accumulators, 8 bytes of 16 rows at a time, the residual alone took
+// 80 us of 16384 x 5120 x 5120 instead of 8.
+template <int MB, int COLS, bool ACT>
+struct TileEpilogue {
+    static constexpr int NB = COLS / 16, LANES = COLS > 64 ? 16 : COLS > 32 ? 8 : 4, ROWS = 64 / LANES, PASSES = 16 / ROWS;
+    static_assert(COLS % 32 == 0 && COLS <= 128, "rows of whole swizzled groups of chunks");
+    struct Residual { u32x4_t v[PASSES][2]; };   // 8 numbers; bf16 ones take the first half
+
+    const LinearArgs& a;
+    char* sums;
+    const char* res_at;                          // of the wavefront's first row and column; a lane adds 32 bits (256 rows of 2^22 numbers fit)
+    char* out_at;
+    int rows, left, r0;                          // rows that are there; columns that are, from the lane's first; the lane's row in a pass
+    uint32_t res_off, out_off, write, read;
+    f32x4_t bias[NB];
+
+    // m, n: the wavefront's first row and column
+    __device__ __forceinline__ TileEpilogue(const LinearArgs& args, char* lds, int lane, int m, int n) : a(args), sums(lds), rows(args.R - m)
+    {
+        const int size = a.out32 ? 4 : 2, c = min(lane % LANES, COLS / 8 - 1), fr = lane & 15, kh = lane >> 4;
+        r0 = lane / LANES;
+        left = c == lane % LANES ? a.N - n - c * 8 : 0;
+        res_at = static_cast<const char*>(a.residual) + ((size_t)m * a.ldr + n) * size;
+        out_at = static_cast<char*>(a.out) + ((size_t)m * a.ldo + n) * size;
+        res_off = (uint32_t)(r0 * (uint32_t)a.ldr + c * 8) * size;
+        out_off = (uint32_t)(r0 * (uint32_t)a.ldo + c * 8) * size;
+        write = fr * (COLS * 4) + ((kh ^ (fr & 3)) + (fr & 4)) * 16;
+        read = r0 * (COLS * 4) + ((2 * c) ^ (r0 & 7)) * 16;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += bias[i];
-        if (a.act != kActNone) {
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = activate(a.act, v[i]);
-        }
-        if (a.residual) {
-            const size_t from = (size_t)(m + r) * a.ldr + n;
-            if (a.out32) {
-                const float* p = static_cast<const float*>(a.residual) + from;
-                if (left >= 8) {
-                    const f32x4_t x = *reinterpret_cast<const f32x4_any4*>(p), y = *reinterpret_cast<const f32x4_any4*>(p + 4);
+            for (int i = 0; i < 4; ++i) bias[b][i] = a.bias ? a.bias[min(n + b * 16 + kh * 4 + i, a.N - 1)] : 0.f;
+    }
+    __device__ __forceinline__ bool there(int mb, int p) const { return mb * 16 + p * ROWS + r0 < rows; }
+    __device__ __forceinline__ void fetch(int mb, Residual& r) const
+    {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) { v[i] += x[i]; v[i + 4] += y[i]; }
-                } else for (int i = 0; i < 8; ++i) if (i < left) v[i] += p[i];
-            } else {
-                const bf16x8_t x = load8(static_cast<const uint16_t*>(a.residual) + from, left);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] += (float)x[i];
-            }
-        }
-        const size_t at = (size_t)(m + r) * a.ldo + n;
-        if (a.out32) {
-            float* p = static_cast<float*>(a.out) + at;
-            if (left >= 8) {
-                *reinterpret_cast<f32x4_any4*>(p) = f32x4_t{v[0], v[1], v[2], v[3]};
-                *reinterpret_cast<f32x4_any4*>(p + 4) = f32x4_t{v[4], v[5], v[6], v[7]};
-            } else for (int i = 0; i < 8; ++i) if (i < left) p[i] = v[i];
-        } else {
-            uint16_t* p = static_cast<uint16_t*>(a.out) + at;
-            const u32x4_t o = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
-            if (left >= 8) *reinterpret_cast<u32x4_any2*>(p) = o;
-            else for (int i = 0; i < 8; ++i) if (i < left) p[i] = (uint16_t)(o[i >> 1] >> (16 * (i & 1)));
+        for (int p = 0; p < PASSES; ++p) {
+            if (!there(mb, p) || left < 8) continue;
+            const char* const at = res_at + (res_off + (uint32_t)(mb * 16 + p * ROWS) * (uint32_t)a.ldr * (a.out32 ? 4u : 2u));
+            r.v[p][0] = *reinterpret_cast<const u32x4_any2*>(at);
+            if (a.out32) r.v[p][1] = *reinterpret_cast<const u32x4_any2*>(at + 16);
         }
     }
+    __device__ __forceinline__ void store(int mb, f32x4_t (&v)[NB], const Residual& res) const
+    {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            v[b] += bias[b];
+            if (ACT) activate<4>(a.act, v[b]);
+            *reinterpret_cast<f32x4_t*>(sums + (b % 2 ? write ^ 64u : write) + b / 2 * 128) = v[b];
+        }
+        wavefront_lds_order();
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            const uint32_t from = (read ^ (p * ROWS & 7) * 16) + p * ROWS * COLS * 4;
+            f32x4_t lo = *reinterpret_cast<const f32x4_t*>(sums + from), hi = *reinterpret_cast<const f32x4_t*>(sums + (from ^ 16u));
+            if (!there(mb, p) || left < 8) continue;
+            if (a.residual) {
+                const u32x4_t r = res.v[p][0];
+                if (a.out32) {
+                    lo += __builtin_bit_cast(f32x4_t, r);
+                    hi += __builtin_bit_cast(f32x4_t, res.v[p][1]);
+                } else {
+                    lo += f32x4_t{bf16_lo(r[0]), bf16_hi(r[0]), bf16_lo(r[1]), bf16_hi(r[1])};
+                    hi += f32x4_t{bf16_lo(r[2]), bf16_hi(r[2]), bf16_lo(r[3]), bf16_hi(r[3])};
+                }
+            }
+            char* const to = out_at + (out_off + (uint32_t)(mb * 16 + p * ROWS) * (uint32_t)a.ldo * (a.out32 ? 4u : 2u));
+            if (a.out32) {
+                *reinterpret_cast<f32x4_any4*>(to) = lo;
+                *reinterpret_cast<f32x4_any4*>(to + 16) = hi;
+            } else *reinterpret_cast<u32x4_any2*>(to) = u32x4_t{pack_bf16x2(lo[0], lo[1]), pack_bf16x2(lo[2], lo[3]), pack_bf16x2(hi[0], hi[1]), pack_bf16x2(hi[2], hi[3])};
+        }
+        if (left > 0 && left < 8) {   // the last columns, one by one
+#pragma unroll 1
+            for (int p = 0; p < PASSES; ++p) {
+                if (!there(mb, p)) break;
+                const uint32_t from = (read ^ (p * ROWS & 7) * 16) + p * ROWS * COLS * 4, row = mb * 16 + p * ROWS;
+                const char* const r = res_at + (res_off + row * (uint32_t)a.ldr * (a.out32 ? 4u : 2u));
+                char* const to = out_at + (out_off + row * (uint32_t)a.ldo * (a.out32 ? 4u : 2u));
+#pragma unroll 1
+                for (int i = 0; i < left; ++i) {
+                    float x = *reinterpret_cast<const float*>(sums + ((from ^ (i >> 2) * 16u) + (i & 3) * 4));
+                    if (a.residual) x += a.out32 ? reinterpret_cast<const float*>(r)[i] : bf16_lo(reinterpret_cast<const uint16_t*>(r)[i]);
+                    if (a.out32) reinterpret_cast<float*>(to)[i] = x;
+                    else reinterpret_cast<uint16_t*>(to)[i] = (uint16_t)pack_bf16x2(x, 0.f);
+                }
+            }
+        }
+        wavefront_lds_order();
+    }
+};
+
+// v = acc[mb]; constants only, so that the accumulators stay in registers
+template <int B, int MB, int NB>
+__device__ __forceinline__ void row_of_blocks(int mb, const f32x4_t (&acc)[MB][NB], f32x4_t (&v)[NB])
+{
+    if (mb == B) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) v[nb] = acc[B][nb];
+    } else if constexpr (B + 1 < MB) row_of_blocks<B + 1, MB, NB>(mb, acc, v);
 }
 
-// RAGGED: the last K step is not whole
-template <int BM, int BN, int OCC, bool RAGGED>
+// RAGGED: the last K step is not whole.  ACT: there is an activation; a launch without one does not fetch the code of all of them (256 x 256
+// tiles: 3 us of 19)
+template <int BM, int BN, int SLOTS, int OCC, bool RAGGED, bool ACT>
 __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a)
 {
-    using C = TileCfg<BM, BN>;
+    using C = TileCfg<BM, BN, SLOTS>;
     constexpr int MB = C::MB, NB = C::NB, RPW = C::RPW, RX = C::RX;
     extern __shared__ uint4 lds4[];
     char* const lds = reinterpret_cast<char*>(lds4);
@@ -305,14 +627,21 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a)
             off[i] = ((uint32_t)row * (uint32_t)(i < RX ? a.ldx : a.ldw) + c * 8) * 2u;
         }
     };
+    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
     const auto issue = [&](int ks, int ring, int i) __attribute__((always_inline)) {
         const int j = wave + C::NW * (i < RX ? i : i - RX);
-        const char* src = (i < RX ? xi : wi) + ks * (C::KS * 2) + off[i];
-        if (RAGGED && ks == KT - 1 && ks * C::KS + ((j & 1) ? ld_c ^ 4 : ld_c) * 8 >= a.K) src = reinterpret_cast<const char*>(kZeros);
-        __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint4*>(src), reinterpret_cast<uint4*>(lds + ring * C::SLOT_BYTES + (i < RX ? 0 : BM * 128) + j * 1024), 16, 0, 0);
+        const char* const base = (i < RX ? xi : wi) + ks * (C::KS * 2);
+        const uint32_t to = lds_base + (uint32_t)(ring * C::SLOT_BYTES + (i < RX ? 0 : BM * 128) + j * 1024);
+        if (RAGGED && ks == KT - 1) {
+            const char* src = base + off[i];
+            if (ks * C::KS + ((j & 1) ? ld_c ^ 4 : ld_c) * 8 >= a.K) src = reinterpret_cast<const char*>(kZeros);
+            load_to_lds(to, src);
+        } else load_to_lds(to, base, off[i]);
     };
     const auto hand_over = [&]() __attribute__((always_inline)) {
-        __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0): this wavefront's loads have landed, its reads have returned
+        // this wavefront's loads into the next slot have landed (all but those into later ones), its reads have returned
+        constexpr int LATER = (SLOTS - 2) * RPW;
+        __builtin_amdgcn_s_waitcnt((LATER & 15) | ((LATER >> 4) << 14) | 0x0070);
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
@@ -334,23 +663,27 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a)
     int m0, n0, it = 0;
     if (!tile_at(0, m0, n0)) return;
     aim(m0, n0);
-    int ring = 0, ki = 1, next_m0 = m0, next_n0 = n0;   // ki: the K step whose loads start at the next hand-over
+    int ring = 0, ki = 0, next_m0 = m0, next_n0 = n0;   // ki: the K step whose loads start at the next hand-over
     bool more = true;                                    // there is a tile behind the one that is multiplied
-#pragma unroll
-    for (int i = 0; i < RPW; ++i) issue(0, 0, i);
-    hand_over();
-    // K step 1 (or the next tile's first one) starts as every later one does
     const auto advance = [&]() __attribute__((always_inline)) {
         if (ki == KT) {
             more = tile_at(it + 1, next_m0, next_n0);
-            if (more) aim(next_m0, next_n0);     // the last tile's loads go round to its own first K step, and are not used
+            if (more) aim(next_m0, next_n0);     // the last tile's loads go round to its own first K steps, and are not used
             ki = 0;
         }
     };
+#pragma unroll
+    for (int st = 0; st < SLOTS - 1; ++st) {
+#pragma unroll
+        for (int i = 0; i < RPW; ++i) issue(ki, st, i);
+        ++ki;
+    }
+    hand_over();
+    // the last slot's loads start as every later one's do
     advance();
 #pragma unroll
     for (int p = 0; p < C::TAIL; ++p)
-        if (C::load_at(p) >= 0) issue(ki, 1, C::load_at(p) < 0 ? 0 : C::load_at(p));
+        if (C::load_at(p) >= 0) issue(ki, SLOTS - 1, C::load_at(p) < 0 ? 0 : C::load_at(p));
 #pragma unroll
     for (int f = 0; f < MB + NB; ++f) frag(0, 0, f);
     for (;;) {
@@ -363,7 +696,7 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a)
         asm volatile("s_nop 7");
         SB();
         for (int kt = 0; kt < KT; ++kt) {
-            const int other = ring ^ 1;
+            const int other = ring == SLOTS - 1 ? 0 : ring + 1, last = ring == 0 ? SLOTS - 1 : ring - 1;
 #pragma unroll
             for (int p = 0; p < C::M; ++p) {
                 const int j = p / (MB * NB), q = p % (MB * NB), nb = q / MB, mb = (nb & 1) ? MB - 1 - q % MB : q % MB;
@@ -381,7 +714,7 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a)
                 }
                 if (p >= C::HO) {
                     if (C::load_at(p - C::HO) >= 0) issue(ki, ring, C::load_at(p - C::HO) < 0 ? 0 : C::load_at(p - C::HO));
-                } else if (C::load_at(p + C::TAIL) >= 0) issue(ki, other, C::load_at(p + C::TAIL) < 0 ? 0 : C::load_at(p + C::TAIL));
+                } else if (C::load_at(p + C::TAIL) >= 0) issue(ki, last, C::load_at(p + C::TAIL) < 0 ? 0 : C::load_at(p + C::TAIL));
                 SB();
             }
             ring = other;
@@ -390,25 +723,17 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a)
         asm volatile("s_nop 15");
         asm volatile("s_nop 15");
         SB();
-// A lane holds row (lane & 15) of each block and 4 consecutive columns of it.  A row of blocks at a time goes through LDS, so that a
-        // store carries whole pieces of a row and the code of the epilogue is there once.
-        char* const sums = lds + C::SLOTS * C::SLOT_BYTES + wave * C::SUM_BYTES;
-        const int n = n0 + wn * C::WTN + (lane % C::LANES) * 8;
-        float bias[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) bias[i] = a.bias && n + i < a.N ? a.bias[n + i] : 0.f;
+// A row of blocks at a time, in a loop with one body: every row with code of its own (80 KB) took 15 us of a launch to fetch.
+        const TileEpilogue<MB, C::WTN, ACT> e(a, lds + SLOTS * C::SLOT_BYTES + wave * C::SUM_BYTES, lane, m0 + wm * C::WTM, n0 + wn * C::WTN);
+        typename TileEpilogue<MB, C::WTN, ACT>::Residual ahead;
+        if (a.residual) e.fetch(0, ahead);
 #pragma unroll 1
         for (int mb = 0; mb < MB; ++mb) {
-#pragma unroll
-            for (int b = 0; b < MB; ++b)
-                if (b == mb) {
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb)
-                        *reinterpret_cast<f32x4_t*>(sums + fr * (NB * 64) + ((nb * 4 + kh) ^ (fr & 7)) * 16) = acc[b][nb];
-                }
-            wavefront_lds_order();
-            finish_rows<C::LANES>(a, sums, lane, m0 + wm * C::WTM + mb * 16, n, bias);
-            wavefront_lds_order();
+            const typename TileEpilogue<MB, C::WTN, ACT>::Residual res = ahead;
+            if (a.residual && mb + 1 < MB) e.fetch(mb + 1, ahead);
+            f32x4_t v[NB];
+            row_of_blocks<0, MB, NB>(mb, acc, v);
+            e.store(mb, v, res);
         }
         if (!more) break;
         m0 = next_m0;
@@ -418,26 +743,72 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a)
     __builtin_amdgcn_s_waitcnt(0x0f70);   // no load may land in LDS that is another workgroup's by then
 }
 
-template <int BM, int BN, int OCC, bool RAGGED>
-hipError_t launch_tiled_k(const LinearArgs& a, int n_cu, hipStream_t s)
+template <int BM, int BN, int SLOTS, int OCC, bool RAGGED, bool ACT>
+hipError_t launch_tiled_as(const LinearArgs& a, int n_cu, hipStream_t s)
 {
-    using C = TileCfg<BM, BN>;
+    using C = TileCfg<BM, BN, SLOTS>;
     static_assert(C::LDS_BYTES * OCC <= 160 * 1024, "LDS of a compute unit");
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&linear_tiled_kernel<BM, BN, OCC, RAGGED>), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS_BYTES);
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&linear_tiled_kernel<BM, BN, SLOTS, OCC, RAGGED, ACT>), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS_BYTES);
     if (e != hipSuccess) return e;
     const long long total = (long long)((a.R + BM - 1) / BM) * ((a.N + BN - 1) / BN);
     if (total > 0x3fffffffll) return hipErrorInvalidValue;
     // as few workgroups as it takes for as many rounds, the same number on every XCD
     const long long wgs = (long long)n_cu * OCC, rounds = (total + wgs - 1) / wgs;
     const int grid = (int)(((total + rounds - 1) / rounds + 7) / 8 * 8);
-    hipLaunchKernelGGL((linear_tiled_kernel<BM, BN, OCC, RAGGED>), dim3(grid), dim3(256), C::LDS_BYTES, s, a);
+    hipLaunchKernelGGL((linear_tiled_kernel<BM, BN, SLOTS, OCC, RAGGED, ACT>), dim3(grid), dim3(256), C::LDS_BYTES, s, a);
     return hipGetLastError();
 }
 
-template <int BM, int BN, int OCC>
+template <int BM, int BN, int SLOTS, int OCC>
 hipError_t launch_tiled(const LinearArgs& a, int n_cu, hipStream_t s)
 {
-    return a.K % TileCfg<BM, BN>::KS ? launch_tiled_k<BM, BN, OCC, true>(a, n_cu, s) : launch_tiled_k<BM, BN, OCC, false>(a, n_cu, s);
+    if (a.act == kActNone) return a.K % 64 ? launch_tiled_as<BM, BN, SLOTS, OCC, true, false>(a, n_cu, s) : launch_tiled_as<BM, BN, SLOTS, OCC, false, false>(a, n_cu, s);
+    return a.K % 64 ? launch_tiled_as<BM, BN, SLOTS, OCC, true, true>(a, n_cu, s) : launch_tiled_as<BM, BN, SLOTS, OCC, false, true>(a, n_cu, s);
+}
+
+// What a tile costs, us: `fixed` and, per K step, `alone` where most compute units have none, `full` where all have (power and
+// L2 are shared).  Fitted to launches of 256 x 256 to 16384 x 5120 results, K from 256 to 8192.
+struct Tiling { int rows, cols, slots, per_cu; double alone, full, fixed; };
+constexpr Tiling kTilings[] = {
+    {256, 256, 2, 1, 1.02, 1.40, 12.0}, {256, 192, 2, 1, 0.84, 1.13, 9.5}, {192, 256, 2, 1, 0.85, 1.13, 9.0},
+    {128, 128, 4, 1, 0.33, 0.44, 5.0}, {64, 64, 4, 2, 0.15, 0.37, 1.2}};
+
+// a launch lasts as many rounds as its busiest compute unit has tiles
+double tiled_us(const Tiling& t, const LinearArgs& a, int n_cu)
+{
+    const double tiles = (double)((a.R + t.rows - 1) / t.rows) * ((a.N + t.cols - 1) / t.cols), slots = (double)n_cu * t.per_cu;
+    const double rounds = std::ceil(tiles / slots), fill = tiles / (rounds * slots);
+    return rounds * ((a.K + 63) / 64 * (t.alone + (t.full - t.alone) * fill) + t.fixed);
+}
+
+hipError_t launch_tiled_best(const LinearArgs& a, int n_cu, hipStream_t s)
+{
+    int best = 0;
+    double us = 0.0;
+    for (int i = 0; i < (int)(sizeof kTilings / sizeof *kTilings); ++i) {
+        const double t = tiled_us(kTilings[i], a, n_cu);
+        if (kTilings[i].slots <= (a.K + 63) / 64 && (us == 0.0 || t < us)) { us = t; best = i; }
+    }
+    switch (best) {
+    case 0: return launch_tiled<256, 256, 2, 1>(a, n_cu, s);
+    case 1: return launch_tiled<256, 192, 2, 1>(a, n_cu, s);
+    case 2: return launch_tiled<192, 256, 2, 1>(a, n_cu, s);
+    case 3: return launch_tiled<128, 128, 4, 1>(a, n_cu, s);
+    default: return launch_tiled<64, 64, 4, 2>(a, n_cu, s);
+    }
+}
+
+// The largest of the split tiles that still gives enough compute units work: half of them, three quarters where every tile also takes fp32
+// weights apart.
+hipError_t launch_split_best(const LinearArgs& a, int n_cu, hipStream_t s)
+{
+    const auto tiles = [&](int mb, int nb) { return (double)((a.R + mb * 16 - 1) / (mb * 16)) * ((a.N + nb * 16 - 1) / (nb * 16)); };
+    const double enough = a.w32 ? 0.75 * n_cu : 0.5 * n_cu;
+    if (a.R > 32 && tiles(4, 2) >= 2 * n_cu) return launch_split<4, 2, 4>(a, s);
+    if (a.R > 32 && tiles(4, 2) >= enough) return launch_split<4, 2, 8>(a, s);
+    if (a.R > 32 && tiles(4, 1) >= enough) return launch_split<4, 1, 8>(a, s);
+    if (a.R > 16 && tiles(2, 1) >= enough) return launch_split<2, 1, 16>(a, s);
+    return launch_split<1, 1, 16>(a, s);
 }
 
 }  // namespace
@@ -446,17 +817,19 @@ hipError_t launch_linear(const LinearArgs& a, int n_cu, hipStream_t s)
 {
     if (a.R <= 0) return hipSuccess;
     if (a.N < 1 || a.K < 1) return hipErrorInvalidValue;
-    // the tiled kernel moves 16 bytes at a time
-    // (and is always one K step ahead: two at least)
-    const bool by_16 = !a.w32 && a.K > 64 && a.K % 8 == 0 && a.ldx % 8 == 0 && a.ldw % 8 == 0 && !((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w)) & 15);
-    if (by_16 && a.R > 64) {
-        const long long big = (long long)((a.R + 255) / 256) * ((a.N + 255) / 256);
-        if (big >= n_cu) return launch_tiled<256, 256, 1>(a, n_cu, s);
-        return launch_tiled<128, 128, 2>(a, n_cu, s);
+    const auto tiles = [&](int edge) { return (double)((a.R + edge - 1) / edge) * ((a.N + edge - 1) / edge); };
+    // Few blocks of 16 x 16 for a matrix instruction, and little to multiply.  Rows / split, us: 1, 16, 33 x 160 x 5120, fp32 weights, 3.1 / 8.6,
+    // 5.1 / 8.6, 6.5 / 8.7; 64, 256 x 128 x 4096 6.6 / 7.5, 17 / 9.1; bf16 weights, 1, 8 x 2048 x 1408 3.6 / 3.8, 7.6 / 3.9.
+    const double products = (double)a.R * a.N * a.K;
+    if ((products <= 40e6 && tiles(16) < n_cu / 2) || products <= 3e6) {
+        if (a.R <= 8) return launch_rows<1, 1>(a, s);
+        return a.R <= 16 ? launch_rows<4, 1>(a, s) : launch_rows<4, 2>(a, s);
     }
-    if (a.R <= 16) return launch_split<1, 1, 16>(a, s);
-    if (a.R <= 32) return launch_split<2, 1, 16>(a, s);
-    return launch_split<4, 2, 8>(a, s);
+    // The tiled kernels move 16 bytes at a time, and are a K step ahead at least.  Of few tiles, each a compute unit's, a long K is better shared:
+    // tiled / split, us: 64 x 1536 x 5120 17 / 9.7; 64 x 5120 x 2048 9.8 / 9.5, 256 x 2048 x 2048 9.6 / 12.
+    const bool by_16 = !a.w32 && a.K > 64 && a.K % 8 == 0 && a.ldx % 8 == 0 && a.ldw % 8 == 0 && !((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w)) & 15);
+    if (by_16 && a.R > 64 && tiles(64) >= n_cu / 4) return launch_tiled_best(a, n_cu, s);
+    return launch_split_best(a, n_cu, s);
 }
 
 }  // namespace moe_ep
