@@ -5,6 +5,7 @@
 //
 // fp32 weights are three bf16 numbers each, 8 mantissa bits at a time cut off the top (24 together: all of them), and a product is three
 // matrix instructions: as exact as fp32 multiplications at 5 times their rate.
+#include <atomic>
 #include <cmath>
 #include <type_traits>
 
@@ -197,6 +198,18 @@ __device__ __forceinline__ u32x4_t load_part(const T* p, int left)
         else v[i] = __float_as_uint(p[i]);
     }
     return v;
+}
+
+// The kernel may ask for `bytes` of LDS: told once per device, of the first 64
+template <class K>
+hipError_t allow_lds(K* kernel, int bytes, std::atomic<uint64_t>& told)
+{
+    int device = 0;
+    hipError_t e = hipGetDevice(&device);
+    if (e != hipSuccess || (device < 64 && (told.load(std::memory_order_relaxed) >> device & 1))) return e;
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == hipSuccess && device < 64) told.fetch_or(1ull << device, std::memory_order_relaxed);
+    return e;
 }
 
 // ---- a few rows: no matrix instruction is full
@@ -428,7 +441,8 @@ hipError_t launch_split_as(const LinearArgs& a, unsigned grid, hipStream_t s)
 {
     constexpr int bytes = WAVES * SplitCfg<MB, NB, W32>::BYTES;
     static_assert(bytes <= 160 * 1024, "LDS of a compute unit");
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&linear_split_kernel<MB, NB, WAVES, W32>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    static std::atomic<uint64_t> told{0};
+    const hipError_t e = allow_lds(&linear_split_kernel<MB, NB, WAVES, W32>, bytes, told);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((linear_split_kernel<MB, NB, WAVES, W32>), dim3(grid), dim3(WAVES * 64), bytes, s, a);
     return hipGetLastError();
@@ -748,7 +762,8 @@ hipError_t launch_tiled_as(const LinearArgs& a, int n_cu, hipStream_t s)
 {
     using C = TileCfg<BM, BN, SLOTS>;
     static_assert(C::LDS_BYTES * OCC <= 160 * 1024, "LDS of a compute unit");
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&linear_tiled_kernel<BM, BN, SLOTS, OCC, RAGGED, ACT>), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS_BYTES);
+    static std::atomic<uint64_t> told{0};
+    const hipError_t e = allow_lds(&linear_tiled_kernel<BM, BN, SLOTS, OCC, RAGGED, ACT>, C::LDS_BYTES, told);
     if (e != hipSuccess) return e;
     const long long total = (long long)((a.R + BM - 1) / BM) * ((a.N + BN - 1) / BN);
     if (total > 0x3fffffffll) return hipErrorInvalidValue;
