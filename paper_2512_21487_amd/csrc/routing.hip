@@ -17,24 +17,47 @@ constexpr int kRtExperts = 512, kRtTopK = 64;
 constexpr int kRtLaneExperts = kRtExperts / 64;
 constexpr int kRtFewTokens = 2048;   // 16 lanes per token up to here: more wavefronts, and shorter ones
 
-__device__ __forceinline__ double wave_max(double x)
+// the value of the lane that row_exchange names, of wider types
+template <int CTRL>
+__device__ __forceinline__ float exchange(float x) { return __int_as_float(row_exchange<CTRL>(__float_as_int(x))); }
+template <int CTRL>
+__device__ __forceinline__ int exchange(int x) { return row_exchange<CTRL>(x); }
+template <int CTRL>
+__device__ __forceinline__ double exchange(double x)
 {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) x = fmax(x, __shfl_xor(x, d, 64));
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = (uint32_t)row_exchange<CTRL>((int)(uint32_t)u), hi = (uint32_t)row_exchange<CTRL>((int)(u >> 32));
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// f over n lanes (a power of two up to 16) of every n: neighbours, pairs, then mirrors
+template <class T, class F>
+__device__ __forceinline__ T over_lanes(T x, int n, F f)
+{
+    if (n > 1) x = f(x, exchange<0xB1>(x));
+    if (n > 2) x = f(x, exchange<0x4E>(x));
+    if (n > 4) x = f(x, exchange<0x141>(x));
+    if (n > 8) x = f(x, exchange<0x140>(x));
     return x;
 }
-__device__ __forceinline__ double wave_sum(double x)
+// f over the wavefront: its rows of 16 lanes, then what their first lanes have
+template <class T>
+__device__ __forceinline__ T of_lane(T x, int lane)
 {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d, 64);
-    return x;
+    if constexpr (sizeof(T) == 8) {
+        const uint64_t u = __builtin_bit_cast(uint64_t, x);
+        const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)u, lane), hi = __builtin_amdgcn_readlane((uint32_t)(u >> 32), lane);
+        return __builtin_bit_cast(T, (uint64_t)hi << 32 | lo);
+    } else return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
 }
-__device__ __forceinline__ int wave_min(int x)
+template <class T, class F>
+__device__ __forceinline__ T over_wave(T x, F f)
 {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) x = min(x, __shfl_xor(x, d, 64));
-    return x;
+    x = over_lanes(x, 16, f);
+    return f(f(of_lane(x, 0), of_lane(x, 16)), f(of_lane(x, 32), of_lane(x, 48)));
 }
+struct Most { template <class T> __device__ __forceinline__ T operator()(T a, T b) const { return a > b ? a : b; } };
+struct Least { template <class T> __device__ __forceinline__ T operator()(T a, T b) const { return a < b ? a : b; } };
+struct Plus { template <class T> __device__ __forceinline__ T operator()(T a, T b) const { return a + b; } };
 
 // a score as the rule reads it: -inf for an expert that is not there (NaN, -inf or the type's lowest value), +inf as the largest number
 __device__ __forceinline__ float read_score(bool bf16, const void* row, int e)
@@ -59,84 +82,99 @@ __device__ __forceinline__ float slot_weight(const Weights& r, float s, bool ful
     return r.renorm ? expf(s - best_chosen) : expf(s - top) / total;
 }
 
-// One token by one wavefront, everything in double.  c: E doubles of LDS; slot_e: top_k integers of LDS.
+// One token by one wavefront, everything in double.  c: E doubles of LDS; slot_e: top_k integers of LDS.  In route_kernel a launch waits for the
+// few tokens that come here: no exchange over the wavefront goes through LDS.
 __device__ __forceinline__ void route_token(const RouteArgs& a, long long t, int lane, double* c, int* slot_e)
 {
     const int E = a.E, k = a.k, G = a.groups, S = E / G;
+    const double none = -__builtin_inf();
     const char* const row = static_cast<const char*>(a.scores) + t * a.stride * (a.bf16 ? 2 : 4);
     const bool live = !a.token_mask || a.token_mask[t] != 0;
-    float s[kRtLaneExperts];
-    double key[kRtLaneExperts];
-    double top = -__builtin_inf();
+    const bool by_value = a.bias != nullptr, group_value = by_value || a.group_top2;
+    float s[kRtLaneExperts], b[kRtLaneExperts];
+    double p[kRtLaneExperts], key[kRtLaneExperts];
+    float top = -__builtin_inff();
 #pragma unroll
     for (int i = 0; i < kRtLaneExperts; ++i) {
         const int e = lane + 64 * i;
         s[i] = -__builtin_inff();
+        b[i] = 0.f;
+        if (64 * i >= E) continue;
         if (live && e < E) {
-            const float b = a.bias ? a.bias[e] : 0.f;
-            if (b > -__builtin_inff()) s[i] = read_score(a.bf16, row, e);
+            b[i] = by_value ? a.bias[e] : 0.f;
+            if (b[i] > -__builtin_inff()) s[i] = read_score(a.bf16, row, e);
         }
-        top = fmax(top, (double)s[i]);
+        top = fmaxf(top, s[i]);
     }
-    top = wave_max(top);
-    const bool any = top > -__builtin_inf();
+    top = over_wave(top, Most());
     double sum = 0.0;
-    if (!a.sigmoid) {
+    if (!a.sigmoid && (group_value || !a.renorm)) {
 #pragma unroll
-        for (int i = 0; i < kRtLaneExperts; ++i) sum += s[i] > -__builtin_inff() ? exp((double)s[i] - top) : 0.0;
-        sum = wave_sum(sum);
+        for (int i = 0; i < kRtLaneExperts; ++i) {
+            p[i] = 0.0;
+            if (64 * i < E && s[i] > -__builtin_inff()) p[i] = exp((double)s[i] - (double)top);
+            sum += p[i];
+        }
+        sum = over_wave(sum, Plus());
     }
     // c, or s where its order is c's
-    const bool by_value = a.bias != nullptr, group_value = by_value || a.group_top2;
 #pragma unroll
     for (int i = 0; i < kRtLaneExperts; ++i) {
-        const int e = lane + 64 * i;
-        key[i] = -__builtin_inf();
-        double v = -__builtin_inf();
+        key[i] = none;
+        if (64 * i >= E) continue;
+        double v = none;
         if (s[i] > -__builtin_inff()) {
             v = s[i];
-            if (group_value) v = a.sigmoid ? 1.0 / (1.0 + exp(-(double)s[i])) : exp((double)s[i] - top) / sum;
-            if (by_value) v += (double)a.bias[e];
+            if (group_value) v = a.sigmoid ? 1.0 / (1.0 + exp(-(double)s[i])) : p[i] / sum;
+            v += (double)b[i];
             key[i] = by_value ? v : (double)s[i];
         }
-        if (G > 1 && e < E) c[e] = v;
+        if (G > 1 && lane + 64 * i < E) c[lane + 64 * i] = v;
     }
     if (G > 1) {
         wavefront_lds_order();
-        double value = -__builtin_inf();
-        if (lane < G) {
-            double m1 = -__builtin_inf(), m2 = -__builtin_inf();
-            for (int i = 0; i < S; ++i) {
-                const double v = c[lane * S + i];
-                if (v > m1) { m2 = m1; m1 = v; } else m2 = fmax(m2, v);
-            }
-            value = a.group_top2 && m2 > -__builtin_inf() ? m1 + m2 : m1;
-        }
+        // P lanes per group, a power of two up to 16
+        const int P = G > 32 ? 1 : G > 16 ? 2 : G > 8 ? 4 : G > 4 ? 8 : 16, g = lane / P;
+        double m1 = none, m2 = none;
+        const auto take = [&](double v1, double v2) {
+            const double low = v1 < m1 ? v1 : m1, high = v2 > m2 ? v2 : m2;
+            m1 = v1 > m1 ? v1 : m1;
+            m2 = low > high ? low : high;
+        };
+        if (g < G)
+            for (int i = lane % P; i < S; i += P) take(c[g * S + i], none);
+        if (P > 1) take(exchange<0xB1>(m1), exchange<0xB1>(m2));
+        if (P > 2) take(exchange<0x4E>(m1), exchange<0x4E>(m2));
+        if (P > 4) take(exchange<0x141>(m1), exchange<0x141>(m2));
+        if (P > 8) take(exchange<0x140>(m1), exchange<0x140>(m2));
         wavefront_lds_order();
+        const double value = g < G ? a.group_top2 && m2 > none ? m1 + m2 : m1 : none;
         int ahead = 0;
-        for (int g = 0; g < G; ++g) {
-            const double other = __shfl(value, g, 64);
-            ahead += other > value || (other == value && g < lane);
+        for (int h = 0; h < G; ++h) {
+            const double other = of_lane(value, h * P);
+            ahead += other > value || (other == value && h < g);
         }
-        const unsigned long long kept = __ballot(lane < G && value > -__builtin_inf() && ahead < a.top_groups);
+        const unsigned long long kept = __ballot(value > none && ahead < a.top_groups);   // a group's P lanes alike
 #pragma unroll
         for (int i = 0; i < kRtLaneExperts; ++i) {
             const int e = lane + 64 * i;
-            if (e < E && !((kept >> (e / S)) & 1)) key[i] = -__builtin_inf();
+            if (e < E && !((kept >> (e / S * P)) & 1)) key[i] = none;
         }
     }
     for (int r = 0; r < k; ++r) {
         double best = key[0];
 #pragma unroll
-        for (int i = 1; i < kRtLaneExperts; ++i) best = fmax(best, key[i]);
-        best = wave_max(best);
+        for (int i = 1; i < kRtLaneExperts; ++i)
+            if (64 * i < E) best = key[i] > best ? key[i] : best;
+        best = over_wave(best, Most());
         int e = INT_MAX;
-        if (best > -__builtin_inf()) {
+        if (best > none) {
 #pragma unroll
-            for (int i = kRtLaneExperts - 1; i >= 0; --i) e = key[i] == best ? lane + 64 * i : e;
-            e = wave_min(e);
+            for (int i = kRtLaneExperts - 1; i >= 0; --i)
+                if (64 * i < E) e = key[i] == best ? lane + 64 * i : e;
+            e = over_wave(e, Least());
 #pragma unroll
-            for (int i = 0; i < kRtLaneExperts; ++i) key[i] = e == lane + 64 * i ? -__builtin_inf() : key[i];
+            for (int i = 0; i < kRtLaneExperts; ++i) key[i] = e == lane + 64 * i ? none : key[i];
         }
         if (lane == 0) slot_e[r] = e == INT_MAX ? -1 : e;
     }
@@ -145,15 +183,11 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, long long t, int
     wavefront_lds_order();
     const bool full = e >= 0;
     const float se = full ? read_score(a.bf16, row, e) : -__builtin_inff();
-    float best_chosen = se;
-#pragma unroll
-    for (int d = 32; d; d >>= 1) best_chosen = fmaxf(best_chosen, __shfl_xor(best_chosen, d, 64));
+    const float best_chosen = over_wave(se, Most());
     const Weights r{a.sigmoid, a.renorm, a.scale};
-    float w = slot_weight(r, se, full, best_chosen, any ? (float)top : 0.f, (float)sum);
+    float w = slot_weight(r, se, full, best_chosen, top, (float)sum);
     if (a.renorm) {
-        float total = w;
-#pragma unroll
-        for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d, 64);
+        const float total = over_wave(w, Plus());
         w = total > 0.f ? w / total : 0.f;
     }
     if (lane < k) {
@@ -166,15 +200,14 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, long long t, int
 
 // an expert as one number: its value's order (gate.h) in the upper bits, then the lower expert first; positive doubles that are no NaN have the
 // order of their bits, and the f64 maximum and minimum run at the rate of fp32
-__device__ __forceinline__ double ranked(float v, int e)
+__device__ __forceinline__ double ranked(float v, int behind)   // behind: kRtExperts - 1 - expert
 {
-    const uint32_t key = v > -__builtin_inff() ? order_key(v) : 0u;
-    const uint64_t bits = (uint64_t)(key >> 2) << 32 | (key ? key << 30 | (uint32_t)(kRtExperts - 1 - e) : 0u);
-    return __builtin_bit_cast(double, bits);
+    const uint32_t u = __float_as_uint(v + 0.0f), key = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);   // v is no NaN
+    return __builtin_bit_cast(double, (uint64_t)(key >> 2) << 32 | (key << 30 | (uint32_t)behind));
 }
-__device__ __forceinline__ bool ranked_none(double x) { return __builtin_bit_cast(uint64_t, x) == 0; }
-__device__ __forceinline__ int ranked_expert(double x) { return kRtExperts - 1 - (int)(__builtin_bit_cast(uint64_t, x) & (kRtExperts - 1)); }
 __device__ __forceinline__ float ranked_value(double x) { return key_score((uint32_t)(__builtin_bit_cast(uint64_t, x) >> 30)); }
+__device__ __forceinline__ bool ranked_none(double x) { return (uint32_t)(__builtin_bit_cast(uint64_t, x) >> 32) <= 0x007fffffu >> 2; }   // -inf, or no expert at all
+__device__ __forceinline__ int ranked_expert(double x) { return kRtExperts - 1 - (int)(__builtin_bit_cast(uint64_t, x) & (kRtExperts - 1)); }
 
 __device__ __forceinline__ double larger(double a, double b)
 {
@@ -220,15 +253,6 @@ __device__ __forceinline__ void merge(double (&a)[N], const double (&b)[N])
         for (int i = 0; i < N; ++i)
             if (!(i & d)) in_order(a[i], a[i + d]);
 }
-template <int CTRL>
-__device__ __forceinline__ float exchange(float x) { return __int_as_float(row_exchange<CTRL>(__float_as_int(x))); }
-template <int CTRL>
-__device__ __forceinline__ double exchange(double x)
-{
-    const uint64_t u = __builtin_bit_cast(uint64_t, x);
-    const uint32_t lo = (uint32_t)row_exchange<CTRL>((int)(uint32_t)u), hi = (uint32_t)row_exchange<CTRL>((int)(u >> 32));
-    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-}
 template <int CTRL, int N>
 __device__ __forceinline__ void merge_lanes(double (&a)[N])
 {
@@ -237,22 +261,11 @@ __device__ __forceinline__ void merge_lanes(double (&a)[N])
     for (int i = 0; i < N; ++i) b[i] = exchange<CTRL>(a[i]);
     merge(a, b);
 }
-// over the first n (a power of two) lanes of every n: neighbours, pairs, then mirrors
-template <class F>
-__device__ __forceinline__ float over_lanes(float x, int n, F f)
-{
-    if (n > 1) x = f(x, exchange<0xB1>(x));
-    if (n > 2) x = f(x, exchange<0x4E>(x));
-    if (n > 4) x = f(x, exchange<0x141>(x));
-    if (n > 8) x = f(x, exchange<0x140>(x));
-    return x;
-}
-
 // A token is LANES lanes', each with REGS of its experts: of one group those of a group's lanes, VEC consecutive ones at a time.  The K
 // best of a lane are sorted in registers, and the lanes' lists merged pair by pair: no round waits for another.  What bounds it is the
 // instructions, about 50 a token (8 lanes, 32 experts a lane), and the scores' bytes close behind.
-template <int LANES, int REGS, int K, int VEC>
-__global__ __launch_bounds__(256, REGS * K <= 256 ? 4 : 3) void route_kernel(RouteArgs a)
+template <int LANES, int REGS, int K, int VEC, bool BIASED>
+__global__ __launch_bounds__(256, !BIASED || REGS < 32 ? REGS * K <= 256 ? 4 : 3 : 2) void route_kernel(RouteArgs a)
 {
     static_assert(K <= LANES && REGS % VEC == 0 && (REGS % K == 0 || REGS < K), "a slot per lane");
     __shared__ double s_c[4][kRtExperts];
@@ -293,60 +306,57 @@ __global__ __launch_bounds__(256, REGS * K <= 256 ? 4 : 3) void route_kernel(Rou
             } else s[r] = m < S ? row[m] : __uint_as_float(~0u);
         }
     }
-    const bool by_value = a.bias != nullptr, group_value = by_value || a.group_top2;
+    constexpr bool by_value = BIASED;
+    const bool group_value = by_value || a.group_top2;
     const float lowest = live ? a.bf16 ? __uint_as_float(0xff7f0000u) : -__FLT_MAX__ : __builtin_inff();
-    if (by_value) {
 #pragma unroll
-        for (int r = 0; r < REGS; ++r) {
-            const int m = first + r / VEC * (LG * VEC) + r % VEC;
-            v[r] = m < S ? a.bias[g * S + m] : none;
+    for (int r = 0; r < REGS; ++r) s[r] = s[r] > lowest ? fminf(s[r], __FLT_MAX__) : none;
+    if (by_value) {
+        const float* const bias = a.bias + g * S;
+        typedef float v4 __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+        for (int r = 0; r < REGS; r += VEC) {
+            const int m = first + r / VEC * (LG * VEC);
+            if constexpr (VEC == 4) {
+                v4 x = {none, none, none, none};
+                if (m < S) x = *reinterpret_cast<const v4*>(bias + m);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[r + j] = x[j];
+            } else v[r] = m < S ? bias[m] : none;
         }
 #pragma unroll
-        for (int r = 0; r < REGS; ++r) s[r] = s[r] > lowest && v[r] > none ? fminf(s[r], __FLT_MAX__) : none;
-    } else {
-#pragma unroll
-        for (int r = 0; r < REGS; ++r) s[r] = s[r] > lowest ? fminf(s[r], __FLT_MAX__) : none;
+        for (int r = 0; r < REGS; ++r) s[r] = v[r] > none ? s[r] : none;
     }
-    const auto most = [](float x, float y) { return fmaxf(x, y); };
-    const auto plus = [](float x, float y) { return x + y; };
     float top = 0.f, total = 0.f;
     if (!a.sigmoid && (group_value || !a.renorm)) {
         top = s[0];
 #pragma unroll
         for (int r = 1; r < REGS; ++r) top = fmaxf(top, s[r]);
-        top = over_lanes(top, LANES, most);
+        top = over_lanes(top, LANES, Most());
         top = top > none ? top : 0.f;
+        float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int r = 0; r < REGS; ++r) part[r & 3] += __builtin_amdgcn_exp2f((s[r] - top) * 1.4426950408889634f);
+        total = over_lanes((part[0] + part[1]) + (part[2] + part[3]), LANES, Plus());
     }
-    // v: p, then c; s itself where its order is asked for
-    if (group_value || (!a.sigmoid && !a.renorm)) {
-        float p[REGS];
+    // v: c; s itself where its order is asked for
+    if (group_value) {
+        const float by = total > 0.f ? __builtin_amdgcn_rcpf(total) : 0.f;
 #pragma unroll
         for (int r = 0; r < REGS; ++r) {
-            if (a.sigmoid) p[r] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s[r] * -1.4426950408889634f));
-            else p[r] = __builtin_amdgcn_exp2f((s[r] - top) * 1.4426950408889634f);
+            const float p = a.sigmoid ? __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s[r] * -1.4426950408889634f))
+                                      : __builtin_amdgcn_exp2f((s[r] - top) * 1.4426950408889634f) * by;
+            v[r] = s[r] > none ? by_value ? p + v[r] : p : none;
         }
-        if (!a.sigmoid) {
-            float part[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int r = 0; r < REGS; ++r) part[r & 3] += p[r];
-            total = over_lanes((part[0] + part[1]) + (part[2] + part[3]), LANES, plus);
-        }
-        if (group_value) {
-            const float by = a.sigmoid ? 1.0f : total > 0.f ? __builtin_amdgcn_rcpf(total) : 0.f;
-#pragma unroll
-            for (int r = 0; r < REGS; ++r) {
-                const float c = by_value ? fmaf(p[r], by, v[r]) : p[r] * by;
-                v[r] = s[r] > none ? c : none;
-            }
-        }
-    }
-    if (!group_value) {
+    } else {
 #pragma unroll
         for (int r = 0; r < REGS; ++r) v[r] = s[r];
     }
-    // two values that close may be in the other order: p is off by less than 2^-20, c by its own rounding too
-    const auto close = [=](float x, float y) { return x > none && y > none && !(fabsf(x - y) > 0x1p-19f + 0x1p-22f * fmaxf(fabsf(x), fabsf(y))); };
-    bool unsure = false, kept = true;
+    // Two values that close may be in the other order.  p is off by up to a step or two of exp2 and the reciprocal (2^-22 of p <= 1 together), where it is a
+    // softmax by its sum's rounding too (2^-21); c by half a step of its own.  Twice that.
+    const float slack = a.sigmoid ? 0x1p-20f : 0x1p-19f;
+    const auto close = [=](float x, float y) { return x > none && y > none && !(fabsf(x - y) > slack + 0x1p-22f * fmaxf(fabsf(x), fabsf(y))); };
+    bool unsure = false;
     if (G > 1) {
         float m1 = v[0], m2 = none;
 #pragma unroll
@@ -366,28 +376,32 @@ __global__ __launch_bounds__(256, REGS * K <= 256 ? 4 : 3) void route_kernel(Rou
         for (int h = 0; h < G; ++h) {
             const float other = __shfl(value, (lane & ~(LANES - 1)) + h * LG, 64);
             ahead += other > value || (other == value && h < g);
-            unsure = unsure || (group_value && h != g && close(other, value));
         }
-        kept = m1 > none && ahead < a.top_groups;
+        const bool stays = ahead < a.top_groups;   // (of a group without an expert every value says so)
+        // an order hangs on the last group that stays and the first that does not
+        if (group_value) unsure = close(over_lanes(stays ? value : __builtin_inff(), LANES, Least()), over_lanes(stays ? none : value, LANES, Most()));
+        if (!stays) {
+#pragma unroll
+            for (int r = 0; r < REGS; ++r) v[r] = s[r] = none;
+        }
     }
     // without a bias experts are in the order of s
+    if (!by_value) {
+#pragma unroll
+        for (int r = 0; r < REGS; ++r) v[r] = s[r];
+    }
     double list[K];
+    const int behind = kRtExperts - 1 - (g * S + first);
     if constexpr (REGS <= K) {
 #pragma unroll
-        for (int r = 0; r < K; ++r) {
-            const int m = first + r / VEC * (LG * VEC) + r % VEC;
-            list[r] = r < REGS ? ranked(kept ? by_value ? v[r < REGS ? r : 0] : s[r < REGS ? r : 0] : none, g * S + m) : 0.0;
-        }
+        for (int r = 0; r < K; ++r) list[r] = r < REGS ? ranked(v[r < REGS ? r : 0], behind - (r / VEC * (LG * VEC) + r % VEC)) : 0.0;
         sort(list);
     } else {
 #pragma unroll
         for (int b = 0; b < REGS; b += K) {
             double next[K];
 #pragma unroll
-            for (int r = 0; r < K; ++r) {
-                const int m = first + (b + r) / VEC * (LG * VEC) + (b + r) % VEC;
-                next[r] = ranked(kept ? by_value ? v[b + r] : s[b + r] : none, g * S + m);
-            }
+            for (int r = 0; r < K; ++r) next[r] = ranked(v[b + r], behind - ((b + r) / VEC * (LG * VEC) + (b + r) % VEC));
             sort(next);
             if (b == 0) {
 #pragma unroll
@@ -400,52 +414,92 @@ __global__ __launch_bounds__(256, REGS * K <= 256 ? 4 : 3) void route_kernel(Rou
     merge_lanes<0x141>(list);
     if (LANES > 8) merge_lanes<0x140>(list);
 
-    // a slot per lane
+    // a slot per lane, up to K: those from k on may still move up
     double mine = 0.0;
 #pragma unroll
     for (int i = 0; i < K; ++i) mine = sub == i ? list[i] : mine;
-    const bool full = sub < k && !ranked_none(mine);
-    const int e = full ? ranked_expert(mine) : -1;
+    bool full = sub < K && !ranked_none(mine);
+    int e = full ? ranked_expert(mine) : -1, place = sub;
+    const auto score_of = [&](int expert) { return read_score(a.bf16, static_cast<const char*>(a.scores) + row_at * (a.bf16 ? 2 : 4), expert); };
     float se = none;
-    if (full) se = by_value ? read_score(a.bf16, static_cast<const char*>(a.scores) + row_at * (a.bf16 ? 2 : 4), e) : ranked_value(mine);
-    if (by_value) {
+    if (full) se = by_value ? score_of(e) : ranked_value(mine);
+    if constexpr (by_value) {
         // an order hangs on neighbouring slots, unless they are alike, and on the last slot and every expert behind it
         const float value = full ? ranked_value(mine) : none, be = full ? a.bias[e] : 0.f;
-        const int next = lane + 1;
+        const int base = lane & ~(LANES - 1), next = lane + 1;
         const float nv = __shfl(value, next, 64), ns = __shfl(se, next, 64), nb = __shfl(be, next, 64);
-        const int ne = __shfl(e, next, 64);
-        unsure = unsure || (sub + 1 < k && full && ne >= 0 && close(value, nv) && !(se == ns && be == nb));
-        const int last = (lane & ~(LANES - 1)) + k - 1;
-        const float lv = __shfl(value, last, 64);
-        const int le = __shfl(e, last, 64);
+        bool near = sub < k && sub + 1 < K && close(value, nv) && !(se == ns && be == nb);
+        const float lv = __shfl(value, base + k - 1, 64);
+        const float line = lv > none ? lv - (slack + 0x1p-21f * fabsf(lv)) : __builtin_inff();   // a last slot that is empty has nobody behind it
         int found = 0;
 #pragma unroll
-        for (int r = 0; r < REGS; ++r) found += __popcll(__ballot(kept && le >= 0 && v[r] > none && (v[r] >= lv || close(v[r], lv))));
-        if (found > __popcll(__ballot(full && le >= 0))) {   // of some token of the wavefront: look which, and at those that are like the last one
-            const float ls = __shfl(se, last, 64), lb = __shfl(be, last, 64);
+        for (int r = 0; r < REGS; ++r) found += __popcll(__ballot(v[r] >= line));
+        double extra = 0.0;   // the best of those that are no slot
+        if (found > __popcll(__ballot(full && value >= line))) {   // of some token of the wavefront: look which, and not at those that are like its last slot
+            const int le = __shfl(e, base + K - 1, 64);
+            const float ls = __shfl(se, base + K - 1, 64), lb = __shfl(be, base + K - 1, 64);
+            int others = 0;
 #pragma unroll
             for (int r = 0; r < REGS; ++r) {
-                const int m = first + r / VEC * (LG * VEC) + r % VEC;
-                if (kept && le >= 0 && v[r] > none && close(v[r], lv) && g * S + m != le) {
-                    // chosen ones are close to the last slot only if a neighbour is: said above
-                    const bool behind = v[r] < lv || (v[r] == lv && g * S + m > le);
-                    unsure = unsure || (behind && !(s[r] == ls && a.bias[g * S + m] == lb));
-                }
+                const int at = behind - (r / VEC * (LG * VEC) + r % VEC), other = kRtExperts - 1 - at;
+                if (!(v[r] >= line)) continue;
+                const double x = ranked(v[r], at);
+                if (!(x < list[K - 1]) || (le >= 0 && other > le && a.bias[other] == lb && score_of(other) == ls)) continue;
+                extra = larger(extra, x);
+                ++others;
+            }
+            extra = over_lanes(extra, LANES, [](double x, double y) { return larger(x, y); });
+            others = over_lanes(others, LANES, Plus());
+            near = near || others > 0;
+            unsure = unsure || others > 1;
+        }
+        if (__ballot(near)) {
+            // The slots' own values in double, of all tokens at once, and their order; the one in front of which all K are gives way to the other.
+            // A softmax's sum stays in fp32: it is the same for both, so that the difference of two p is off by 2^-21 of itself.
+            const auto p_of = [&](float score) { return a.sigmoid ? 1.0 / (1.0 + exp(-(double)score)) : exp((double)score - (double)top) / (double)total; };
+            double p = 0.0, c = -__builtin_inf(), p_extra = 0.0, c_extra = -__builtin_inf();
+            if (full) { p = p_of(se); c = p + (double)be; }
+            int e_extra = -1, place_extra = 0;
+            float s_extra = none;
+            if (extra > 0.0) {
+                e_extra = ranked_expert(extra);
+                s_extra = score_of(e_extra);
+                p_extra = p_of(s_extra);
+                c_extra = p_extra + (double)a.bias[e_extra];
+            }
+            const auto ahead_of = [](double x, int ex, double y, int ey) { return x > y || (x == y && ex < ey); };
+            const auto unclear = [&](double px, double x, double py, double y) { return !a.sigmoid && px != py && fabs(x - y) <= 0x1p-20 * fabs(px - py); };
+            place = 0;
+#pragma unroll 1
+            for (int i = 0; i < K; ++i) {
+                const int oe = __shfl(e, base + i, 64);
+                const double op = __shfl(p, base + i, 64), oc = __shfl(c, base + i, 64);
+                if (oe < 0) continue;
+                place += !full || ahead_of(oc, oe, c, e);   // empty slots stay behind
+                place_extra += ahead_of(oc, oe, c_extra, e_extra);
+                unsure = unsure || (full && unclear(op, oc, p, c)) || (e_extra >= 0 && unclear(op, oc, p_extra, c_extra));
+            }
+            if (!full) place = sub;
+            else if (e_extra >= 0) {
+                place += ahead_of(c_extra, e_extra, c, e);
+                if (place == K) { e = e_extra; se = s_extra; place = place_extra; }
             }
         }
     }
+    full = full && place < k;
+    if (!full) se = none;
     const Weights rule{a.sigmoid, a.renorm, a.scale};
-    const float best_chosen = over_lanes(se, LANES, most);
+    const float best_chosen = over_lanes(se, LANES, Most());
     float w = slot_weight(rule, se, full, best_chosen, top, total);
     if (a.renorm) {
-        const float sum = over_lanes(w, LANES, plus);
+        const float sum = over_lanes(w, LANES, Plus());
         w = sum > 0.f ? w / sum : 0.f;
     }
     unsigned long long again = __ballot(unsure && there);
     constexpr unsigned long long TOKEN = (1ull << LANES) - 1ull;
-    if (there && sub < k && !((again >> (lane & ~(LANES - 1))) & TOKEN)) {
-        a.idx[t * k + sub] = e;
-        a.w[t * k + sub] = w * a.scale;
+    if (there && sub < K && place < k && !((again >> (lane & ~(LANES - 1))) & TOKEN)) {
+        a.idx[t * k + place] = full ? e : -1;
+        a.w[t * k + place] = w * a.scale;
     }
     while (again) {   // a token at a time, by the whole wavefront
         const int from = __builtin_ctzll(again) & ~(LANES - 1);
@@ -460,7 +514,9 @@ template <int LANES, int REGS, int K, int VEC>
 hipError_t launch(const RouteArgs& a, hipStream_t s)
 {
     const long long tokens = 4 * (64 / LANES);
-    hipLaunchKernelGGL((route_kernel<LANES, REGS, K, VEC>), dim3((unsigned)((a.T + tokens - 1) / tokens)), dim3(256), 0, s, a);
+    const dim3 grid((unsigned)((a.T + tokens - 1) / tokens));
+    if (a.bias) hipLaunchKernelGGL((route_kernel<LANES, REGS, K, VEC, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((route_kernel<LANES, REGS, K, VEC, false>), grid, dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
@@ -470,6 +526,8 @@ hipError_t launch_regs(const RouteArgs& a, int regs, hipStream_t s)
     if (regs <= 8) return launch<LANES, 8, K, VEC>(a, s);
     return regs <= 16 ? launch<LANES, 16, K, VEC>(a, s) : launch<LANES, 32, K, VEC>(a, s);
 }
+
+// ---- every shape
 
 __global__ __launch_bounds__(256) void route_exact_kernel(RouteArgs a)
 {
@@ -491,7 +549,7 @@ hipError_t launch_route(const RouteArgs& a, hipStream_t s)
     const int size = a.E / a.groups, vec = size % 4 == 0 ? 4 : 1;
     const auto regs = [&](int lanes) { return (size + lanes / a.groups * vec - 1) / (lanes / a.groups * vec) * vec; };
     if (groups_fit && a.k <= 16) {
-        if (a.k <= 8 && a.groups <= 8 && regs(8) <= 32 && a.T > kRtFewTokens)
+        if (a.k <= 8 && a.groups <= 8 && regs(8) <= (a.bias ? 16 : 32) && a.T > kRtFewTokens)
             return vec == 4 ? launch_regs<8, 8, 4>(a, regs(8), s) : launch_regs<8, 8, 1>(a, regs(8), s);
         if (regs(16) <= 32) {
             if (a.k <= 8) return vec == 4 ? launch_regs<16, 8, 4>(a, regs(16), s) : launch_regs<16, 8, 1>(a, regs(16), s);
