@@ -108,6 +108,7 @@ int moe_ep_create(const moe_ep_config *cfg, moe_ep_ctx **out_ctx);
  *               assignments to experts outside [local_begin, local_begin + n_local) are
  *               dropped without renormalising (they belong to another GPU).
  *               NaN / Inf scores are not supported.
+ *               (moe_ep_set_routing: other rules.)
  *   routed_w    bf16, device: for each local expert, contiguous, W_gate [H, M],
  *               W_up [H, M], W_down [M, H], all row-major (Sec. 3.1); experts contiguous.
  *               (A pointer that moe_ep_prepare_weights has seen is read from the context's
@@ -257,6 +258,15 @@ int moe_ep_validate_routing(const moe_ep_routing *rule, const char **why);
  */
 int moe_ep_route(const moe_ep_routing *rule, const void *scores, const float *bias, const uint8_t *token_mask,
                  int32_t n_tokens, int32_t *idx, float *w, void *stream, const char **why);
+
+/*
+ * The gate of a context by a rule: later moe_ep_forward and moe_ep_forward_dep choose and weigh experts as moe_ep_route does, instead of by the
+ * softmax over the top_k largest scores.  Their top_k must then be the rule's; the rule's n_experts and device are the context's, its top_k at most
+ * max_top_k, its scores fp32 without gaps (gate_logits).  Slots without an expert (idx -1) take no part in the layer: a token whose scores are all
+ * minus infinity gets the shared experts only, or zeros.  bias (fp32 [E], device memory, or NULL) is read by every forward and stays the caller's.
+ * rule NULL: as without this call.  moe_ep_forward_noalloc has no context, and no rule.
+ */
+int moe_ep_set_routing(moe_ep_ctx *ctx, const moe_ep_routing *rule, const float *bias);
 
 /*
  * Matrix product with an epilogue: out = act(x W^T + bias) + residual.  The gate's scores are one (fp32 weights and results), a dense

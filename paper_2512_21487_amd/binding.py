@@ -152,6 +152,8 @@ def load_library() -> ctypes.CDLL:
     lib.moe_ep_validate_routing.argtypes = [ctypes.POINTER(Routing), whyp]
     lib.moe_ep_route.restype = ctypes.c_int
     lib.moe_ep_route.argtypes = [ctypes.POINTER(Routing), vp, vp, vp, i32, vp, vp, vp, whyp]
+    lib.moe_ep_set_routing.restype = ctypes.c_int
+    lib.moe_ep_set_routing.argtypes = [vp, ctypes.POINTER(Routing), vp]
     lib.moe_ep_validate_linear.restype = ctypes.c_int
     lib.moe_ep_validate_linear.argtypes = [ctypes.POINTER(LinearConfig), whyp]
     lib.moe_ep_linear.restype = ctypes.c_int
@@ -550,6 +552,16 @@ class MoeEp:
         if rc != 0:
             raise MoeEpError(rc, self.last_error())
         self._last = (n_tokens, top_k, int(self._lib.moe_ep_last_chunks(self._ctx)), 1)
+        return rc
+
+    # -- moe_ep_set_routing -----------------------------------------------------------------
+    def set_routing(self, rule: Optional[Routing] = None, bias=None) -> int:
+        """Later forwards route by ``rule`` (None: as a new context); the context keeps ``bias`` alive."""
+        _check_vector(bias, "bias", self.cfg.n_experts, 4)
+        rc = self._lib.moe_ep_set_routing(self._ctx, ctypes.byref(rule) if rule is not None else None, _ptr(bias))
+        if rc != 0:
+            raise MoeEpError(rc, self.last_error())
+        self._routing_bias = bias
         return rc
 
     # -- moe_ep_prepare_weights / moe_ep_forget_weights -------------------------------------

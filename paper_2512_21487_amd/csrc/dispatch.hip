@@ -60,6 +60,23 @@ __global__ __launch_bounds__(kPermuteThreads) void dispatch_permute_kernel(
     }
 }
 
+// The masks of 64 tokens from the experts chosen for them (a routing rule of the caller's; the gate's own launch writes its masks itself).
+// -1, a slot that no expert was left for, is no local expert.
+__global__ __launch_bounds__(256) void dispatch_masks_kernel(const int32_t* __restrict__ idx, int Tn, int k, int e0, int El,
+                                                             unsigned long long* __restrict__ blk_mask)
+{
+    extern __shared__ unsigned long long smem[];
+    for (int e = threadIdx.x; e < El; e += 256) smem[e] = 0ull;
+    __syncthreads();
+    const int t0 = blockIdx.x * kTokPerBlock, n = min(kTokPerBlock, Tn - t0) * k;
+    for (int a = threadIdx.x; a < n; a += 256) {
+        const int chosen = idx[(size_t)t0 * k + a], e = chosen - e0;
+        if (chosen >= 0 && e >= 0 && e < El) atomicOr(&smem[e], 1ull << (a / k));
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < El; e += 256) blk_mask[(size_t)blockIdx.x * El + e] = smem[e];
+}
+
 // no tokens: the counts and their prefix sum are zeros
 __global__ void dispatch_empty_kernel(int El, int32_t* __restrict__ count, int32_t* __restrict__ offset)
 {
@@ -100,6 +117,13 @@ hipError_t launch_dispatch(const int32_t* idx, const unsigned long long* blk_mas
     hipLaunchKernelGGL(dispatch_permute_kernel, dim3(nblk), dim3(kPermuteThreads),
                        El * (sizeof(unsigned long long) + 2 * sizeof(int)), s, idx, blk_mask, nblk, Tn, k, e0, El,
                        count, offset, pos, perm, clear);
+    return hipGetLastError();
+}
+
+hipError_t launch_masks(const int32_t* idx, int Tn, int k, int e0, int El, unsigned long long* blk_mask, hipStream_t s)
+{
+    if (Tn <= 0) return hipSuccess;
+    hipLaunchKernelGGL(dispatch_masks_kernel, dim3((Tn + kTokPerBlock - 1) / kTokPerBlock), dim3(256), El * sizeof(unsigned long long), s, idx, Tn, k, e0, El, blk_mask);
     return hipGetLastError();
 }
 

@@ -222,6 +222,8 @@ struct RouteArgs {
     float scale;
 };
 hipError_t launch_route(const RouteArgs& a, hipStream_t s);
+// the masks launch_router writes, from idx (dispatch.hip)
+hipError_t launch_masks(const int32_t* idx, int Tn, int k, int e0, int El, unsigned long long* blk_mask, hipStream_t s);
 
 // ---- matrix product with an epilogue (linear.hip)
 enum { kActNone = 0, kActRelu, kActSilu, kActGelu, kActGeluTanh, kActCount };

@@ -163,6 +163,10 @@ struct moe_ep_ctx {
     uint32_t prof_mask = ~0u;
     std::vector<hipEvent_t> prof_pool; size_t prof_next = 0;
     std::vector<ProfSpan> prof_spans;
+    // the gate's routing rule, where it is not the softmax over the selection (moe_ep_set_routing)
+    bool has_rule = false;
+    moe_ep_routing rule{};
+    const float* rule_bias = nullptr;
     // timing model for r_chunks == 0
     bool has_model = false;
     moe_ep_pipeline_model model{};
@@ -588,6 +592,37 @@ int moe_ep_set_pipeline_model(moe_ep_ctx* ctx, const moe_ep_pipeline_model* m)
     return MOE_EP_OK;
 }
 
+int moe_ep_set_routing(moe_ep_ctx* ctx, const moe_ep_routing* rule, const float* bias)
+{
+    if (!ctx) return MOE_EP_EINVAL;
+    if (!rule) {
+        if (bias) return fail(ctx, MOE_EP_EINVAL, "bias without a rule");
+        ctx->has_rule = false;
+        ctx->rule_bias = nullptr;
+        return MOE_EP_OK;
+    }
+    const moe_ep_config& c = ctx->cfg;
+    const char* why = nullptr;
+    if (moe_ep_validate_routing(rule, &why) != MOE_EP_OK) return fail(ctx, MOE_EP_EINVAL, why);
+    if (rule->n_experts != c.n_experts) return fail(ctx, MOE_EP_EINVAL, "the rule's n_experts must be the context's");
+    if (rule->top_k > c.max_top_k) return fail(ctx, MOE_EP_EINVAL, "the rule's top_k must be at most max_top_k");
+    if (rule->score_type != MOE_EP_F32 || (rule->score_stride != 0 && rule->score_stride != c.n_experts))
+        return fail(ctx, MOE_EP_EINVAL, "the rule's scores must be fp32 without gaps, as gate_logits are");
+    if (rule->device != c.device) return fail(ctx, MOE_EP_EINVAL, "the rule's device must be the context's");
+    if (reinterpret_cast<uintptr_t>(bias) & 3) return fail(ctx, MOE_EP_EINVAL, "bias must be aligned to its elements");
+    if (bias && ctx->check_spans) {
+        HIP_TRY(ctx, hipSetDevice(c.device));
+        if (const char* bad = check_span(bias, (size_t)c.n_experts * 4, false, nullptr)) {
+            snprintf(ctx->err, sizeof ctx->err, "bias %s", bad);
+            return MOE_EP_EINVAL;
+        }
+    }
+    ctx->rule = *rule;
+    ctx->rule_bias = bias;
+    ctx->has_rule = true;
+    return MOE_EP_OK;
+}
+
 int moe_ep_set_profiling(moe_ep_ctx* ctx, int32_t depth)
 {
     if (!ctx || depth < 0 || depth > 256) return MOE_EP_EINVAL;
@@ -768,7 +803,7 @@ int forward_impl(moe_ep_ctx* ctx, const void* tokens, const float* gate_logits, 
     // share in 2 chunks, its first one on the copies' stream / here: 500 / 1024 / 2000 / 4096 tokens 373 / 362, 512 / 502, 750 / 732,
     // 1343 / 1343 us (there the next chunk's rows are the longer wait); in 4 chunks 300 / 4096 tokens 565 / 545, 1379 / 1368.
     const bool shared_first = !dep && Ns > 0 && order == MOE_EP_ORDER_SHARED_FIRST;
-    const bool in_place = pinned && !dep && rows_come_with_gate(E, r, shared_first) && !ctx->memcpy_in && !(reinterpret_cast<uintptr_t>(h_tokens) & 15) &&
+    const bool in_place = pinned && !dep && !ctx->has_rule && rows_come_with_gate(E, r, shared_first) && !ctx->memcpy_in && !(reinterpret_cast<uintptr_t>(h_tokens) & 15) &&
                           !(prof && (ctx->prof_mask & (1u << ST_COPY_IN)));
     const auto comes_in = [&](int cidx) { return pinned && !(in_place && cidx == 0); };
     const bool inbound = comes_in(r - 1);
@@ -976,7 +1011,13 @@ int forward_impl(moe_ep_ctx* ctx, const void* tokens, const float* gate_logits, 
         const float* scores = here ? reinterpret_cast<const float*>(h_logits) : log_dev + (size_t)t0 * E;
         const RowCopy rows{ctx->d_tokens, h_tokens, (size_t)Tn * M * 2, 0};
         const int sp = prof_begin(ctx, prof, ST_ROUTER, s_comp);
-        if (Tn > 0 && Tn <= kTokPerBlock)   // one workgroup's tokens: partitioned in the same launch
+        if (ctx->has_rule) {
+            const moe_ep_routing& u = ctx->rule;
+            const int groups = u.n_groups > 1 ? u.n_groups : 1;
+            HIP_TRY(ctx, launch_route(RouteArgs{scores, ctx->rule_bias, nullptr, idx, w, E, Tn, E, k, groups, groups > 1 ? u.top_groups : 1, false,
+                                                u.score == MOE_EP_SCORE_SIGMOID, u.group_score == MOE_EP_GROUP_TOP2, u.renormalise != 0, u.scale}, s_comp));
+            HIP_TRY(ctx, launch_masks(idx, Tn, k, e0, El, ctx->blk_mask, s_comp));
+        } else if (Tn > 0 && Tn <= kTokPerBlock)   // one workgroup's tokens: partitioned in the same launch
             HIP_TRY(ctx, launch_route_and_partition(scores, Tn, E, k, e0, El, idx, w, ctx->count + (size_t)cidx * El,
                                                     ctx->offset + (size_t)cidx * (El + 1), ctx->pos + (size_t)t0 * k, ctx->perm + (size_t)t0 * k,
                                                     s_comp, here ? &rows : nullptr, to_clear(cidx, Tn)));
@@ -1016,11 +1057,11 @@ int forward_impl(moe_ep_ctx* ctx, const void* tokens, const float* gate_logits, 
         int32_t* perm = ctx->perm + (size_t)t0 * k;
 
         // a few tokens that are on the GPU: the gate/up projection's launch routes, unless one of the two is timed
-        const bool routes = narrow && Tn > 0 && Tn <= kGateTokens && E <= kGateExperts && k <= E && (ctx->narrow_named || narrow_gate_pays(Tn, k, El, H, n_cu)) && !dep && !pinned && !(along && takes_all && T != Tn) &&
+        const bool routes = narrow && !ctx->has_rule && Tn > 0 && Tn <= kGateTokens && E <= kGateExperts && k <= E && (ctx->narrow_named || narrow_gate_pays(Tn, k, El, H, n_cu)) && !dep && !pinned && !(along && takes_all && T != Tn) &&
                             !(prof && (ctx->prof_mask & ((1u << ST_ROUTER) | (1u << ST_PARTITION) | (1u << ST_GEMM1))));
         const GateArgs route{log_dev + (size_t)t0 * E, Tn, E, k, e0, idx, w, count, offset, pos, perm};
         if (!routes && !(in_place && cidx == 0)) { const int rc = gate(cidx); if (rc != MOE_EP_OK) return rc; }
-        const bool one_block = Tn > 0 && Tn <= kTokPerBlock;
+        const bool one_block = !ctx->has_rule && Tn > 0 && Tn <= kTokPerBlock;
 
         // the fused gather addresses a chunk's token rows with 32-bit byte offsets
         const bool fused = ctx->fused_gather && (unsigned long long)Tn * M * 2 < (1ull << 32);
@@ -1209,6 +1250,7 @@ int moe_ep_forward(moe_ep_ctx* ctx, const void* tokens, const float* gate_logits
     if (moe_ep_validate_forward(&ctx->cfg, tokens, gate_logits, routed_w, shared_w, top_k, r_chunks,
                                 order, n_tokens, out, &why) != MOE_EP_OK)
         return fail(ctx, MOE_EP_EINVAL, why);
+    if (ctx->has_rule && top_k != ctx->rule.top_k) return fail(ctx, MOE_EP_EINVAL, "top_k must be the routing rule's (moe_ep_set_routing)");
     ctx->err[0] = 0;
     if (r_chunks == 0) {
         if (!ctx->has_model) return fail(ctx, MOE_EP_ESTATE, "r_chunks == 0 needs moe_ep_set_pipeline_model first");
@@ -1310,6 +1352,7 @@ int moe_ep_forward_dep(moe_ep_ctx* ctx, const void* tokens, const float* gate_lo
     if (moe_ep_validate_forward(&ctx->cfg, tokens, gate_logits, routed_w, shared_w, top_k, r_1 * r_2,
                                 MOE_EP_ORDER_INTERLEAVED, n_tokens, out, &why) != MOE_EP_OK)
         return fail(ctx, MOE_EP_EINVAL, why);
+    if (ctx->has_rule && top_k != ctx->rule.top_k) return fail(ctx, MOE_EP_EINVAL, "top_k must be the routing rule's (moe_ep_set_routing)");
     ctx->err[0] = 0;
     HIP_TRY(ctx, hipSetDevice(ctx->cfg.device));
     if (!ctx->s_ag) {  // first call: the attention-group stream and its events
