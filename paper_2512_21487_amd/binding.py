@@ -297,37 +297,45 @@ def _current_stream(device: int) -> int:
         return 0
 
 
-def _check_rows(x, name: str, n_rows: int, cols: int, stride: int, size: int) -> None:
-    """Marshalling check of a torch tensor argument of rows that may lie apart: element size, at least ``n_rows`` rows of ``cols``
-    contiguous elements ``stride`` apart, on the GPU (raw addresses pass through)."""
-    if x is None or not hasattr(x, "stride"):
-        return
-    have, apart = x.shape, x.stride()
+def _rows(x, name: str, n_rows: int, cols: int, stride: int, size: int) -> Optional[int]:
+    """Address of an argument of rows that may lie apart.  A torch tensor is checked: element size, at least ``n_rows`` rows of
+    ``cols`` contiguous elements ``stride`` apart, on the GPU (raw addresses pass through)."""
+    if x is None:
+        return None
+    try:
+        have, apart = x.shape, x.stride()
+    except (AttributeError, TypeError):
+        return _ptr(x)
+    # the usual case, decided in half the time
     if len(have) == 2 and have[0] >= n_rows and have[1] >= cols and apart[1] == 1 and apart[0] == stride and x.is_cuda and x.element_size() == size:
-        return   # the usual case, decided in half the time
+        return x.data_ptr()
     if x.element_size() != size:
         raise ValueError(f"{name} has elements of {x.element_size()} bytes, the call reads {size}")
     if not (x.is_cuda or x.is_pinned()):
         raise ValueError(f"{name} must be a device tensor")
-    if x.dim() == 1 and n_rows == 1:
-        if x.shape[0] < cols or (cols > 1 and x.stride(0) != 1):
+    if len(have) == 1 and n_rows == 1:
+        if have[0] < cols or (cols > 1 and apart[0] != 1):
             raise ValueError(f"{name} must be a contiguous row of {cols}")
-        return
-    if x.dim() != 2 or x.shape[0] < n_rows or x.shape[1] < cols:
-        raise ValueError(f"{name} must be at least {n_rows} rows of {cols}, got {tuple(x.shape)}")
-    if (cols > 1 and x.stride(1) != 1) or (n_rows > 1 and x.stride(0) != stride):
-        raise ValueError(f"{name} has strides {x.stride()}, the call reads rows {stride} apart")
+        return x.data_ptr()
+    if len(have) != 2 or have[0] < n_rows or have[1] < cols:
+        raise ValueError(f"{name} must be at least {n_rows} rows of {cols}, got {tuple(have)}")
+    if (cols > 1 and apart[1] != 1) or (n_rows > 1 and apart[0] != stride):
+        raise ValueError(f"{name} has strides {apart}, the call reads rows {stride} apart")
+    return x.data_ptr()
 
 
-def _check_vector(x, name: str, n: int, size: int) -> None:
-    if x is None or not hasattr(x, "stride"):
-        return
-    if x.numel() >= n and x.element_size() == size and x.is_cuda and x.is_contiguous():
-        return
-    if x.element_size() != size or not x.is_contiguous() or x.numel() < n:
-        raise ValueError(f"{name} must be {n} contiguous elements of {size} bytes")
+def _vector(x, name: str, n: int, size: int) -> Optional[int]:
+    """Address of a contiguous argument; a torch tensor is checked for n elements of ``size`` bytes on the GPU."""
+    if x is None:
+        return None
+    try:
+        if x.numel() < n or x.element_size() != size or not x.is_contiguous():
+            raise ValueError(f"{name} must be {n} contiguous elements of {size} bytes")
+    except AttributeError:
+        return _ptr(x)
     if not (x.is_cuda or x.is_pinned()):
         raise ValueError(f"{name} must be a device tensor")
+    return x.data_ptr()
 
 
 def validate_routing(rule: Routing) -> Tuple[int, str]:
@@ -343,15 +351,12 @@ def route(rule: Routing, scores, bias=None, token_mask=None, n_tokens: Optional[
         n_tokens = int(scores.shape[0])
     if stream is None:
         stream = _current_stream(rule.device)
-    k = rule.top_k
-    _check_rows(scores, "scores", n_tokens, rule.n_experts, rule.score_stride or rule.n_experts, 4 if rule.score_type else 2)
-    _check_vector(bias, "bias", rule.n_experts, 4)
-    _check_vector(token_mask, "token_mask", n_tokens, 1)
-    _check_vector(idx, "idx", n_tokens * k, 4)
-    _check_vector(w, "w", n_tokens * k, 4)
+    k, E = rule.top_k, rule.n_experts
     why = ctypes.c_char_p()
-    rc = load_library().moe_ep_route(ctypes.byref(rule), _ptr(scores), _ptr(bias), _ptr(token_mask), n_tokens, _ptr(idx),
-                                     _ptr(w), stream, ctypes.byref(why))
+    rc = (_lib or load_library()).moe_ep_route(
+        ctypes.byref(rule), _rows(scores, "scores", n_tokens, E, rule.score_stride or E, 4 if rule.score_type else 2),
+        _vector(bias, "bias", E, 4), _vector(token_mask, "token_mask", n_tokens, 1), n_tokens, _vector(idx, "idx", n_tokens * k, 4),
+        _vector(w, "w", n_tokens * k, 4), stream, ctypes.byref(why))
     if rc != 0:
         raise MoeEpError(rc, (why.value or b"").decode())
     return rc
@@ -372,14 +377,11 @@ def linear(cfg: LinearConfig, x, weight, bias=None, residual=None, out=None, n_r
         stream = _current_stream(cfg.device)
     K, N = cfg.in_features, cfg.out_features
     size = 4 if cfg.out_type else 2
-    _check_rows(x, "x", n_rows, K, cfg.x_stride or K, 2)
-    _check_rows(weight, "weight", N, K, cfg.weight_stride or K, 4 if cfg.weight_type else 2)
-    _check_vector(bias, "bias", N, 4)
-    _check_rows(residual, "residual", n_rows, N, cfg.residual_stride or N, size)
-    _check_rows(out, "out", n_rows, N, cfg.out_stride or N, size)
     why = ctypes.c_char_p()
-    rc = load_library().moe_ep_linear(ctypes.byref(cfg), _ptr(x), _ptr(weight), _ptr(bias), _ptr(residual), n_rows,
-                                      _ptr(out), stream, ctypes.byref(why))
+    rc = (_lib or load_library()).moe_ep_linear(
+        ctypes.byref(cfg), _rows(x, "x", n_rows, K, cfg.x_stride or K, 2), _rows(weight, "weight", N, K, cfg.weight_stride or K, 4 if cfg.weight_type else 2),
+        _vector(bias, "bias", N, 4), _rows(residual, "residual", n_rows, N, cfg.residual_stride or N, size), n_rows,
+        _rows(out, "out", n_rows, N, cfg.out_stride or N, size), stream, ctypes.byref(why))
     if rc != 0:
         raise MoeEpError(rc, (why.value or b"").decode())
     return rc
@@ -557,8 +559,8 @@ class MoeEp:
     # -- moe_ep_set_routing -----------------------------------------------------------------
     def set_routing(self, rule: Optional[Routing] = None, bias=None) -> int:
         """Later forwards route by ``rule`` (None: as a new context); the context keeps ``bias`` alive."""
-        _check_vector(bias, "bias", self.cfg.n_experts, 4)
-        rc = self._lib.moe_ep_set_routing(self._ctx, ctypes.byref(rule) if rule is not None else None, _ptr(bias))
+        rc = self._lib.moe_ep_set_routing(self._ctx, ctypes.byref(rule) if rule is not None else None,
+                                          _vector(bias, "bias", self.cfg.n_experts, 4))
         if rc != 0:
             raise MoeEpError(rc, self.last_error())
         self._routing_bias = bias
