@@ -185,12 +185,21 @@ __device__ __forceinline__ f32x8_t load8(const float* p, int left)
     return v;
 }
 
-// 16 bytes of a row, the `left` first elements of which are there, and zeros
+// 16 bytes of a row, the `left` first elements of which are there, and zeros.  A row of N elements and more: its last 16 bytes, shifted
+// (an element at a time, the last K step of 1531 x 1409 x 2049 took 7 of 49 us).
 template <int N, class T>
-__device__ __forceinline__ u32x4_t load_part(const T* p, int left)
+__device__ __forceinline__ u32x4_t load_part(const T* p, int left, int cols)
 {
-    u32x4_t v = {0, 0, 0, 0};
     if (left >= N) return *reinterpret_cast<const u32x4_any2*>(p);
+    u32x4_t v = {0, 0, 0, 0};
+    if (cols >= N) {
+        if (left <= 0) return v;
+        const u32x4_t u = *reinterpret_cast<const u32x4_any2*>(p - (N - left));
+        const uint64_t lo = (uint64_t)u[1] << 32 | u[0], hi = (uint64_t)u[3] << 32 | u[2];
+        const int drop = (N - left) * (128 / N);                     // bits, 16 .. 112
+        const uint64_t a = drop < 64 ? lo >> drop | hi << (64 - drop) : hi >> (drop - 64), b = drop < 64 ? hi >> drop : 0;
+        return u32x4_t{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)};
+    }
 #pragma unroll
     for (int i = 0; i < N - 1; ++i) {
         if (i >= left) continue;
@@ -349,12 +358,12 @@ __global__ __launch_bounds__(WAVES * 64) void linear_split_kernel(LinearArgs a)
 #pragma unroll
         for (int i = 0; i < C::WL; ++i) {
             const Weight* p = w0 + step * KS + wo[i];
-            f.w[i] = whole ? *reinterpret_cast<const u32x4_any2*>(p) : load_part<PER>(p, left - wc * PER);
+            f.w[i] = whole ? *reinterpret_cast<const u32x4_any2*>(p) : load_part<PER>(p, left - wc * PER, a.K);
         }
 #pragma unroll
         for (int i = 0; i < C::XL; ++i) {
             const uint16_t* p = x0 + step * KS + xo[i];
-            f.x[i] = whole ? *reinterpret_cast<const u32x4_any2*>(p) : load_part<8>(p, left - xc * 8);
+            f.x[i] = whole ? *reinterpret_cast<const u32x4_any2*>(p) : load_part<8>(p, left - xc * 8, a.K);
         }
     };
     const uint32_t xw = xr * 128, ww = C::X_BYTES + wr * C::WROW;
@@ -604,9 +613,10 @@ __device__ __forceinline__ void row_of_blocks(int mb, const f32x4_t (&acc)[MB][N
     } else if constexpr (B + 1 < MB) row_of_blocks<B + 1, MB, NB>(mb, acc, v);
 }
 
+// STAGED: operands that are not on 16 bytes come in through registers, a K step ahead, and are written to the next slot in front of its hand-over.
 // RAGGED: the last K step is not whole.  ACT: there is an activation; a launch without one does not fetch the code of all of them (256 x 256
 // tiles: 3 us of 19)
-template <int BM, int BN, int SLOTS, int OCC, bool RAGGED, bool ACT>
+template <int BM, int BN, int SLOTS, int OCC, bool RAGGED, bool ACT, bool STAGED>
 __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a)
 {
     using C = TileCfg<BM, BN, SLOTS>;
@@ -642,8 +652,16 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a)
         }
     };
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+    static_assert(!STAGED || SLOTS == 2, "one K step in registers");
+    u32x4_t staged[STAGED ? RPW : 1];
     const auto issue = [&](int ks, int ring, int i) __attribute__((always_inline)) {
         const int j = wave + C::NW * (i < RX ? i : i - RX);
+        if constexpr (STAGED) {
+            const uint16_t* const p = reinterpret_cast<const uint16_t*>((i < RX ? xi : wi) + ks * (C::KS * 2) + off[i]);
+            if (RAGGED && ks == KT - 1) staged[i] = load_part<8>(p, a.K - ks * C::KS - ((j & 1) ? ld_c ^ 4 : ld_c) * 8, a.K);
+            else staged[i] = *reinterpret_cast<const u32x4_any2*>(p);
+            return;
+        }
         const char* const base = (i < RX ? xi : wi) + ks * (C::KS * 2);
         const uint32_t to = lds_base + (uint32_t)(ring * C::SLOT_BYTES + (i < RX ? 0 : BM * 128) + j * 1024);
         if (RAGGED && ks == KT - 1) {
@@ -651,6 +669,13 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a)
             if (ks * C::KS + ((j & 1) ? ld_c ^ 4 : ld_c) * 8 >= a.K) src = reinterpret_cast<const char*>(kZeros);
             load_to_lds(to, src);
         } else load_to_lds(to, base, off[i]);
+    };
+    const auto to_slot = [&](int ring) __attribute__((always_inline)) {
+        if constexpr (STAGED) {
+#pragma unroll
+            for (int i = 0; i < RPW; ++i)
+                *reinterpret_cast<u32x4_t*>(lds + ring * C::SLOT_BYTES + (i < RX ? 0 : BM * 128) + (wave + C::NW * (i < RX ? i : i - RX)) * 1024 + lane * 16) = staged[i];
+        }
     };
     const auto hand_over = [&]() __attribute__((always_inline)) {
         // this wavefront's loads into the next slot have landed (all but those into later ones), its reads have returned
@@ -692,6 +717,7 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a)
         for (int i = 0; i < RPW; ++i) issue(ki, st, i);
         ++ki;
     }
+    to_slot(0);
     hand_over();
     // the last slot's loads start as every later one's do
     advance();
@@ -717,6 +743,7 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a)
                 if (p == C::HO) {
                     ++ki;
                     advance();
+                    to_slot(other);
                     hand_over();
                 }
                 asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc[mb][nb]) : "v"(wf[j][nb]), "v"(xf[j][mb]));
@@ -757,28 +784,32 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a)
     __builtin_amdgcn_s_waitcnt(0x0f70);   // no load may land in LDS that is another workgroup's by then
 }
 
-template <int BM, int BN, int SLOTS, int OCC, bool RAGGED, bool ACT>
+template <int BM, int BN, int SLOTS, int OCC, bool RAGGED, bool ACT, bool STAGED>
 hipError_t launch_tiled_as(const LinearArgs& a, int n_cu, hipStream_t s)
 {
     using C = TileCfg<BM, BN, SLOTS>;
     static_assert(C::LDS_BYTES * OCC <= 160 * 1024, "LDS of a compute unit");
     static std::atomic<uint64_t> told{0};
-    const hipError_t e = allow_lds(&linear_tiled_kernel<BM, BN, SLOTS, OCC, RAGGED, ACT>, C::LDS_BYTES, told);
+    const hipError_t e = allow_lds(&linear_tiled_kernel<BM, BN, SLOTS, OCC, RAGGED, ACT, STAGED>, C::LDS_BYTES, told);
     if (e != hipSuccess) return e;
     const long long total = (long long)((a.R + BM - 1) / BM) * ((a.N + BN - 1) / BN);
     if (total > 0x3fffffffll) return hipErrorInvalidValue;
     // as few workgroups as it takes for as many rounds, the same number on every XCD
     const long long wgs = (long long)n_cu * OCC, rounds = (total + wgs - 1) / wgs;
     const int grid = (int)(((total + rounds - 1) / rounds + 7) / 8 * 8);
-    hipLaunchKernelGGL((linear_tiled_kernel<BM, BN, SLOTS, OCC, RAGGED, ACT>), dim3(grid), dim3(256), C::LDS_BYTES, s, a);
+    hipLaunchKernelGGL((linear_tiled_kernel<BM, BN, SLOTS, OCC, RAGGED, ACT, STAGED>), dim3(grid), dim3(256), C::LDS_BYTES, s, a);
     return hipGetLastError();
 }
 
-template <int BM, int BN, int SLOTS, int OCC>
+template <int BM, int BN, int SLOTS, int OCC, bool STAGED = false>
 hipError_t launch_tiled(const LinearArgs& a, int n_cu, hipStream_t s)
 {
-    if (a.act == kActNone) return a.K % 64 ? launch_tiled_as<BM, BN, SLOTS, OCC, true, false>(a, n_cu, s) : launch_tiled_as<BM, BN, SLOTS, OCC, false, false>(a, n_cu, s);
-    return a.K % 64 ? launch_tiled_as<BM, BN, SLOTS, OCC, true, true>(a, n_cu, s) : launch_tiled_as<BM, BN, SLOTS, OCC, false, true>(a, n_cu, s);
+    // (staged: K is seldom whole)
+    if constexpr (!STAGED) {
+        if (a.act == kActNone && a.K % 64 == 0) return launch_tiled_as<BM, BN, SLOTS, OCC, false, false, false>(a, n_cu, s);
+        if (a.K % 64 == 0) return launch_tiled_as<BM, BN, SLOTS, OCC, false, true, false>(a, n_cu, s);
+    }
+    return a.act == kActNone ? launch_tiled_as<BM, BN, SLOTS, OCC, true, false, STAGED>(a, n_cu, s) : launch_tiled_as<BM, BN, SLOTS, OCC, true, true, STAGED>(a, n_cu, s);
 }
 
 // What a tile costs, us: `fixed` and, per K step, `alone` where most compute units have none, `full` where all have (power and
@@ -844,6 +875,12 @@ hipError_t launch_linear(const LinearArgs& a, int n_cu, hipStream_t s)
     // tiled / split, us: 64 x 1536 x 5120 17 / 9.7; 64 x 5120 x 2048 9.8 / 9.5, 256 x 2048 x 2048 9.6 / 12.
     const bool by_16 = !a.w32 && a.K > 64 && a.K % 8 == 0 && a.ldx % 8 == 0 && a.ldw % 8 == 0 && !((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w)) & 15);
     if (by_16 && a.R > 64 && tiles(64) >= n_cu / 4) return launch_tiled_best(a, n_cu, s);
+    // Operands that are not on 16 bytes: 64 x 64 tiles / 128 x 64 tiles / split, us: 1531 x 1409 x 2049 39 / 43 / 49, 3112 x 839 x 182 8.9 / 11 / 12,
+    // 8192 x 2048 x 2049 197 / 149 / 260, 16384 x 5120 x 1001 486 / 426 / 755; of few tiles 300 x 1409 x 2049 27 / 37 / 14.
+    if (!a.w32 && !by_16 && a.K > 64) {
+        if (2 * tiles(128) >= 4 * n_cu) return launch_tiled<128, 64, 2, 2, true>(a, n_cu, s);
+        if (tiles(64) >= 1.5 * n_cu) return launch_tiled<64, 64, 2, 3, true>(a, n_cu, s);
+    }
     return launch_split_best(a, n_cu, s);
 }
 

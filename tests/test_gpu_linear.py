@@ -232,3 +232,18 @@ def test_buffers_that_are_too_small_or_elsewhere():
     assert ei.value.code == -3 and torch.cuda.current_device() == before
     pkg.linear(cfg, x, w, out=out)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("R,N,K", [(1531, 1409, 2049), (3000, 839, 182), (4200, 4100, 65), (1300, 1300, 71), (4097, 4097, 129), (400, 65, 4100)])
+@pytest.mark.parametrize("name,out32,residual", [("none", False, True), ("gelu_tanh", True, False)])
+def test_large_products_that_are_not_on_16_bytes(R, N, K, name, out32, residual):
+    c = Case(R, N, K, out32=out32, bias=True, residual=residual, name=name, pads=(3, 0, 1, 5), shifts=(1, 2, 0, 0))
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("R,N,K", [(4096, 128, 4096), (2100, 60, 3000), (700, 512, 2304), (16384, 160, 640), (64, 128, 5120)])
+def test_gates_of_many_tokens(R, N, K):
+    c = Case(R, N, K, w32=True, out32=True, bias=True)
+    c.run()
+    c.check()
