@@ -245,7 +245,7 @@ typedef struct {
 int moe_ep_validate_routing(const moe_ep_routing *rule, const char **why);
 
 /*
- * Experts and weights of n_tokens tokens by a rule.
+ * Experts and weights of n_tokens tokens (0..2^30) by a rule.
  *   scores      score_type [n_tokens, E], rows score_stride apart, aligned to their elements
  *   bias        fp32 [E], or NULL;   token_mask  one byte per token, 0 = padding, or NULL
  *   idx, w      int32 and fp32 [n_tokens, top_k]; neither may overlap the other or an input
@@ -298,7 +298,8 @@ int moe_ep_validate_linear(const moe_ep_linear_config *cfg, const char **why);
 /*
  *   x         bf16 [n_rows, K];   weight  weight_type [N, K];   bias  fp32 [N], or NULL
  *   residual  out_type [n_rows, N], or NULL; may be `out` itself (with the same stride)
- *   out       out_type [n_rows, N]; must not overlap anything else.  What lies between its rows is left as it is.
+ *   out       out_type [n_rows, N]; must not overlap anything else (rows of the same distance may lie side by side).  What lies between its rows is left as it is.
+ *   n_rows    0..2^30
  * Rows are contiguous and every pointer is aligned to its elements; no more is asked of sizes, strides and addresses.  Products are summed in fp32 (fp32
  * weights enter with their whole mantissa and must be finite), bias, activation and residual are fp32 too, and a result is rounded once.  The same call gives the
  * same bits.  Streams, graphs, devices, checks, `why` and n_rows == 0 as for moe_ep_route.

@@ -43,19 +43,29 @@ bool checks_pointers()
     return on;
 }
 
-struct Span { const void* p; size_t bytes; const char* name; bool written; };
+// rows of row_bytes, row_stride bytes apart
+struct Span { const void* p; size_t rows, row_stride, row_bytes; const char* name; bool written; };
+size_t extent(const Span& s) { return s.rows ? (s.rows - 1) * s.row_stride + s.row_bytes : 0; }
+
+// whether some row of one lies on some row of the other; rows of the same distance may lie side by side
+bool meet(const Span& s, const Span& t)
+{
+    const Span &a = s.p <= t.p ? s : t, &b = s.p <= t.p ? t : s;
+    const size_t off = (size_t)(static_cast<const char*>(b.p) - static_cast<const char*>(a.p));
+    if (off >= extent(a)) return false;
+    if (a.row_stride != b.row_stride || a.rows < 2 || b.rows < 2) return true;
+    const size_t at = off % a.row_stride;
+    return at < a.row_bytes || at + b.row_bytes > a.row_stride;
+}
 
 // a result that lies on something else of its call, or NULL: needs no GPU
 const char* overlap(const Span* sp, int n)
 {
     for (int i = 0; i < n; ++i)
         for (int j = 0; j < n; ++j) {
-            if (!sp[i].written || i == j || !sp[i].p || !sp[j].p) continue;
-            const char *a = static_cast<const char*>(sp[i].p), *b = static_cast<const char*>(sp[j].p);
-            if (a < b + sp[j].bytes && b < a + sp[i].bytes) {
-                snprintf(t_text, sizeof t_text, "%s must not overlap %s", sp[i].name, sp[j].name);
-                return t_text;
-            }
+            if (!sp[i].written || i == j || !sp[i].p || !sp[j].p || !meet(sp[i], sp[j])) continue;
+            snprintf(t_text, sizeof t_text, "%s must not overlap %s", sp[i].name, sp[j].name);
+            return t_text;
         }
     return nullptr;
 }
@@ -64,7 +74,7 @@ const char* out_of_reach(const Span* sp, int n)
 {
     for (int i = 0; i < n && checks_pointers(); ++i) {
         if (!sp[i].p) continue;
-        if (const char* bad = check_span(sp[i].p, sp[i].bytes, false, nullptr)) {
+        if (const char* bad = check_span(sp[i].p, extent(sp[i]), false, nullptr)) {
             snprintf(t_text, sizeof t_text, "%s %s", sp[i].name, bad);
             return t_text;
         }
@@ -74,10 +84,7 @@ const char* out_of_reach(const Span* sp, int n)
 
 bool off_alignment(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) != 0; }
 
-// bytes from the first element of the first row to the last element of the last one
-size_t extent(long long rows, long long stride, long long cols, int size) { return rows ? (size_t)((rows - 1) * stride + cols) * size : 0; }
-
-constexpr long long kMostStride = 1ll << 22, kMostFeatures = 1 << 20;
+constexpr long long kMostStride = 1ll << 22, kMostFeatures = 1 << 20, kMostRows = 1 << 30;
 
 }  // namespace
 
@@ -107,7 +114,7 @@ int moe_ep_route(const moe_ep_routing* r, const void* scores, const float* bias,
                  int32_t* idx, float* w, void* stream, const char** why)
 {
     if (moe_ep_validate_routing(r, why) != MOE_EP_OK) return MOE_EP_EINVAL;
-    if (n_tokens < 0) return refuse(why, "n_tokens must be >= 0");
+    if (n_tokens < 0 || n_tokens > kMostRows) return refuse(why, "n_tokens must be in 0..2^30");
     if (n_tokens == 0) return MOE_EP_OK;
     if (!scores || !idx || !w) return refuse(why, "scores, idx and w must not be NULL");
     const int size = r->score_type == MOE_EP_BF16 ? 2 : 4;
@@ -115,11 +122,11 @@ int moe_ep_route(const moe_ep_routing* r, const void* scores, const float* bias,
     if (off_alignment(scores, size) || off_alignment(bias, 4) || off_alignment(idx, 4) || off_alignment(w, 4))
         return refuse(why, "scores, bias, idx and w must be aligned to their elements");
     const size_t out = (size_t)n_tokens * r->top_k * 4;
-    const Span sp[] = {{scores, extent(n_tokens, stride, r->n_experts, size), "scores", false},
-                       {bias, (size_t)r->n_experts * 4, "bias", false},
-                       {token_mask, (size_t)n_tokens, "token_mask", false},
-                       {idx, out, "idx", true},
-                       {w, out, "w", true}};
+    const Span sp[] = {{scores, (size_t)n_tokens, (size_t)stride * size, (size_t)r->n_experts * size, "scores", false},
+                       {bias, 1, 0, (size_t)r->n_experts * 4, "bias", false},
+                       {token_mask, 1, 0, (size_t)n_tokens, "token_mask", false},
+                       {idx, 1, 0, out, "idx", true},
+                       {w, 1, 0, out, "w", true}};
     if (const char* bad = overlap(sp, 5)) return refuse(why, bad);
     DeviceScope device(r->device);
     if (device.error != hipSuccess) return hip_failed(why, "selecting the device", device.error);
@@ -153,7 +160,7 @@ int moe_ep_linear(const moe_ep_linear_config* c, const void* x, const void* weig
                   int32_t n_rows, void* out, void* stream, const char** why)
 {
     if (moe_ep_validate_linear(c, why) != MOE_EP_OK) return MOE_EP_EINVAL;
-    if (n_rows < 0) return refuse(why, "n_rows must be >= 0");
+    if (n_rows < 0 || n_rows > kMostRows) return refuse(why, "n_rows must be in 0..2^30");
     if (n_rows == 0) return MOE_EP_OK;
     if (!x || !weight || !out) return refuse(why, "x, weight and out must not be NULL");
     const int K = c->in_features, N = c->out_features;
@@ -164,11 +171,12 @@ int moe_ep_linear(const moe_ep_linear_config* c, const void* x, const void* weig
         return refuse(why, "x, weight, bias, residual and out must be aligned to their elements");
     // an element of the residual is read by the lane that writes the result in its place: the same buffer may be both
     const bool in_place = residual == out && ldr == ldo;
-    const Span sp[] = {{x, extent(n_rows, ldx, K, 2), "x", false},
-                       {weight, extent(N, ldw, K, ws), "weight", false},
-                       {bias, (size_t)N * 4, "bias", false},
-                       {in_place ? nullptr : residual, extent(n_rows, ldr, N, os), "residual", false},
-                       {out, extent(n_rows, ldo, N, os), "out", true}};
+    const size_t rows = (size_t)n_rows;
+    const Span sp[] = {{x, rows, (size_t)ldx * 2, (size_t)K * 2, "x", false},
+                       {weight, (size_t)N, (size_t)ldw * ws, (size_t)K * ws, "weight", false},
+                       {bias, 1, 0, (size_t)N * 4, "bias", false},
+                       {in_place ? nullptr : residual, rows, (size_t)ldr * os, (size_t)N * os, "residual", false},
+                       {out, rows, (size_t)ldo * os, (size_t)N * os, "out", true}};
     if (const char* bad = overlap(sp, 5)) return refuse(why, bad);
     DeviceScope device(c->device);
     if (device.error != hipSuccess) return hip_failed(why, "selecting the device", device.error);

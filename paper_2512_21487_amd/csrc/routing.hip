@@ -352,10 +352,10 @@ __global__ __launch_bounds__(256, !BIASED || REGS < 32 ? REGS * K <= 256 ? 4 : 3
 #pragma unroll
         for (int r = 0; r < REGS; ++r) v[r] = s[r];
     }
-    // Two values that close may be in the other order.  p is off by up to a step or two of exp2 and the reciprocal (2^-22 of p <= 1 together), where it is a
-    // softmax by its sum's rounding too (2^-21); c by half a step of its own.  Twice that.
-    const float slack = a.sigmoid ? 0x1p-20f : 0x1p-19f;
-    const auto close = [=](float x, float y) { return x > none && y > none && !(fabsf(x - y) > slack + 0x1p-22f * fmaxf(fabsf(x), fabsf(y))); };
+    // Two values that close may be in the other order.  Of a sigmoid p is off by less than 2^-22 (exp2, its argument, a sum, the reciprocal); of a softmax the
+    // difference of two by 2^-21 and by 2^-19.3 of itself (their sum: 14 roundings in a row, and the arguments' of exponentials); c by half a step.  Twice all that.
+    const float slack = a.sigmoid ? 0x1p-20f : 0x1p-18f;
+    const auto close = [=](float x, float y, float by) { return x > none && y > none && !(fabsf(x - y) > by + 0x1p-22f * fmaxf(fabsf(x), fabsf(y))); };
     bool unsure = false;
     if (G > 1) {
         float m1 = v[0], m2 = none;
@@ -379,7 +379,7 @@ __global__ __launch_bounds__(256, !BIASED || REGS < 32 ? REGS * K <= 256 ? 4 : 3
         }
         const bool stays = ahead < a.top_groups;   // (of a group without an expert every value says so)
         // an order hangs on the last group that stays and the first that does not
-        if (group_value) unsure = close(over_lanes(stays ? value : __builtin_inff(), LANES, Least()), over_lanes(stays ? none : value, LANES, Most()));
+        if (group_value) unsure = close(over_lanes(stays ? value : __builtin_inff(), LANES, Least()), over_lanes(stays ? none : value, LANES, Most()), 2.f * slack);
         if (!stays) {
 #pragma unroll
             for (int r = 0; r < REGS; ++r) v[r] = s[r] = none;
@@ -428,7 +428,7 @@ __global__ __launch_bounds__(256, !BIASED || REGS < 32 ? REGS * K <= 256 ? 4 : 3
         const float value = full ? ranked_value(mine) : none, be = full ? a.bias[e] : 0.f;
         const int base = lane & ~(LANES - 1), next = lane + 1;
         const float nv = __shfl(value, next, 64), ns = __shfl(se, next, 64), nb = __shfl(be, next, 64);
-        bool near = sub < k && sub + 1 < K && close(value, nv) && !(se == ns && be == nb);
+        bool near = sub < k && sub + 1 < K && close(value, nv, slack) && !(se == ns && be == nb);
         const float lv = __shfl(value, base + k - 1, 64);
         const float line = lv > none ? lv - (slack + 0x1p-21f * fabsf(lv)) : __builtin_inff();   // a last slot that is empty has nobody behind it
         int found = 0;
@@ -455,7 +455,7 @@ __global__ __launch_bounds__(256, !BIASED || REGS < 32 ? REGS * K <= 256 ? 4 : 3
         }
         if (__ballot(near)) {
             // The slots' own values in double, of all tokens at once, and their order; the one in front of which all K are gives way to the other.
-            // A softmax's sum stays in fp32: it is the same for both, so that the difference of two p is off by 2^-21 of itself.
+            // A softmax's sum stays in fp32: it is the same for both, so that the difference of two p is off by less than 2^-18 of itself.
             const auto p_of = [&](float score) { return a.sigmoid ? 1.0 / (1.0 + exp(-(double)score)) : exp((double)score - (double)top) / (double)total; };
             double p = 0.0, c = -__builtin_inf(), p_extra = 0.0, c_extra = -__builtin_inf();
             if (full) { p = p_of(se); c = p + (double)be; }
@@ -468,7 +468,7 @@ __global__ __launch_bounds__(256, !BIASED || REGS < 32 ? REGS * K <= 256 ? 4 : 3
                 c_extra = p_extra + (double)a.bias[e_extra];
             }
             const auto ahead_of = [](double x, int ex, double y, int ey) { return x > y || (x == y && ex < ey); };
-            const auto unclear = [&](double px, double x, double py, double y) { return !a.sigmoid && px != py && fabs(x - y) <= 0x1p-20 * fabs(px - py); };
+            const auto unclear = [&](double px, double x, double py, double y) { return !a.sigmoid && px != py && fabs(x - y) <= 0x1p-18 * fabs(px - py); };
             place = 0;
 #pragma unroll 1
             for (int i = 0; i < K; ++i) {

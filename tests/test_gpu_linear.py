@@ -247,3 +247,16 @@ def test_gates_of_many_tokens(R, N, K):
     c = Case(R, N, K, w32=True, out32=True, bias=True)
     c.run()
     c.check()
+
+
+def test_columns_of_one_buffer():
+    import paper_2512_21487_amd as pkg
+    R, N, K = 300, 96, 128
+    buf = torch.zeros((R, 384), dtype=torch.bfloat16, device="cuda")
+    buf[:, :K].normal_()
+    w = torch.empty((N, K), dtype=torch.bfloat16, device="cuda").normal_(0.0, 0.1)
+    apart = torch.zeros((R, N), dtype=torch.bfloat16, device="cuda")
+    pkg.linear(pkg.LinearConfig(in_features=K, out_features=N, x_stride=384), buf[:, :K], w, out=apart)
+    pkg.linear(pkg.LinearConfig(in_features=K, out_features=N, x_stride=384, out_stride=384), buf[:, :K], w, out=buf[:, 200:200 + N])
+    torch.cuda.synchronize()
+    assert torch.equal(buf[:, 200:200 + N], apart) and not bool(buf[:, K:200].any()) and not bool(buf[:, 200 + N:].any())

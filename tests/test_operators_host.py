@@ -101,6 +101,27 @@ def test_in_place_residual_with_another_stride_is_refused():
     assert ei.value.code == -1 and "overlap residual" in str(ei.value)
 
 
+def test_rows_side_by_side_do_not_overlap():
+    """x, residual and out as columns of one buffer: the refusal is another one (there is no GPU here), or none at all."""
+    wide = config(x_stride=160, residual_stride=160, out_stride=160)
+    for out, inside in ((A + 128, False), (A + 256, False), (A + 126, True), (A + 258, True), (A + 320 + 126, True), (A + 320 + 128, False)):
+        try:
+            pkg.linear(wide, A, B, None, None, out=out, n_rows=4, stream=0)
+        except pkg.MoeEpError as e:
+            assert ("overlap" in str(e)) == inside
+        else:
+            raise AssertionError("addresses that are no memory were taken")
+    with pytest.raises(pkg.MoeEpError, match="out must not overlap x"):   # other distances: from the first element to the last
+        pkg.linear(config(x_stride=160, out_stride=96), A, B, None, None, out=A + 128, n_rows=4, stream=0)
+
+
+def test_more_rows_than_are_taken():
+    with pytest.raises(pkg.MoeEpError, match="n_rows"):
+        pkg.linear(config(), A, B, out=C, n_rows=(1 << 30) + 1, stream=0)
+    with pytest.raises(pkg.MoeEpError, match="n_tokens"):
+        pkg.route(rule(), A, n_tokens=(1 << 30) + 1, idx=B, w=C, stream=0)
+
+
 def test_calls_without_a_row_do_nothing():
     assert pkg.route(rule(), None, n_tokens=0, stream=0) == 0
     assert pkg.linear(config(), None, None, n_rows=0, stream=0) == 0
