@@ -42,4 +42,12 @@ __device__ __forceinline__ float silu_f(float g)
     return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.4426950408889634f));
 }
 
+// Workgroups of a launch that may have more threads than the 2^32 of one grid dimension: rows of 2^20 workgroups (a multiple of the XCDs)
+inline dim3 grid_of(long long workgroups)
+{
+    const long long x = workgroups < 1 << 20 ? workgroups : 1 << 20;
+    return dim3((unsigned)x, (unsigned)((workgroups + x - 1) / x));
+}
+__device__ __forceinline__ long long workgroup() { return (long long)blockIdx.y * gridDim.x + blockIdx.x; }
+
 }  // namespace moe_ep

@@ -6,7 +6,9 @@
 // Which expert is chosen is a whole number and may not hang on how a sum was rounded: choices are those of c in double precision.  Computing
 // them so for every token (route_exact_kernel, a wavefront per token, also the kernel of shapes that the other one does not have) took 150 us
 // for 65536 tokens of 256 experts.  route_kernel computes c in fp32 and looks whether two values that an order hangs on are closer than its
-// rounding; of normal scores about one token in a thousand is such, and is done again in double.
+// rounding; chosen slots that are close are compared in double by the lanes that hold them, and only a token whose last slot or last
+// group hangs on such a pair is done again in double as a whole (5 us where it is the last one of a launch).  The same 65536 tokens
+// take 19 us, 37 with a bias, of which reading the scores is 14: instruction issue bounds it.
 #include "gate.h"
 
 namespace moe_ep {
@@ -15,7 +17,7 @@ namespace {
 
 constexpr int kRtExperts = 512, kRtTopK = 64;
 constexpr int kRtLaneExperts = kRtExperts / 64;
-constexpr int kRtFewTokens = 2048;   // 16 lanes per token up to here: more wavefronts, and shorter ones
+constexpr int kRtFewTokens = 8192;   // 16 lanes per token up to here (launch_route)
 
 // the value of the lane that row_exchange names, of wider types
 template <int CTRL>
@@ -262,8 +264,9 @@ __device__ __forceinline__ void merge_lanes(double (&a)[N])
     merge(a, b);
 }
 // A token is LANES lanes', each with REGS of its experts: of one group those of a group's lanes, VEC consecutive ones at a time.  The K
-// best of a lane are sorted in registers, and the lanes' lists merged pair by pair: no round waits for another.  What bounds it is the
-// instructions, about 50 a token (8 lanes, 32 experts a lane), and the scores' bytes close behind.
+// best of a lane are sorted in registers, and the lanes' lists merged pair by pair: no round waits for another.  (A selection in rounds,
+// a maximum over the lanes in each, waits for k of them.)  Instructions bound it where the tokens are many, 37 us of 65536 x 256 with a bias
+// where the bytes are 14, and latency where they are few: 3.8 us of 256 tokens.
 template <int LANES, int REGS, int K, int VEC, bool BIASED>
 __global__ __launch_bounds__(256, !BIASED || REGS < 32 ? REGS * K <= 256 ? 4 : 3 : 2) void route_kernel(RouteArgs a)
 {
@@ -271,7 +274,7 @@ __global__ __launch_bounds__(256, !BIASED || REGS < 32 ? REGS * K <= 256 ? 4 : 3
     __shared__ double s_c[4][kRtExperts];
     __shared__ int s_slot[4][kRtTopK];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane % LANES;
-    const long long t = ((long long)blockIdx.x * 4 + wave) * (64 / LANES) + lane / LANES;
+    const long long t = (workgroup() * 4 + wave) * (64 / LANES) + lane / LANES;
     const int E = a.E, k = a.k, G = a.groups, S = E / G, LG = LANES / G, g = sub / LG;
     const bool there = t < a.T, live = there && (!a.token_mask || a.token_mask[t] != 0);
     const long long row_at = there ? t * a.stride : 0;   // a token that is not there reads the first one's scores
@@ -514,7 +517,7 @@ template <int LANES, int REGS, int K, int VEC>
 hipError_t launch(const RouteArgs& a, hipStream_t s)
 {
     const long long tokens = 4 * (64 / LANES);
-    const dim3 grid((unsigned)((a.T + tokens - 1) / tokens));
+    const dim3 grid = grid_of(((long long)a.T + tokens - 1) / tokens);
     if (a.bias) hipLaunchKernelGGL((route_kernel<LANES, REGS, K, VEC, true>), grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((route_kernel<LANES, REGS, K, VEC, false>), grid, dim3(256), 0, s, a);
     return hipGetLastError();
@@ -534,7 +537,7 @@ __global__ __launch_bounds__(256) void route_exact_kernel(RouteArgs a)
     __shared__ double s_c[4][kRtExperts];
     __shared__ int s_slot[4][kRtTopK];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long t = (long long)blockIdx.x * 4 + wave;
+    const long long t = workgroup() * 4 + wave;
     if (t < a.T) route_token(a, t, lane, s_c[wave], s_slot[wave]);
 }
 
@@ -549,14 +552,17 @@ hipError_t launch_route(const RouteArgs& a, hipStream_t s)
     const int size = a.E / a.groups, vec = size % 4 == 0 ? 4 : 1;
     const auto regs = [&](int lanes) { return (size + lanes / a.groups * vec - 1) / (lanes / a.groups * vec) * vec; };
     if (groups_fit && a.k <= 16) {
-        if (a.k <= 8 && a.groups <= 8 && regs(8) <= (a.bias ? 16 : 32) && a.T > kRtFewTokens)
+        // 8 lanes a token sort and merge less in all, 16 lanes are shorter.  8 / 16, us, 256 experts: 4096 tokens 4.5 / 4.0, 8192 4.6 / 4.7,
+        // 65536 19.7 / 20.9; 128 with a bias: 4096 7.4 / 5.8, 8192 7.4 / 7.5, 65536 18.8 / 23.7; 160 in 8 groups 5.3 / 4.7, 5.4 / 5.4, 20 / 24.
+        // 64 experts: 512 3.3 / 3.4, 65536 9.1 / 15.5.  32 experts a lane with a bias, which keeps p and c, spill: 65536 35 / 31.
+        if (a.k <= 8 && a.groups <= 8 && regs(8) <= (a.bias ? 16 : 32) && (a.T > kRtFewTokens || (!a.bias && regs(8) <= 8)))
             return vec == 4 ? launch_regs<8, 8, 4>(a, regs(8), s) : launch_regs<8, 8, 1>(a, regs(8), s);
         if (regs(16) <= 32) {
             if (a.k <= 8) return vec == 4 ? launch_regs<16, 8, 4>(a, regs(16), s) : launch_regs<16, 8, 1>(a, regs(16), s);
             return vec == 4 ? launch_regs<16, 16, 4>(a, regs(16), s) : launch_regs<16, 16, 1>(a, regs(16), s);
         }
     }
-    const dim3 grid((unsigned)(((long long)a.T + 3) / 4));
+    const dim3 grid = grid_of(((long long)a.T + 3) / 4);
     hipLaunchKernelGGL(route_exact_kernel, grid, dim3(256), 0, s, a);
     return hipGetLastError();
 }

@@ -260,3 +260,14 @@ def test_columns_of_one_buffer():
     pkg.linear(pkg.LinearConfig(in_features=K, out_features=N, x_stride=384, out_stride=384), buf[:, :K], w, out=buf[:, 200:200 + N])
     torch.cuda.synchronize()
     assert torch.equal(buf[:, 200:200 + N], apart) and not bool(buf[:, K:200].any()) and not bool(buf[:, 200 + N:].any())
+
+
+def test_more_rows_than_a_grid_has_rows_of_threads():
+    """2^32 threads are a grid dimension's; a workgroup of 256 has 64 rows of one column."""
+    import paper_2512_21487_amd as pkg
+    R = 2 ** 30
+    x = torch.randint(-8, 8, (R, 1), device="cuda", dtype=torch.int8).to(torch.bfloat16)
+    out = torch.full((R + 1, 1), 77.0, dtype=torch.bfloat16, device="cuda")
+    pkg.linear(pkg.LinearConfig(in_features=1, out_features=1), x, torch.tensor([[0.5]], device="cuda", dtype=torch.bfloat16), out=out, n_rows=R)
+    torch.cuda.synchronize()
+    assert torch.equal(out[:R], x * 0.5) and float(out[R]) == 77.0

@@ -265,3 +265,44 @@ def test_buffers_that_are_too_small_or_elsewhere():
     pkg.route(rule, s, idx=idx, w=w)
     torch.cuda.synchronize()
     assert idx.view(8, 6)[0].tolist() == [0, 1, 2, 3, 4, 5]
+
+
+@pytest.mark.parametrize("T", [8191, 8192, 8193, 9001])
+@pytest.mark.parametrize("E,groups,top_groups,k", [(64, 1, 1, 6), (61, 1, 1, 8), (128, 8, 3, 8), (160, 2, 1, 5), (256, 1, 1, 8), (256, 16, 4, 8)])
+@pytest.mark.parametrize("sigmoid,with_bias,top2", [(False, False, False), (True, True, True), (False, True, False), (False, False, True)])
+def test_many_tokens(T, E, groups, top_groups, k, sigmoid, with_bias, top2):
+    """Fewer lanes have a token from some number of tokens on.  Rows of every kind among ordinary ones: nobody there, few, equal, huge."""
+    s = normal(T, E, T + E)
+    if E % 2:                                        # equal scores, as bf16 has many
+        s = np.round(s * 16) / 16
+    s[5::97, 2:] = -np.inf
+    s[6::101] = np.nan
+    s[7::103] = 0.25
+    s[8::107, ::2] = -FMAX
+    s[9::109] = np.inf
+    s[10::113] = -1e4
+    bias = None
+    if with_bias:
+        bias = 0.05 * normal(1, E, 7)[0]
+        bias[3], bias[E // 2] = -np.inf, bias[1]
+    mask = (np.random.default_rng(T).random(T) < 0.9).astype(np.uint8)
+    check(s, bias, mask if k < 8 else None, k=k, groups=groups, top_groups=top_groups, top2=top2, sigmoid=sigmoid, renorm=True, scale=1.5)
+
+
+@pytest.mark.parametrize("T,E,groups", [(2 ** 29 + 5, 2, 1), (2 ** 26 + 5, 3, 3)])
+def test_more_tokens_than_a_grid_has_rows_of_threads(T, E, groups):
+    """2^32 threads are a grid dimension's; eight lanes, or a wavefront, have a token."""
+    import paper_2512_21487_amd as pkg
+    s = torch.randint(0, 7, (T, E), device="cuda", dtype=torch.int8).to(torch.bfloat16)
+    idx = torch.full((T + 1, 1), 9, dtype=torch.int32, device="cuda")
+    w = torch.full((T + 1, 1), 9.0, dtype=torch.float32, device="cuda")
+    pkg.route(pkg.Routing(n_experts=E, top_k=1, n_groups=groups, top_groups=1, renormalise=1, scale=1.5, score_type=pkg.BF16), s, n_tokens=T, idx=idx, w=w)
+    want = torch.zeros(T, dtype=torch.int32, device="cuda")
+    best = s[:, 0].clone()
+    for e in range(1, E):
+        more = s[:, e] > best
+        want[more] = e
+        best = torch.maximum(best, s[:, e])
+    torch.cuda.synchronize()
+    assert torch.equal(idx[:T, 0], want) and bool((w[:T] == 1.5).all())
+    assert int(idx[T]) == 9 and float(w[T]) == 9.0
