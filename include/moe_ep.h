@@ -301,7 +301,7 @@ int moe_ep_validate_linear(const moe_ep_linear_config *cfg, const char **why);
  *   out       out_type [n_rows, N]; must not overlap anything else (rows of the same distance may lie side by side).  What lies between its rows is left as it is.
  *   n_rows    0..2^30
  * Rows are contiguous and every pointer is aligned to its elements; no more is asked of sizes, strides and addresses.  Products are summed in fp32 (fp32
- * weights enter with their whole mantissa and must be finite), bias, activation and residual are fp32 too, and a result is rounded once.  The same call gives the
+ * weights enter with their whole mantissa and must be finite; with them a row of x that is not finite may give NaN where the formula gives an infinity), bias, activation and residual are fp32 too, and a result is rounded once.  The same call gives the
  * same bits.  Streams, graphs, devices, checks, `why` and n_rows == 0 as for moe_ep_route.
  */
 int moe_ep_linear(const moe_ep_linear_config *cfg, const void *x, const void *weight, const float *bias,
