@@ -381,8 +381,9 @@ __global__ __launch_bounds__(256, !BIASED || REGS < 32 ? REGS * K <= 256 ? 4 : 3
             ahead += other > value || (other == value && h < g);
         }
         const bool stays = ahead < a.top_groups;   // (of a group without an expert every value says so)
+        unsure = m1 > none && fabsf(m1) < __builtin_inff() && !(fabsf(value) < __builtin_inff());   // a sum that is beyond fp32, not beyond double
         // an order hangs on the last group that stays and the first that does not
-        if (group_value) unsure = close(over_lanes(stays ? value : __builtin_inff(), LANES, Least()), over_lanes(stays ? none : value, LANES, Most()), 2.f * slack);
+        if (group_value) unsure |= close(over_lanes(stays ? value : __builtin_inff(), LANES, Least()), over_lanes(stays ? none : value, LANES, Most()), 2.f * slack);
         if (!stays) {
 #pragma unroll
             for (int r = 0; r < REGS; ++r) v[r] = s[r] = none;

@@ -2,7 +2,7 @@
 import numpy as np
 import pytest
 
-from test_gpu_route import FMAX, check, normal
+from test_gpu_route import FMAX, check, normal, run
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -23,3 +23,45 @@ def test_slots_left_to_biases_near_the_lowest_number(E, groups, top_groups, k, T
         check(s, bias, k=k, groups=groups, top_groups=top_groups, sigmoid=sigmoid)
         bias[1], bias[E - 1] = -np.inf, np.nan
         check(s, bias, k=k, groups=groups, top_groups=top_groups, sigmoid=sigmoid)
+
+
+def groups_rule(s, bias, *, S, top_groups, k, sigmoid):
+    """idx of the rule with GROUP_TOP2 in float64, for groups of S >= 2 experts."""
+    T, E = s.shape
+    s = np.where(s > -FMAX, s.astype(np.float64), -np.inf)
+    if sigmoid:
+        p = 1.0 / (1.0 + np.exp(-s))
+    else:
+        p = np.exp(s - s.max(axis=1, keepdims=True))
+        p = p / p.sum(axis=1, keepdims=True)
+    c = np.where(s > -np.inf, p + bias.astype(np.float64), -np.inf)
+    best = -np.sort(-c.reshape(T, E // S, S), axis=2)[:, :, :2]
+    value = np.where(best[:, :, 1] > -np.inf, best.sum(axis=2), best[:, :, 0])
+    kept = np.argsort(-value, axis=1, kind="stable")[:, :top_groups]
+    stays = np.zeros(value.shape, bool)
+    np.put_along_axis(stays, kept, True, 1)
+    c = np.where(np.repeat(stays, S, axis=1), c, -np.inf)
+    idx = np.argsort(-c, axis=1, kind="stable")[:, :k]
+    return np.where(np.take_along_axis(c, idx, 1) > -np.inf, idx, -1)
+
+
+@pytest.mark.parametrize("E,groups", [(32, 8), (64, 4), (24, 3)])
+@pytest.mark.parametrize("T", [50, 8500])
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_groups_whose_sum_is_beyond_fp32(E, groups, T, sigmoid):
+    """Two lowest biases add up to what fp32 does not hold; such a group still comes before one without an expert, and two largest before two smaller ones."""
+    S = E // groups
+    s = normal(T, E, E + T)
+    s[:, :S] = -np.inf                                # the first group has no expert
+    s[2::3, S:2 * S - 1] = np.nan                     # the second but one, sometimes
+    keep = min(S, 5)
+    s[:, 2 * S + keep:3 * S] = -np.inf
+    bias = np.full(E, -FMAX, np.float32)
+    bias[2 * S:3 * S] = 0.1
+    for top_groups, k in ((2, keep + 1), (1, 2)):
+        _, idx, _ = run(s, bias, k=k, groups=groups, top_groups=top_groups, top2=True, sigmoid=sigmoid)
+        assert np.array_equal(idx, groups_rule(s, bias, S=S, top_groups=top_groups, k=k, sigmoid=sigmoid))
+    bias = np.linspace(2e38, 3.4e38, E).astype(np.float32)
+    bias[E // 2:] = bias[:E // 2][::-1]
+    _, idx, _ = run(s, bias, k=2, groups=groups, top_groups=1, top2=True, sigmoid=sigmoid)
+    assert np.array_equal(idx, groups_rule(s, bias, S=S, top_groups=1, k=2, sigmoid=sigmoid))
