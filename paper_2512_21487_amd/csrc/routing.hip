@@ -382,8 +382,11 @@ __global__ __launch_bounds__(256, !BIASED || REGS < 32 ? REGS * K <= 256 ? 4 : 3
         }
         const bool stays = ahead < a.top_groups;   // (of a group without an expert every value says so)
         unsure = m1 > none && fabsf(m1) < __builtin_inff() && !(fabsf(value) < __builtin_inff());   // a sum that is beyond fp32, not beyond double
-        // an order hangs on the last group that stays and the first that does not
-        if (group_value) unsure |= close(over_lanes(stays ? value : __builtin_inff(), LANES, Least()), over_lanes(stays ? none : value, LANES, Most()), 2.f * slack);
+        // An order hangs on the last group that stays and the first that does not, each off by `off` at most: a p or two (half the slack, and half of that
+        // again), and the steps of the two numbers, of their sum, which may be far smaller than they are, and of the sum with `off` (2^-24 of both, three times).
+        const float off = m1 < __builtin_inff() ? 0.75f * slack + 0x1.9p-23f * fabsf(m1) + (a.group_top2 && m2 > none ? 0x1.9p-23f * fabsf(m2) : 0.f) : 0.f;
+        if (group_value)
+            unsure |= over_lanes(stays && value > none ? value - off : __builtin_inff(), LANES, Least()) <= over_lanes(!stays && value > none ? value + off : none, LANES, Most());
         if (!stays) {
 #pragma unroll
             for (int r = 0; r < REGS; ++r) v[r] = s[r] = none;

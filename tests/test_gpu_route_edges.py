@@ -65,3 +65,18 @@ def test_groups_whose_sum_is_beyond_fp32(E, groups, T, sigmoid):
     bias[E // 2:] = bias[:E // 2][::-1]
     _, idx, _ = run(s, bias, k=2, groups=groups, top_groups=1, top2=True, sigmoid=sigmoid)
     assert np.array_equal(idx, groups_rule(s, bias, S=S, top_groups=1, k=2, sigmoid=sigmoid))
+
+
+@pytest.mark.parametrize("opposite", [64.3, 1000.0, 3e5])
+@pytest.mark.parametrize("T", [8000, 30000])
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_groups_whose_two_best_nearly_cancel(opposite, T, sigmoid):
+    """A group's sum may be far smaller than the two numbers that were rounded for it."""
+    E, S = 16, 2
+    s = normal(T, E, 31)
+    # one of many such tokens: in fp32 the second group's sum is the larger one
+    s[0] = np.float32([-0.98689717, 0.34717762, -0.43605295, -0.14113410] * 4)
+    bias = np.tile(np.float32([opposite, -(opposite - 0.4)]), E // S)
+    for top_groups, k in ((1, 2), (3, 5)):
+        _, idx, _ = run(s, bias, k=k, groups=E // S, top_groups=top_groups, top2=True, sigmoid=sigmoid)
+        assert np.array_equal(idx, groups_rule(s, bias, S=S, top_groups=top_groups, k=k, sigmoid=sigmoid))
