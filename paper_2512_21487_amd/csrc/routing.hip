@@ -356,7 +356,7 @@ __global__ __launch_bounds__(256, !BIASED || REGS < 32 ? REGS * K <= 256 ? 4 : 3
         for (int r = 0; r < REGS; ++r) v[r] = s[r];
     }
     // Two values that close may be in the other order.  Of a sigmoid p is off by less than 2^-22 (exp2, its argument, a sum, the reciprocal); of a softmax the
-    // difference of two by 2^-21 and by 2^-19.3 of itself (their sum: 14 roundings in a row, and the arguments' of exponentials); c by half a step.  Twice all that.
+    // difference of two by 2^-21 and by 2^-19.3 of itself (their sum: 14 roundings in a row, and the arguments' of exponentials); c by half a step.  Twice all that (of a softmax 1.88 times).
     const float slack = a.sigmoid ? 0x1p-20f : 0x1p-18f;
     const auto close = [=](float x, float y, float by) { return x > none && y > none && !(fabsf(x - y) > by + 0x1p-22f * fmaxf(fabsf(x), fabsf(y))); };
     bool unsure = false;
