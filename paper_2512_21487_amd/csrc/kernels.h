@@ -234,6 +234,15 @@ struct LinearArgs {
     bool w32, out32;
     bool rows_first;   // set by the launcher: consecutive tiles are of one column tile
 };
+// What launch_linear launches on a device of n_cu compute units (tests name it): rows x columns of dot products, tiles, tiles through
+// registers, tiles whose reduction wavefronts share
+enum {
+    kLinearRows1x1 = 0, kLinearRows4x1, kLinearRows4x2,
+    kLinearTiled,   // 256 x 256, 256 x 192, 192 x 256, 128 x 128, 64 x 64
+    kLinearStaged128x64 = kLinearTiled + 5, kLinearStaged64x64,
+    kLinearSplit64x32by4, kLinearSplit64x32, kLinearSplit64x16, kLinearSplit32x16, kLinearSplit16x16
+};
+int linear_kernel(const LinearArgs& a, int n_cu);
 hipError_t launch_linear(const LinearArgs& a, int n_cu, hipStream_t s);
 
 // What the kernels are about to read or write through a caller's pointer (moe_ep.hip): NULL where it is usable, else what is wrong

@@ -829,7 +829,8 @@ double tiled_us(const Tiling& t, const LinearArgs& a, int n_cu)
     return rounds * ((a.K + 63) / 64 * (t.alone + (t.full - t.alone) * fill) + t.fixed);
 }
 
-hipError_t launch_tiled_best(const LinearArgs& a, int n_cu, hipStream_t s)
+// the tiling of kTilings that costs least
+int cheapest_tiling(const LinearArgs& a, int n_cu)
 {
     int best = 0;
     double us = 0.0;
@@ -837,53 +838,65 @@ hipError_t launch_tiled_best(const LinearArgs& a, int n_cu, hipStream_t s)
         const double t = tiled_us(kTilings[i], a, n_cu);
         if (kTilings[i].slots <= (a.K + 63) / 64 && (us == 0.0 || t < us)) { us = t; best = i; }
     }
-    switch (best) {
-    case 0: return launch_tiled<256, 256, 2, 1>(a, n_cu, s);
-    case 1: return launch_tiled<256, 192, 2, 1>(a, n_cu, s);
-    case 2: return launch_tiled<192, 256, 2, 1>(a, n_cu, s);
-    case 3: return launch_tiled<128, 128, 4, 1>(a, n_cu, s);
-    default: return launch_tiled<64, 64, 4, 2>(a, n_cu, s);
-    }
+    return best;
 }
 
 // The largest of the split tiles that still gives enough compute units work: half of them, three quarters where every tile also takes fp32
 // weights apart.
-hipError_t launch_split_best(const LinearArgs& a, int n_cu, hipStream_t s)
+int split_kernel(const LinearArgs& a, int n_cu)
 {
     const auto tiles = [&](int mb, int nb) { return (double)((a.R + mb * 16 - 1) / (mb * 16)) * ((a.N + nb * 16 - 1) / (nb * 16)); };
     const double enough = a.w32 ? 0.75 * n_cu : 0.5 * n_cu;
-    if (a.R > 32 && tiles(4, 2) >= 2 * n_cu) return launch_split<4, 2, 4>(a, s);
-    if (a.R > 32 && tiles(4, 2) >= enough) return launch_split<4, 2, 8>(a, s);
-    if (a.R > 32 && tiles(4, 1) >= enough) return launch_split<4, 1, 8>(a, s);
-    if (a.R > 16 && tiles(2, 1) >= enough) return launch_split<2, 1, 16>(a, s);
-    return launch_split<1, 1, 16>(a, s);
+    if (a.R > 32 && tiles(4, 2) >= 2 * n_cu) return kLinearSplit64x32by4;
+    if (a.R > 32 && tiles(4, 2) >= enough) return kLinearSplit64x32;
+    if (a.R > 32 && tiles(4, 1) >= enough) return kLinearSplit64x16;
+    if (a.R > 16 && tiles(2, 1) >= enough) return kLinearSplit32x16;
+    return kLinearSplit16x16;
 }
 
 }  // namespace
+
+int linear_kernel(const LinearArgs& a, int n_cu)
+{
+    const auto tiles = [&](int edge) { return (double)((a.R + edge - 1) / edge) * ((a.N + edge - 1) / edge); };
+    // Few blocks of 16 x 16 for a matrix instruction, and little to multiply.  Rows / split, us: 1, 16, 33 x 160 x 5120, fp32 weights, 3.1 / 8.6,
+    // 5.1 / 8.6, 6.5 / 8.7; 64, 256 x 128 x 4096 6.6 / 7.5, 17 / 9.1; bf16 weights, 1, 8 x 2048 x 1408 3.6 / 3.8, 7.6 / 3.9.
+    const double products = (double)a.R * a.N * a.K;
+    if ((products <= 40e6 && tiles(16) < n_cu / 2) || products <= 3e6) return a.R <= 8 ? kLinearRows1x1 : a.R <= 16 ? kLinearRows4x1 : kLinearRows4x2;
+    // The tiled kernels move 16 bytes at a time, and are a K step ahead at least.  Of few tiles, each a compute unit's, a long K is better shared:
+    // tiled / split, us: 64 x 1536 x 5120 17 / 9.7; 64 x 5120 x 2048 9.8 / 9.5, 256 x 2048 x 2048 9.6 / 12.
+    const bool by_16 = !a.w32 && a.K > 64 && a.K % 8 == 0 && a.ldx % 8 == 0 && a.ldw % 8 == 0 && !((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w)) & 15);
+    if (by_16 && a.R > 64 && tiles(64) >= n_cu / 4) return kLinearTiled + cheapest_tiling(a, n_cu);
+    // Operands that are not on 16 bytes: 64 x 64 tiles / 128 x 64 tiles / split, us: 1531 x 1409 x 2049 39 / 43 / 49, 3112 x 839 x 182 8.9 / 11 / 12,
+    // 8192 x 2048 x 2049 197 / 149 / 260, 16384 x 5120 x 1001 486 / 426 / 755; of few tiles 300 x 1409 x 2049 27 / 37 / 14.
+    if (!a.w32 && !by_16 && a.K > 64) {
+        if (2 * tiles(128) >= 4 * n_cu) return kLinearStaged128x64;
+        if (tiles(64) >= 1.5 * n_cu) return kLinearStaged64x64;
+    }
+    return split_kernel(a, n_cu);
+}
 
 hipError_t launch_linear(const LinearArgs& a, int n_cu, hipStream_t s)
 {
     if (a.R <= 0) return hipSuccess;
     if (a.N < 1 || a.K < 1) return hipErrorInvalidValue;
-    const auto tiles = [&](int edge) { return (double)((a.R + edge - 1) / edge) * ((a.N + edge - 1) / edge); };
-    // Few blocks of 16 x 16 for a matrix instruction, and little to multiply.  Rows / split, us: 1, 16, 33 x 160 x 5120, fp32 weights, 3.1 / 8.6,
-    // 5.1 / 8.6, 6.5 / 8.7; 64, 256 x 128 x 4096 6.6 / 7.5, 17 / 9.1; bf16 weights, 1, 8 x 2048 x 1408 3.6 / 3.8, 7.6 / 3.9.
-    const double products = (double)a.R * a.N * a.K;
-    if ((products <= 40e6 && tiles(16) < n_cu / 2) || products <= 3e6) {
-        if (a.R <= 8) return launch_rows<1, 1>(a, s);
-        return a.R <= 16 ? launch_rows<4, 1>(a, s) : launch_rows<4, 2>(a, s);
+    switch (linear_kernel(a, n_cu)) {
+    case kLinearRows1x1: return launch_rows<1, 1>(a, s);
+    case kLinearRows4x1: return launch_rows<4, 1>(a, s);
+    case kLinearRows4x2: return launch_rows<4, 2>(a, s);
+    case kLinearTiled + 0: return launch_tiled<256, 256, 2, 1>(a, n_cu, s);
+    case kLinearTiled + 1: return launch_tiled<256, 192, 2, 1>(a, n_cu, s);
+    case kLinearTiled + 2: return launch_tiled<192, 256, 2, 1>(a, n_cu, s);
+    case kLinearTiled + 3: return launch_tiled<128, 128, 4, 1>(a, n_cu, s);
+    case kLinearTiled + 4: return launch_tiled<64, 64, 4, 2>(a, n_cu, s);
+    case kLinearStaged128x64: return launch_tiled<128, 64, 2, 2, true>(a, n_cu, s);
+    case kLinearStaged64x64: return launch_tiled<64, 64, 2, 3, true>(a, n_cu, s);
+    case kLinearSplit64x32by4: return launch_split<4, 2, 4>(a, s);
+    case kLinearSplit64x32: return launch_split<4, 2, 8>(a, s);
+    case kLinearSplit64x16: return launch_split<4, 1, 8>(a, s);
+    case kLinearSplit32x16: return launch_split<2, 1, 16>(a, s);
+    default: return launch_split<1, 1, 16>(a, s);
     }
-    // The tiled kernels move 16 bytes at a time, and are a K step ahead at least.  Of few tiles, each a compute unit's, a long K is better shared:
-    // tiled / split, us: 64 x 1536 x 5120 17 / 9.7; 64 x 5120 x 2048 9.8 / 9.5, 256 x 2048 x 2048 9.6 / 12.
-    const bool by_16 = !a.w32 && a.K > 64 && a.K % 8 == 0 && a.ldx % 8 == 0 && a.ldw % 8 == 0 && !((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w)) & 15);
-    if (by_16 && a.R > 64 && tiles(64) >= n_cu / 4) return launch_tiled_best(a, n_cu, s);
-    // Operands that are not on 16 bytes: 64 x 64 tiles / 128 x 64 tiles / split, us: 1531 x 1409 x 2049 39 / 43 / 49, 3112 x 839 x 182 8.9 / 11 / 12,
-    // 8192 x 2048 x 2049 197 / 149 / 260, 16384 x 5120 x 1001 486 / 426 / 755; of few tiles 300 x 1409 x 2049 27 / 37 / 14.
-    if (!a.w32 && !by_16 && a.K > 64) {
-        if (2 * tiles(128) >= 4 * n_cu) return launch_tiled<128, 64, 2, 2, true>(a, n_cu, s);
-        if (tiles(64) >= 1.5 * n_cu) return launch_tiled<64, 64, 2, 3, true>(a, n_cu, s);
-    }
-    return launch_split_best(a, n_cu, s);
 }
 
 }  // namespace moe_ep
