@@ -34,7 +34,7 @@ __device__ __forceinline__ float gelu_f(float z)
     const float x = fabsf(z) * 0.7071067811865476f;
     const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
     const float q = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-    const float h = 0.5f * z * (q * exp_f(-x * x));   // 0.5 z (1 - erf(x))
+    const float h = 0.5f * fminf(z, __FLT_MAX__) * (q * exp_f(-x * x));   // 0.5 z (1 - erf(x)), 0 of plus infinity
     return z >= 0.f ? z - h : h;
 }
 

@@ -52,3 +52,32 @@ def test_fp32_weights_count_to_the_last_bit_on_every_kernel_that_takes_them(name
     pkg.linear(pkg.LinearConfig(in_features=K, out_features=N, weight_type=pkg.F32, out_type=pkg.F32), x, w, out=out)
     torch.cuda.synchronize()
     assert bool((out == -(K // 2) * 2.0 ** -23).all())
+
+
+@pytest.mark.parametrize("name,R,N,K,w32", ALL)
+def test_activations_of_numbers_that_are_huge_or_infinite(name, R, N, K, w32):
+    """A pre-activation of plus infinity, or that overflows, is one of every activation; a huge one is itself, a huge negative one 0 but without an activation."""
+    import paper_2512_21487_amd as pkg
+    runs_on(name, R, N, K, w32)
+    huge = (float("inf"), 1e30, -1e30, 3e38, -3e38)
+    for out32 in (False, True):
+        for act in ACTS:
+            c = Case(R, N, K, w32=w32, out32=out32, bias=True, name=act)
+            cols = range(0, 10, 2)
+            for n, v in zip(cols, huge):
+                c.b[n] = v
+            if not w32:                                   # 3e38 + 3e38 in the sum
+                c.w[1, :2] = 2.0
+                c.x[R - 1, :2] = 3e38
+            c.run()
+            torch.cuda.synchronize()
+            for n, v in zip(cols, huge):
+                got = c.out[:R - 1, n].double()
+                if v > 0 or act == "none":
+                    want = torch.full_like(got, v) if not out32 else torch.full_like(got, float(torch.tensor(v, dtype=torch.float32)))
+                    assert torch.equal(got, want) if v == float("inf") else bool(((got - want).abs() <= 2.0 ** -8 * abs(v)).all())
+                else:
+                    assert bool((got == 0).all())
+            if not w32:
+                assert float(c.out[R - 1, 1]) == float("inf")
+            assert bool(torch.isfinite(c.out[:R - 1, 10:]).all()) and bool(torch.isfinite(c.out[:R - 1, 1::2]).all())
