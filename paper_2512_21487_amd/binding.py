@@ -297,8 +297,25 @@ def _current_stream(device: int) -> int:
         return 0
 
 
-def _rows(x, name: str, n_rows: int, cols: int, stride: int, size: int) -> Optional[int]:
-    """Address of an argument of rows that may lie apart.  A torch tensor is checked: element size, at least ``n_rows`` rows of
+_I32, _BYTE = 2, 3             # kinds of elements beside BF16 and F32
+_SIZES = (2, 4, 4, 1)
+_kinds = (set(), set(), set(), set())   # what a torch tensor of a kind may be typed as; filled at the first one
+
+
+def _check_type(x, name: str, kind: int) -> None:
+    if x.element_size() != _SIZES[kind]:
+        raise ValueError(f"{name} has elements of {x.element_size()} bytes, the call reads {_SIZES[kind]}")
+    if not _kinds[kind]:
+        import torch
+        # bf16 may come as integers that hold its bits
+        for have, types in zip(_kinds, ((torch.bfloat16, torch.int16, torch.uint16), (torch.float32,), (torch.int32,), (torch.uint8, torch.int8, torch.bool))):
+            have.update(types)
+    if x.dtype not in _kinds[kind]:
+        raise ValueError(f"{name} holds {x.dtype}, the call reads {('bfloat16', 'float32', 'int32', 'bytes')[kind]}")
+
+
+def _rows(x, name: str, n_rows: int, cols: int, stride: int, kind: int) -> Optional[int]:
+    """Address of an argument of rows that may lie apart.  A torch tensor is checked: its type, at least ``n_rows`` rows of
     ``cols`` contiguous elements ``stride`` apart, on the GPU (raw addresses pass through)."""
     if x is None:
         return None
@@ -307,10 +324,9 @@ def _rows(x, name: str, n_rows: int, cols: int, stride: int, size: int) -> Optio
     except (AttributeError, TypeError):
         return _ptr(x)
     # the usual case, decided in half the time
-    if len(have) == 2 and have[0] >= n_rows and have[1] >= cols and apart[1] == 1 and apart[0] == stride and x.is_cuda and x.element_size() == size:
+    if len(have) == 2 and have[0] >= n_rows and have[1] >= cols and apart[1] == 1 and apart[0] == stride and x.is_cuda and x.dtype in _kinds[kind]:
         return x.data_ptr()
-    if x.element_size() != size:
-        raise ValueError(f"{name} has elements of {x.element_size()} bytes, the call reads {size}")
+    _check_type(x, name, kind)
     if not (x.is_cuda or x.is_pinned()):
         raise ValueError(f"{name} must be a device tensor")
     if len(have) == 1 and n_rows == 1:
@@ -324,15 +340,17 @@ def _rows(x, name: str, n_rows: int, cols: int, stride: int, size: int) -> Optio
     return x.data_ptr()
 
 
-def _vector(x, name: str, n: int, size: int) -> Optional[int]:
-    """Address of a contiguous argument; a torch tensor is checked for n elements of ``size`` bytes on the GPU."""
+def _vector(x, name: str, n: int, kind: int) -> Optional[int]:
+    """Address of a contiguous argument; a torch tensor is checked for its type and n elements on the GPU."""
     if x is None:
         return None
     try:
-        if x.numel() < n or x.element_size() != size or not x.is_contiguous():
-            raise ValueError(f"{name} must be {n} contiguous elements of {size} bytes")
+        if x.numel() < n or x.element_size() != _SIZES[kind] or not x.is_contiguous():
+            raise ValueError(f"{name} must be {n} contiguous elements of {_SIZES[kind]} bytes")
     except AttributeError:
         return _ptr(x)
+    if x.dtype not in _kinds[kind]:
+        _check_type(x, name, kind)
     if not (x.is_cuda or x.is_pinned()):
         raise ValueError(f"{name} must be a device tensor")
     return x.data_ptr()
@@ -354,9 +372,9 @@ def route(rule: Routing, scores, bias=None, token_mask=None, n_tokens: Optional[
     k, E = rule.top_k, rule.n_experts
     why = ctypes.c_char_p()
     rc = (_lib or load_library()).moe_ep_route(
-        ctypes.byref(rule), _rows(scores, "scores", n_tokens, E, rule.score_stride or E, 4 if rule.score_type else 2),
-        _vector(bias, "bias", E, 4), _vector(token_mask, "token_mask", n_tokens, 1), n_tokens, _vector(idx, "idx", n_tokens * k, 4),
-        _vector(w, "w", n_tokens * k, 4), stream, ctypes.byref(why))
+        ctypes.byref(rule), _rows(scores, "scores", n_tokens, E, rule.score_stride or E, F32 if rule.score_type else BF16),
+        _vector(bias, "bias", E, F32), _vector(token_mask, "token_mask", n_tokens, _BYTE), n_tokens, _vector(idx, "idx", n_tokens * k, _I32),
+        _vector(w, "w", n_tokens * k, F32), stream, ctypes.byref(why))
     if rc != 0:
         raise MoeEpError(rc, (why.value or b"").decode())
     return rc
@@ -376,12 +394,12 @@ def linear(cfg: LinearConfig, x, weight, bias=None, residual=None, out=None, n_r
     if stream is None:
         stream = _current_stream(cfg.device)
     K, N = cfg.in_features, cfg.out_features
-    size = 4 if cfg.out_type else 2
+    result = F32 if cfg.out_type else BF16
     why = ctypes.c_char_p()
     rc = (_lib or load_library()).moe_ep_linear(
-        ctypes.byref(cfg), _rows(x, "x", n_rows, K, cfg.x_stride or K, 2), _rows(weight, "weight", N, K, cfg.weight_stride or K, 4 if cfg.weight_type else 2),
-        _vector(bias, "bias", N, 4), _rows(residual, "residual", n_rows, N, cfg.residual_stride or N, size), n_rows,
-        _rows(out, "out", n_rows, N, cfg.out_stride or N, size), stream, ctypes.byref(why))
+        ctypes.byref(cfg), _rows(x, "x", n_rows, K, cfg.x_stride or K, BF16), _rows(weight, "weight", N, K, cfg.weight_stride or K, F32 if cfg.weight_type else BF16),
+        _vector(bias, "bias", N, F32), _rows(residual, "residual", n_rows, N, cfg.residual_stride or N, result), n_rows,
+        _rows(out, "out", n_rows, N, cfg.out_stride or N, result), stream, ctypes.byref(why))
     if rc != 0:
         raise MoeEpError(rc, (why.value or b"").decode())
     return rc
@@ -559,8 +577,8 @@ class MoeEp:
     # -- moe_ep_set_routing -----------------------------------------------------------------
     def set_routing(self, rule: Optional[Routing] = None, bias=None) -> int:
         """Later forwards route by ``rule`` (None: as a new context); the context keeps ``bias`` alive."""
-        rc = self._lib.moe_ep_set_routing(self._ctx, ctypes.byref(rule) if rule is not None else None,
-                                          _vector(bias, "bias", self.cfg.n_experts, 4))
+        at = _vector(bias, "bias", self.cfg.n_experts, F32)
+        rc = self._lib.moe_ep_set_routing(self._ctx, ctypes.byref(rule) if rule is not None else None, at)
         if rc != 0:
             raise MoeEpError(rc, self.last_error())
         self._routing_bias = bias
