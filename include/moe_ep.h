@@ -254,7 +254,7 @@ int moe_ep_validate_routing(const moe_ep_routing *rule, const char **why);
  *   why         may be NULL; receives a string naming the first violated rule or the failed HIP call (valid until
  *               the calling thread's next call)
  * All pointers are GPU-addressable memory; what they point at is checked as moe_ep_forward does (MOE_EP_CHECK_POINTERS, read once).
- * The rule's device need not be the current one, which the call leaves as it was.  n_tokens == 0 is a no-op.
+ * Device memory has to be the rule's device's own, which need not be the current one; the call leaves that as it was.  n_tokens == 0 is a no-op.
  */
 int moe_ep_route(const moe_ep_routing *rule, const void *scores, const float *bias, const uint8_t *token_mask,
                  int32_t n_tokens, int32_t *idx, float *w, void *stream, const char **why);

@@ -314,9 +314,18 @@ def _check_type(x, name: str, kind: int) -> None:
         raise ValueError(f"{name} holds {x.dtype}, the call reads {('bfloat16', 'float32', 'int32', 'bytes')[kind]}")
 
 
-def _rows(x, name: str, n_rows: int, cols: int, stride: int, kind: int) -> Optional[int]:
+def _check_place(x, name: str, device: int) -> None:
+    if not (x.is_cuda or x.is_pinned()):
+        raise ValueError(f"{name} must be a device tensor")
+    if x.is_cuda and x.get_device() != device:
+        import torch
+        if device < torch.cuda.device_count():   # of no such device the call says so
+            raise ValueError(f"{name} is on {x.device}, the call runs on device {device}")
+
+
+def _rows(x, name: str, n_rows: int, cols: int, stride: int, kind: int, device: int) -> Optional[int]:
     """Address of an argument of rows that may lie apart.  A torch tensor is checked: its type, at least ``n_rows`` rows of
-    ``cols`` contiguous elements ``stride`` apart, on the GPU (raw addresses pass through)."""
+    ``cols`` contiguous elements ``stride`` apart, on the call's GPU (raw addresses pass through)."""
     if x is None:
         return None
     try:
@@ -324,11 +333,10 @@ def _rows(x, name: str, n_rows: int, cols: int, stride: int, kind: int) -> Optio
     except (AttributeError, TypeError):
         return _ptr(x)
     # the usual case, decided in half the time
-    if len(have) == 2 and have[0] >= n_rows and have[1] >= cols and apart[1] == 1 and apart[0] == stride and x.is_cuda and x.dtype in _kinds[kind]:
+    if len(have) == 2 and have[0] >= n_rows and have[1] >= cols and apart[1] == 1 and apart[0] == stride and x.get_device() == device and x.dtype in _kinds[kind]:
         return x.data_ptr()
     _check_type(x, name, kind)
-    if not (x.is_cuda or x.is_pinned()):
-        raise ValueError(f"{name} must be a device tensor")
+    _check_place(x, name, device)
     if len(have) == 1 and n_rows == 1:
         if have[0] < cols or (cols > 1 and apart[0] != 1):
             raise ValueError(f"{name} must be a contiguous row of {cols}")
@@ -340,8 +348,8 @@ def _rows(x, name: str, n_rows: int, cols: int, stride: int, kind: int) -> Optio
     return x.data_ptr()
 
 
-def _vector(x, name: str, n: int, kind: int) -> Optional[int]:
-    """Address of a contiguous argument; a torch tensor is checked for its type and n elements on the GPU."""
+def _vector(x, name: str, n: int, kind: int, device: int) -> Optional[int]:
+    """Address of a contiguous argument; a torch tensor is checked for its type and n elements on the call's GPU."""
     if x is None:
         return None
     try:
@@ -351,8 +359,8 @@ def _vector(x, name: str, n: int, kind: int) -> Optional[int]:
         return _ptr(x)
     if x.dtype not in _kinds[kind]:
         _check_type(x, name, kind)
-    if not (x.is_cuda or x.is_pinned()):
-        raise ValueError(f"{name} must be a device tensor")
+    if x.get_device() != device:
+        _check_place(x, name, device)
     return x.data_ptr()
 
 
@@ -369,12 +377,12 @@ def route(rule: Routing, scores, bias=None, token_mask=None, n_tokens: Optional[
         n_tokens = int(scores.shape[0])
     if stream is None:
         stream = _current_stream(rule.device)
-    k, E = rule.top_k, rule.n_experts
+    k, E, at = rule.top_k, rule.n_experts, rule.device
     why = ctypes.c_char_p()
     rc = (_lib or load_library()).moe_ep_route(
-        ctypes.byref(rule), _rows(scores, "scores", n_tokens, E, rule.score_stride or E, F32 if rule.score_type else BF16),
-        _vector(bias, "bias", E, F32), _vector(token_mask, "token_mask", n_tokens, _BYTE), n_tokens, _vector(idx, "idx", n_tokens * k, _I32),
-        _vector(w, "w", n_tokens * k, F32), stream, ctypes.byref(why))
+        ctypes.byref(rule), _rows(scores, "scores", n_tokens, E, rule.score_stride or E, F32 if rule.score_type else BF16, at),
+        _vector(bias, "bias", E, F32, at), _vector(token_mask, "token_mask", n_tokens, _BYTE, at), n_tokens, _vector(idx, "idx", n_tokens * k, _I32, at),
+        _vector(w, "w", n_tokens * k, F32, at), stream, ctypes.byref(why))
     if rc != 0:
         raise MoeEpError(rc, (why.value or b"").decode())
     return rc
@@ -393,13 +401,13 @@ def linear(cfg: LinearConfig, x, weight, bias=None, residual=None, out=None, n_r
         n_rows = int(x.shape[0])
     if stream is None:
         stream = _current_stream(cfg.device)
-    K, N = cfg.in_features, cfg.out_features
+    K, N, at = cfg.in_features, cfg.out_features, cfg.device
     result = F32 if cfg.out_type else BF16
     why = ctypes.c_char_p()
     rc = (_lib or load_library()).moe_ep_linear(
-        ctypes.byref(cfg), _rows(x, "x", n_rows, K, cfg.x_stride or K, BF16), _rows(weight, "weight", N, K, cfg.weight_stride or K, F32 if cfg.weight_type else BF16),
-        _vector(bias, "bias", N, F32), _rows(residual, "residual", n_rows, N, cfg.residual_stride or N, result), n_rows,
-        _rows(out, "out", n_rows, N, cfg.out_stride or N, result), stream, ctypes.byref(why))
+        ctypes.byref(cfg), _rows(x, "x", n_rows, K, cfg.x_stride or K, BF16, at), _rows(weight, "weight", N, K, cfg.weight_stride or K, F32 if cfg.weight_type else BF16, at),
+        _vector(bias, "bias", N, F32, at), _rows(residual, "residual", n_rows, N, cfg.residual_stride or N, result, at), n_rows,
+        _rows(out, "out", n_rows, N, cfg.out_stride or N, result, at), stream, ctypes.byref(why))
     if rc != 0:
         raise MoeEpError(rc, (why.value or b"").decode())
     return rc
@@ -577,8 +585,8 @@ class MoeEp:
     # -- moe_ep_set_routing -----------------------------------------------------------------
     def set_routing(self, rule: Optional[Routing] = None, bias=None) -> int:
         """Later forwards route by ``rule`` (None: as a new context); the context keeps ``bias`` alive."""
-        at = _vector(bias, "bias", self.cfg.n_experts, F32)
-        rc = self._lib.moe_ep_set_routing(self._ctx, ctypes.byref(rule) if rule is not None else None, at)
+        address = _vector(bias, "bias", self.cfg.n_experts, F32, self.cfg.device)
+        rc = self._lib.moe_ep_set_routing(self._ctx, ctypes.byref(rule) if rule is not None else None, address)
         if rc != 0:
             raise MoeEpError(rc, self.last_error())
         self._routing_bias = bias

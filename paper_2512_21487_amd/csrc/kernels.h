@@ -245,7 +245,8 @@ enum {
 int linear_kernel(const LinearArgs& a, int n_cu);
 hipError_t launch_linear(const LinearArgs& a, int n_cu, hipStream_t s);
 
-// What the kernels are about to read or write through a caller's pointer (moe_ep.hip): NULL where it is usable, else what is wrong
-const char* check_span(const void* p, size_t bytes, bool want_host, const void** dev_ptr);
+// What the kernels are about to read or write through a caller's pointer (moe_ep.hip): NULL where it is usable, else what is wrong.
+// device: the one that device memory has to be on, or -1
+const char* check_span(const void* p, size_t bytes, bool want_host, const void** dev_ptr, int device = -1);
 
 }  // namespace moe_ep

@@ -320,7 +320,7 @@ int fail(moe_ep_ctx* ctx, int code, const char* what, hipError_t e = hipSuccess)
 // pointer or an undersized buffer into an error before a kernel faults on it.  Returns nullptr when
 // the span is usable, else what is wrong with it.  `want_host`: pinned host memory is required
 // (the link stand-ins of MOE_EP_IO_PINNED_HOST); *dev_ptr receives the address kernels use.
-const char* moe_ep::check_span(const void* p, size_t bytes, bool want_host, const void** dev_ptr)
+const char* moe_ep::check_span(const void* p, size_t bytes, bool want_host, const void** dev_ptr, int device)
 {
     hipPointerAttribute_t attr;
     if (hipPointerGetAttributes(&attr, p) != hipSuccess) {
@@ -341,6 +341,7 @@ const char* moe_ep::check_span(const void* p, size_t bytes, bool want_host, cons
     }
     if (attr.type != hipMemoryTypeDevice && attr.type != hipMemoryTypeManaged && attr.type != hipMemoryTypeUnified)
         return "is not memory the GPU can address";
+    if (device >= 0 && attr.type == hipMemoryTypeDevice && attr.device != device) return "is memory of another device than the call's";
     hipDeviceptr_t base = nullptr;
     size_t size = 0;
     if (hipMemGetAddressRange(&base, &size, const_cast<void*>(p)) != hipSuccess) {
@@ -612,7 +613,7 @@ int moe_ep_set_routing(moe_ep_ctx* ctx, const moe_ep_routing* rule, const float*
     if (reinterpret_cast<uintptr_t>(bias) & 3) return fail(ctx, MOE_EP_EINVAL, "bias must be aligned to its elements");
     if (bias && ctx->check_spans) {
         HIP_TRY(ctx, hipSetDevice(c.device));
-        if (const char* bad = check_span(bias, (size_t)c.n_experts * 4, false, nullptr)) {
+        if (const char* bad = check_span(bias, (size_t)c.n_experts * 4, false, nullptr, c.device)) {
             snprintf(ctx->err, sizeof ctx->err, "bias %s", bad);
             return MOE_EP_EINVAL;
         }

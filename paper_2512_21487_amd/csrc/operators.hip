@@ -69,12 +69,12 @@ const char* overlap(const Span* sp, int n)
         }
     return nullptr;
 }
-// a buffer that the GPU cannot read or write, or NULL
-const char* out_of_reach(const Span* sp, int n)
+// a buffer that the device cannot read or write, or NULL
+const char* out_of_reach(const Span* sp, int n, int device)
 {
     for (int i = 0; i < n && checks_pointers(); ++i) {
         if (!sp[i].p) continue;
-        if (const char* bad = check_span(sp[i].p, extent(sp[i]), false, nullptr)) {
+        if (const char* bad = check_span(sp[i].p, extent(sp[i]), false, nullptr, device)) {
             snprintf(t_text, sizeof t_text, "%s %s", sp[i].name, bad);
             return t_text;
         }
@@ -130,7 +130,7 @@ int moe_ep_route(const moe_ep_routing* r, const void* scores, const float* bias,
     if (const char* bad = overlap(sp, 5)) return refuse(why, bad);
     DeviceScope device(r->device);
     if (device.error != hipSuccess) return hip_failed(why, "selecting the device", device.error);
-    if (const char* bad = out_of_reach(sp, 5)) return refuse(why, bad);
+    if (const char* bad = out_of_reach(sp, 5, r->device)) return refuse(why, bad);
     const int groups = r->n_groups == 0 ? 1 : r->n_groups;
     const RouteArgs a{scores, bias, token_mask, idx, w, stride, n_tokens, r->n_experts, r->top_k, groups, groups > 1 ? r->top_groups : 1,
                       r->score_type == MOE_EP_BF16, r->score == MOE_EP_SCORE_SIGMOID, r->group_score == MOE_EP_GROUP_TOP2, r->renormalise != 0, r->scale};
@@ -180,7 +180,7 @@ int moe_ep_linear(const moe_ep_linear_config* c, const void* x, const void* weig
     if (const char* bad = overlap(sp, 5)) return refuse(why, bad);
     DeviceScope device(c->device);
     if (device.error != hipSuccess) return hip_failed(why, "selecting the device", device.error);
-    if (const char* bad = out_of_reach(sp, 5)) return refuse(why, bad);
+    if (const char* bad = out_of_reach(sp, 5, c->device)) return refuse(why, bad);
     LinearArgs a{};
     a.x = static_cast<const uint16_t*>(x); a.w = weight; a.bias = bias; a.residual = residual; a.out = out;
     a.ldx = ldx; a.ldw = ldw; a.ldr = ldr; a.ldo = ldo;

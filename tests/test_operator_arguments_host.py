@@ -61,3 +61,29 @@ def test_unknown_types_are_named_by_the_call():
         linear(weight_type=7)
     with pytest.raises(pkg.MoeEpError, match="out_type"):
         linear(out_type=-1)
+
+
+class On:
+    """A tensor as if on another GPU."""
+
+    def __init__(self, t, device):
+        self._t, self._device, self.is_cuda, self.device = t, device, True, torch.device("cuda", device)
+
+    def get_device(self):
+        return self._device
+
+    def __getattr__(self, name):
+        return getattr(self._t, name)
+
+
+@pytest.mark.parametrize("call,name,shape,dtype", [
+    (linear, "x", (4, 64), torch.bfloat16), (linear, "weight", (32, 64), torch.bfloat16), (linear, "bias", (32,), torch.float32),
+    (linear, "residual", (4, 32), torch.bfloat16), (linear, "out", (4, 32), torch.bfloat16), (route, "scores", (4, 64), torch.float32),
+    (route, "bias", (64,), torch.float32), (route, "token_mask", (4,), torch.uint8), (route, "idx", (4, 6), torch.int32), (route, "w", (4, 6), torch.float32)])
+def test_tensors_of_another_device(call, name, shape, dtype, monkeypatch):
+    """A config that was not told of a device runs on the first one, and on its stream."""
+    monkeypatch.setattr(torch.cuda, "device_count", lambda: 2)
+    with pytest.raises(ValueError, match=f"{name} is on cuda:1, .* device 0"):
+        call(**{name: On(zeros(*shape, dtype=dtype), 1)})
+    with pytest.raises(pkg.MoeEpError):   # of this one: there is no GPU here, or it is no memory of one
+        call(**{name: On(zeros(*shape, dtype=dtype), 0)})
