@@ -89,7 +89,18 @@ GROUP_MAX, GROUP_TOP2 = 0, 1
 ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = 0, 1, 2, 3, 4
 
 
-class Routing(ctypes.Structure):
+class _Fields(ctypes.Structure):
+    """A structure whose integer fields refuse what they do not hold (ctypes would keep the lower bits)."""
+
+    def __setattr__(self, name, value):
+        before = getattr(self, name, None)
+        super().__setattr__(name, value)
+        if isinstance(before, int) and getattr(self, name) != value:
+            super().__setattr__(name, before)
+            raise ValueError(f"{name} does not hold {value}")
+
+
+class Routing(_Fields):
     """Mirror of ``moe_ep_routing``; fields that are not named are 0, but for a scale of 1."""
     _fields_ = [(n, ctypes.c_int32) for n in (
         "n_experts", "top_k", "n_groups", "top_groups", "score", "group_score", "renormalise", "score_type",
@@ -101,7 +112,7 @@ class Routing(ctypes.Structure):
         super().__init__(*args, **kw)
 
 
-class LinearConfig(ctypes.Structure):
+class LinearConfig(_Fields):
     """Mirror of ``moe_ep_linear_config``; fields that are not named are 0."""
     _fields_ = [(n, ctypes.c_int32) for n in (
         "in_features", "out_features", "weight_type", "out_type", "activation", "device")] + [
@@ -283,6 +294,7 @@ def forward_noalloc(cfg: MoeEpConfig, tokens, gate_logits, routed_w, shared_w, t
 
 
 _raw_stream = None
+_MOST_ROWS = 1 << 30
 
 
 def _current_stream(device: int) -> int:
@@ -375,6 +387,8 @@ def route(rule: Routing, scores, bias=None, token_mask=None, n_tokens: Optional[
     """moe_ep_route: ``idx`` (int32) and ``w`` (fp32), both [n_tokens, top_k], from the scores by ``rule``."""
     if n_tokens is None:
         n_tokens = int(scores.shape[0])
+    if not 0 <= n_tokens <= _MOST_ROWS:   # an int32 argument would take the lower bits
+        raise MoeEpError(-1, "n_tokens must be in 0..2^30")
     if stream is None:
         stream = _current_stream(rule.device)
     k, E, at = rule.top_k, rule.n_experts, rule.device
@@ -399,6 +413,8 @@ def linear(cfg: LinearConfig, x, weight, bias=None, residual=None, out=None, n_r
     """moe_ep_linear: out = act(x weight^T + bias) + residual."""
     if n_rows is None:
         n_rows = int(x.shape[0])
+    if not 0 <= n_rows <= _MOST_ROWS:
+        raise MoeEpError(-1, "n_rows must be in 0..2^30")
     if stream is None:
         stream = _current_stream(cfg.device)
     K, N, at = cfg.in_features, cfg.out_features, cfg.device

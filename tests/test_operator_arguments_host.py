@@ -87,3 +87,25 @@ def test_tensors_of_another_device(call, name, shape, dtype, monkeypatch):
         call(**{name: On(zeros(*shape, dtype=dtype), 1)})
     with pytest.raises(pkg.MoeEpError):   # of this one: there is no GPU here, or it is no memory of one
         call(**{name: On(zeros(*shape, dtype=dtype), 0)})
+
+
+def test_counts_of_rows_that_32_bits_do_not_hold():
+    for n in (2 ** 32, 2 ** 32 + 4, 2 ** 31, -2 ** 32 + 4):
+        with pytest.raises(pkg.MoeEpError, match="n_rows must be in 0..2.30") as ei:
+            linear(n_rows=n)
+        assert ei.value.code == -1
+        with pytest.raises(pkg.MoeEpError, match="n_tokens must be in 0..2.30") as ei:
+            route(n_tokens=n)
+        assert ei.value.code == -1
+
+
+@pytest.mark.parametrize("make,name,value", [
+    (pkg.LinearConfig, "in_features", 2 ** 32 + 64), (pkg.LinearConfig, "out_features", 2 ** 31), (pkg.LinearConfig, "x_stride", 2 ** 64 + 64),
+    (pkg.LinearConfig, "activation", -2 ** 32 + 1), (pkg.Routing, "n_experts", 2 ** 32 + 8), (pkg.Routing, "score_stride", 2 ** 63)])
+def test_fields_that_do_not_hold_a_number(make, name, value):
+    with pytest.raises(ValueError, match=name):
+        make(**{name: value})
+    made = make(device=1)
+    with pytest.raises(ValueError, match=name):
+        setattr(made, name, value)
+    assert getattr(made, name) == 0 and made.device == 1
