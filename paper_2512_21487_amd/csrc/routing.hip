@@ -435,10 +435,10 @@ __global__ __launch_bounds__(256, !BIASED || REGS < 32 ? REGS * K <= 256 ? 4 : 3
         const float value = full ? ranked_value(mine) : none, be = full ? a.bias[e] : 0.f;
         const int base = lane & ~(LANES - 1), next = lane + 1;
         const float nv = __shfl(value, next, 64), ns = __shfl(se, next, 64), nb = __shfl(be, next, 64);
-        bool near = sub < k && sub + 1 < K && close(value, nv, slack) && !(se == ns && be == nb);
         const float lv = __shfl(value, base + k - 1, 64);
         float line = lv > none ? lv - (slack + 0x1p-21f * fabsf(lv)) : __builtin_inff();   // a last slot that is empty has nobody behind it
         line = line < -__FLT_MAX__ ? -__FLT_MAX__ : line;   // nor are those that are not there behind one whose bias is the lowest number
+        bool near = (sub < k || value >= line) && sub + 1 < K && close(value, nv, slack) && !(se == ns && be == nb);
         int found = 0;
 #pragma unroll
         for (int r = 0; r < REGS; ++r) found += __popcll(__ballot(v[r] >= line));

@@ -80,3 +80,30 @@ def test_groups_whose_two_best_nearly_cancel(opposite, T, sigmoid):
     for top_groups, k in ((1, 2), (3, 5)):
         _, idx, _ = run(s, bias, k=k, groups=E // S, top_groups=top_groups, top2=True, sigmoid=sigmoid)
         assert np.array_equal(idx, groups_rule(s, bias, S=S, top_groups=top_groups, k=k, sigmoid=sigmoid))
+
+
+# p is less than a step of fp32 beside a bias of 1, or a sigmoid's 1 but for one that double alone holds
+def steps_below_fp32(rng, T, E, sigmoid):
+    if sigmoid:
+        return rng.choice(np.float32([20.0, 24.0, 30.5, 33.0, 36.0, 41.25, 50.25, np.inf]), (T, E)), np.full(E, 1.0, np.float32)
+    s = rng.choice(np.float32([-19.0, -19.5, -20.0, -20.5, -21.0, -22.0]), (T, E))
+    s[:, E // 2] = 0.0                                # most of the sum; never chosen
+    bias = np.full(E, 1.0, np.float32)
+    bias[E // 2] = -3.0
+    return s, bias
+
+
+@pytest.mark.parametrize("E,k,there", [(20, 5, 8), (64, 3, 7), (64, 1, 5), (128, 6, 8), (96, 10, 16)])
+@pytest.mark.parametrize("T", [2000, 9000])
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_a_better_expert_behind_some_that_are_alike(E, k, there, T, sigmoid):
+    """The last slot and those next to it may be alike and one behind them be ahead of all in double."""
+    rng = np.random.default_rng(E + k)
+    s, bias = steps_below_fp32(rng, T, E, sigmoid)
+    order = np.argsort(rng.random((T, E)), axis=1)
+    np.put_along_axis(s, order[:, there:], -np.inf, 1)
+    check(s, bias, k=k, sigmoid=sigmoid)
+    # in every token alike but for the last one, so that no other pair of a token beside it has the order looked at
+    np.put_along_axis(s, order[:, :there], np.float32(30.5 if sigmoid else -19.5), 1)
+    np.put_along_axis(s, order[:, :there].max(axis=1, keepdims=True), np.float32(41.25 if sigmoid else -19.0), 1)
+    check(s, bias, k=k, sigmoid=sigmoid)
