@@ -443,7 +443,8 @@ __global__ __launch_bounds__(256, !BIASED || REGS < 32 ? REGS * K <= 256 ? 4 : 3
 #pragma unroll
         for (int r = 0; r < REGS; ++r) found += __popcll(__ballot(v[r] >= line));
         double extra = 0.0;   // the best of those that are no slot
-        if (found > __popcll(__ballot(full && value >= line))) {   // of some token of the wavefront: look which, and not at those that are like its last slot
+        bool alike = false;   // there are some like the last slot, which come right behind it
+        if (found > __popcll(__ballot(full && value >= line))) {   // of some token of the wavefront: look which
             const int le = __shfl(e, base + K - 1, 64);
             const float ls = __shfl(se, base + K - 1, 64), lb = __shfl(be, base + K - 1, 64);
             int others = 0;
@@ -452,10 +453,15 @@ __global__ __launch_bounds__(256, !BIASED || REGS < 32 ? REGS * K <= 256 ? 4 : 3
                 const int at = behind - (r / VEC * (LG * VEC) + r % VEC), other = kRtExperts - 1 - at;
                 if (!(v[r] >= line)) continue;
                 const double x = ranked(v[r], at);
-                if (!(x < list[K - 1]) || (le >= 0 && other > le && a.bias[other] == lb && score_of(other) == ls)) continue;
+                if (!(x < list[K - 1])) continue;
+                if (le >= 0 && other > le && a.bias[other] == lb && score_of(other) == ls) {
+                    alike = true;
+                    continue;
+                }
                 extra = larger(extra, x);
                 ++others;
             }
+            alike = over_lanes((int)alike, LANES, Most()) != 0;
             extra = over_lanes(extra, LANES, [](double x, double y) { return larger(x, y); });
             others = over_lanes(others, LANES, Plus());
             near = near || others > 0;
@@ -487,6 +493,7 @@ __global__ __launch_bounds__(256, !BIASED || REGS < 32 ? REGS * K <= 256 ? 4 : 3
                 place_extra += ahead_of(oc, oe, c_extra, e_extra);
                 unsure = unsure || (full && unclear(op, oc, p, c)) || (e_extra >= 0 && unclear(op, oc, p_extra, c_extra));
             }
+            unsure = unsure || (alike && sub == K - 1 && place + 1 < k);
             if (!full) place = sub;
             else if (e_extra >= 0) {
                 place += ahead_of(c_extra, e_extra, c, e);

@@ -107,3 +107,14 @@ def test_a_better_expert_behind_some_that_are_alike(E, k, there, T, sigmoid):
     np.put_along_axis(s, order[:, :there], np.float32(30.5 if sigmoid else -19.5), 1)
     np.put_along_axis(s, order[:, :there].max(axis=1, keepdims=True), np.float32(41.25 if sigmoid else -19.0), 1)
     check(s, bias, k=k, sigmoid=sigmoid)
+
+
+@pytest.mark.parametrize("E,k", [(20, 5), (61, 8), (64, 3), (128, 8), (96, 12)])
+@pytest.mark.parametrize("T", [2000, 9000])
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_experts_alike_that_only_double_tells_from_others(E, k, T, sigmoid):
+    """Of several experts with one score one may be the last that fp32 keeps, and be ahead of the rest in double: the others come with it."""
+    rng = np.random.default_rng(E + k)
+    s, bias = steps_below_fp32(rng, T, E, sigmoid)
+    s[rng.random((T, E)) < 1.0 - (k + 4.0) / E] = -np.inf   # about as many as the lists are long
+    check(s, bias, k=k, sigmoid=sigmoid)
