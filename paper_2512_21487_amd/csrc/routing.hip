@@ -469,29 +469,34 @@ __global__ __launch_bounds__(256, !BIASED || REGS < 32 ? REGS * K <= 256 ? 4 : 3
         }
         if (__ballot(near)) {
             // The slots' own values in double, of all tokens at once, and their order; the one in front of which all K are gives way to the other.
-            // A softmax's sum stays in fp32: it is the same for both, so that the difference of two p is off by less than 2^-18 of itself.
+            // A softmax's sum stays in fp32: it is the same for both, so that the difference of two p is off by less than 2^-18 of itself, and two c that are
+            // equal, or all but equal, may not have been rounded as they would with the sum in double.
             const auto p_of = [&](float score) { return a.sigmoid ? 1.0 / (1.0 + exp(-(double)score)) : exp((double)score - (double)top) / (double)total; };
             double p = 0.0, c = -__builtin_inf(), p_extra = 0.0, c_extra = -__builtin_inf();
             if (full) { p = p_of(se); c = p + (double)be; }
             int e_extra = -1, place_extra = 0;
-            float s_extra = none;
+            float s_extra = none, b_extra = 0.f;
             if (extra > 0.0) {
                 e_extra = ranked_expert(extra);
                 s_extra = score_of(e_extra);
                 p_extra = p_of(s_extra);
-                c_extra = p_extra + (double)a.bias[e_extra];
+                b_extra = a.bias[e_extra];
+                c_extra = p_extra + (double)b_extra;
             }
             const auto ahead_of = [](double x, int ex, double y, int ey) { return x > y || (x == y && ex < ey); };
-            const auto unclear = [&](double px, double x, double py, double y) { return !a.sigmoid && px != py && fabs(x - y) <= 0x1p-18 * fabs(px - py); };
+            const auto unclear = [&](double px, float bx, double x, double py, float by, double y) {
+                return !a.sigmoid && (px != py || bx != by) && fabs(x - y) <= 0x1p-18 * fabs(px - py) + 0x1p-50 * fmin(fmax(fabs(x), px), fmax(fabs(y), py));
+            };
             place = 0;
 #pragma unroll 1
             for (int i = 0; i < K; ++i) {
                 const int oe = __shfl(e, base + i, 64);
                 const double op = __shfl(p, base + i, 64), oc = __shfl(c, base + i, 64);
+                const float ob = __shfl(be, base + i, 64);
                 if (oe < 0) continue;
                 place += !full || ahead_of(oc, oe, c, e);   // empty slots stay behind
                 place_extra += ahead_of(oc, oe, c_extra, e_extra);
-                unsure = unsure || (full && unclear(op, oc, p, c)) || (e_extra >= 0 && unclear(op, oc, p_extra, c_extra));
+                unsure = unsure || (full && unclear(op, ob, oc, p, be, c)) || (e_extra >= 0 && unclear(op, ob, oc, p_extra, b_extra, c_extra));
             }
             unsure = unsure || (alike && sub == K - 1 && place + 1 < k);
             if (!full) place = sub;

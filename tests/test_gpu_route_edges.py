@@ -118,3 +118,17 @@ def test_experts_alike_that_only_double_tells_from_others(E, k, T, sigmoid):
     s, bias = steps_below_fp32(rng, T, E, sigmoid)
     s[rng.random((T, E)) < 1.0 - (k + 4.0) / E] = -np.inf   # about as many as the lists are long
     check(s, bias, k=k, sigmoid=sigmoid)
+
+
+@pytest.mark.parametrize("E,k", [(12, 4), (64, 6)])
+@pytest.mark.parametrize("T", [3000, 9000])
+def test_softmax_values_a_step_of_double_apart(E, k, T):
+    """Which of two values, equal or a step of double apart, is the larger one is also what double says, with a sum in double."""
+    rng = np.random.default_rng(E)
+    s = np.full((T, E), -40.0, np.float32)
+    s[:, :3] = 0.3 * rng.standard_normal((T, 3))      # most of the sum; never chosen
+    near = (np.float32(-23.5).view(np.int32) + rng.integers(0, 40, (T, 8))).astype(np.int32).view(np.float32)
+    s[:, 4:12] = near                                 # p of 2^-35 or so: a step of the score is half a step of 1 + p
+    bias = np.full(E, -5.0, np.float32)
+    bias[4:12] = 1.0
+    check(s, bias, k=k)
