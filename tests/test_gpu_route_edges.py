@@ -2,7 +2,7 @@
 import numpy as np
 import pytest
 
-from test_gpu_route import FMAX, check, normal, run
+from test_gpu_route import BF_LOWEST, FMAX, by_rule, check, normal, run
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -132,3 +132,32 @@ def test_softmax_values_a_step_of_double_apart(E, k, T):
     bias = np.full(E, -5.0, np.float32)
     bias[4:12] = 1.0
     check(s, bias, k=k)
+
+
+def test_choices_by_rules_and_values_of_all_kinds():
+    """Rules and shapes drawn at random, scores and biases from tiny to the ends of fp32, many of them equal, infinite or not there."""
+    rng = np.random.default_rng(77)
+    pick = lambda *a: a[rng.integers(len(a))]
+    for _ in range(150):
+        G = pick(1, 1, 1, 2, 3, 4, 8, 16, 32)
+        S = max(1, min(int(pick(1, 2, 3, 4, 8, 9, 16, 32, 61, 128)), 512 // G))
+        E, top_groups, T = G * S, int(rng.integers(1, G + 1)), int(pick(1, 7, 65, 200))
+        k = int(rng.integers(1, min(pick(8, 8, 16, 64), S * top_groups) + 1))
+        s = (rng.standard_normal((T, E)) * pick(1e-6, 0.05, 1, 1, 8, 50, 1e4, 1e37)).astype(np.float32)
+        if rng.random() < 0.3:
+            s = np.round(s * 4) / 4
+        if rng.random() < 0.4:
+            s[rng.random((T, E)) < pick(0.02, 0.5, 0.95)] = pick(-np.inf, np.nan, -FMAX)
+        if rng.random() < 0.2:
+            s[rng.random((T, E)) < 0.05] = np.inf
+        bias = None
+        if rng.random() < 0.75:
+            bias = np.clip(rng.standard_normal(E) * pick(0.0, 1e-7, 0.05, 0.05, 1, 64, 1000, 1e6, 1e30, 1e38), -3.4e38, 3.4e38).astype(np.float32)
+            if rng.random() < 0.3:
+                bias[rng.random(E) < pick(0.1, 0.7, 0.95)] = pick(-FMAX, FMAX, np.inf, -np.inf, np.nan, -3e38, 0.0)
+        how = dict(k=k, groups=G, top_groups=top_groups, top2=bool(rng.random() < 0.6), sigmoid=bool(rng.random() < 0.5), renorm=True)
+        bf16 = bool(rng.random() < 0.3)
+        read, idx, w = run(s, bias, bf16=bf16, **how)
+        want, _ = by_rule(read, bias, None, lowest=BF_LOWEST if bf16 else -FMAX, **how)
+        assert np.array_equal(idx, want), how
+        assert np.all(w >= 0.0) and np.all(w[idx < 0] == 0.0)
