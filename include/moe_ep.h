@@ -263,7 +263,8 @@ int moe_ep_route(const moe_ep_routing *rule, const void *scores, const float *bi
  * The gate of a context by a rule: later moe_ep_forward and moe_ep_forward_dep choose and weigh experts as moe_ep_route does, instead of by the
  * softmax over the top_k largest scores.  Their top_k must then be the rule's; the rule's n_experts and device are the context's, its top_k at most
  * max_top_k, its scores fp32 without gaps (gate_logits).  Slots without an expert (idx -1) take no part in the layer: a token whose scores are all
- * minus infinity gets the shared experts only, or zeros.  bias (fp32 [E], device memory, or NULL) is read by every forward and stays the caller's.
+ * minus infinity gets the shared experts only, or zeros.  bias (fp32 [E], device memory, or NULL) is read by every forward and stays the caller's;
+ * a captured forward keeps the rule and the bias it was captured with.
  * rule NULL: as without this call.  moe_ep_forward_noalloc has no context, and no rule.
  */
 int moe_ep_set_routing(moe_ep_ctx *ctx, const moe_ep_routing *rule, const float *bias);
@@ -301,7 +302,7 @@ int moe_ep_validate_linear(const moe_ep_linear_config *cfg, const char **why);
  *   out       out_type [n_rows, N]; must not overlap anything else (rows of the same distance may lie side by side).  What lies between its rows is left as it is.
  *   n_rows    0..2^30
  * Rows are contiguous and every pointer is aligned to its elements; no more is asked of sizes, strides and addresses.  Products are summed in fp32 (fp32
- * weights enter with their whole mantissa and must be finite; with them a row of x that is not finite may give NaN where the formula gives an infinity), bias, activation and residual are fp32 too, and a result is rounded once.  The same call gives the
+ * weights enter with their whole mantissa, but for what is below 2^-133, and must be finite; with them a row of x that is not finite may give NaN where the formula gives an infinity), bias, activation and residual are fp32 too, and a result is rounded once.  The same call gives the
  * same bits.  Streams, graphs, devices, checks, `why` and n_rows == 0 as for moe_ep_route.
  */
 int moe_ep_linear(const moe_ep_linear_config *cfg, const void *x, const void *weight, const float *bias,

@@ -600,7 +600,8 @@ class MoeEp:
 
     # -- moe_ep_set_routing -----------------------------------------------------------------
     def set_routing(self, rule: Optional[Routing] = None, bias=None) -> int:
-        """Later forwards route by ``rule`` (None: as a new context); the context keeps ``bias`` alive."""
+        """Later forwards route by ``rule`` (None: as a new context); the context keeps ``bias`` alive until the next call (a graph's forward reads the
+        one it was captured with: keep that as long as the graph)."""
         address = _vector(bias, "bias", self.cfg.n_experts, F32, self.cfg.device)
         rc = self._lib.moe_ep_set_routing(self._ctx, ctypes.byref(rule) if rule is not None else None, address)
         if rc != 0:

@@ -842,7 +842,11 @@ int cheapest_tiling(const LinearArgs& a, int n_cu)
 }
 
 // The largest of the split tiles that still gives enough compute units work: half of them, three quarters where every tile also takes fp32
-// weights apart.
+// weights apart.  64 x 32 / 64 x 16 / 32 x 16 / 16 x 16 tiles, us: 64 x 5120 x 1536 10 / 12 / 15 / 13; 33, 64 x 2048 x 1408 7.2 / 6.2 / 5.2 / 5.4,
+// 7.3 / 6.4 / 5.2 / 5.5; 64 x 1536 x 5120 22 / 18 / 13 / 14; 24 x 1536 x 5120 18 / 15 / 12 / 9; 17, 32 x 5120 x 1536 8.9 / 11 / 10 / 8.9, 9.2 / 11 / 11 / 9.7;
+// fp32 weights, 4096 x 128 x 4096 27 / 32 / 43 / 62, 1024 x 256 x 4096 23 / 16 / 23 / 33, 256 x 160 x 5120 25 / 17 / 12 / 10.  (Of 33 to 64 rows the
+// rule takes 64 x 16 where 32 x 16 is up to a fifth faster: half of the compute units is too few there.)  64 x 32 with four wavefronts instead of
+// eight, many tiles: 4096 x 256 x 2048 25 / 28, 8192 x 256 x 4096 87 / 94; 4096 x 128 x 4096, few, 31 / 27.
 int split_kernel(const LinearArgs& a, int n_cu)
 {
     const auto tiles = [&](int mb, int nb) { return (double)((a.R + mb * 16 - 1) / (mb * 16)) * ((a.N + nb * 16 - 1) / (nb * 16)); };

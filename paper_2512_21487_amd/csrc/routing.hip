@@ -6,9 +6,10 @@
 // Which expert is chosen is a whole number and may not hang on how a sum was rounded: choices are those of c in double precision.  Computing
 // them so for every token (route_exact_kernel, a wavefront per token, also the kernel of shapes that the other one does not have) took 150 us
 // for 65536 tokens of 256 experts.  route_kernel computes c in fp32 and looks whether two values that an order hangs on are closer than its
-// rounding; chosen slots that are close are compared in double by the lanes that hold them, and only a token whose last slot or last
-// group hangs on such a pair is done again in double as a whole (5 us where it is the last one of a launch).  The same 65536 tokens
-// take 19 us, 37 with a bias, of which reading the scores is 14: instruction issue bounds it.
+// rounding; chosen slots that are close are compared in double by the lanes that hold them.  A token is done again in double as a whole (5 us where it
+// is the last one of a launch) only where its last slot or last group hangs on such a pair, where experts like the last that the list holds may come
+// with it, or where two softmax values are a step of double apart.  The same 65536 tokens take 18 us, 36 with a bias, of which reading the scores is
+// 14: instruction issue bounds it.
 #include "gate.h"
 
 namespace moe_ep {
@@ -265,7 +266,7 @@ __device__ __forceinline__ void merge_lanes(double (&a)[N])
 }
 // A token is LANES lanes', each with REGS of its experts: of one group those of a group's lanes, VEC consecutive ones at a time.  The K
 // best of a lane are sorted in registers, and the lanes' lists merged pair by pair: no round waits for another.  (A selection in rounds,
-// a maximum over the lanes in each, waits for k of them.)  Instructions bound it where the tokens are many, 37 us of 65536 x 256 with a bias
+// a maximum over the lanes in each, waits for k of them.)  Instructions bound it where the tokens are many, 36 us of 65536 x 256 with a bias
 // where the bytes are 14, and latency where they are few: 3.8 us of 256 tokens.
 template <int LANES, int REGS, int K, int VEC, bool BIASED>
 __global__ __launch_bounds__(256, !BIASED || REGS < 32 ? REGS * K <= 256 ? 4 : 3 : 2) void route_kernel(RouteArgs a)
