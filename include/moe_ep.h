@@ -309,6 +309,57 @@ int moe_ep_linear(const moe_ep_linear_config *cfg, const void *x, const void *we
                   const void *residual, int32_t n_rows, void *out, void *stream, const char **why);
 
 /*
+ * Norms behind a block and in front of the next one, with the block's gate and the residual stream between them:
+ *   h = residual_scale * residual + block_scale * f(gate) * N_after(block);   sum = h;   out = N_before(h)
+ *   N(x) = (x - mean) / sqrt(mean((x - mean)^2) + eps) * (weight + weight_offset) + bias   per row; MOE_EP_NORM_RMS: mean = 0 (the
+ *          mean of x^2 stays); MOE_EP_NORM_NONE: x * (weight + weight_offset) + bias, a scale per feature
+ * Operands that are NULL take no part: no residual (0), no gate (1), no weight (1, whatever weight_offset), no bias (0).
+ */
+typedef enum { MOE_EP_NORM_NONE = 0, MOE_EP_NORM_RMS = 1, MOE_EP_NORM_LAYER = 2 } moe_ep_norm_kind;
+typedef enum { MOE_EP_GATE_AS_IS = 0, MOE_EP_GATE_SIGMOID = 1, MOE_EP_GATE_SILU = 2 } moe_ep_gate_form; /* f(g): g, 1 / (1 + exp(-g)), g / (1 + exp(-g)) */
+typedef struct {
+    int32_t features;        /* M; 1..32768                                                         */
+    int32_t norm_after;      /* moe_ep_norm_kind of the block's results                             */
+    int32_t norm_before;     /* moe_ep_norm_kind in front of the next block; NONE: there is no out  */
+    int32_t block_type;      /* moe_ep_type                                                         */
+    int32_t stream_type;     /* moe_ep_type of residual and sum                                     */
+    int32_t out_type;        /* moe_ep_type                                                         */
+    int32_t weight_type;     /* moe_ep_type of weights and biases                                   */
+    int32_t gate_type;       /* moe_ep_type                                                         */
+    int32_t gate_form;       /* moe_ep_gate_form                                                    */
+    int32_t gate_per_row;    /* 1: one gate a row; 0: one an element                                */
+    int32_t device;          /* HIP device ordinal                                                  */
+    float eps;               /* 1e-20..1 (ignored without a norm)                                   */
+    float block_scale;       /* finite                                                              */
+    float residual_scale;    /* finite                                                              */
+    float weight_offset;     /* finite; 1 for weights that are stored around 0                      */
+    int64_t block_stride;    /* elements between two rows; 0 = rows without a gap; up to 2^22       */
+    int64_t residual_stride;
+    int64_t gate_stride;     /* one gate a row: elements between two of them, 0 = 1                 */
+    int64_t sum_stride;
+    int64_t out_stride;
+} moe_ep_norm_config;
+
+/* Pure host check, usable without a GPU; returns and `why` as for moe_ep_validate_config. */
+int moe_ep_validate_norm(const moe_ep_norm_config *cfg, const char **why);
+
+/*
+ *   block      block_type [n_rows, M];   residual  stream_type [n_rows, M], or NULL
+ *   gate       gate_type [n_rows, M], or [n_rows] with gate_per_row, or NULL
+ *   after_weight, after_bias, before_weight, before_bias   weight_type [M], or NULL (the last two need a norm_before)
+ *   sum        stream_type [n_rows, M], or NULL where there is an out; may be the residual itself (with the same stride)
+ *   out        out_type [n_rows, M], exactly where norm_before is not MOE_EP_NORM_NONE; may be the block itself (same type and stride)
+ *   n_rows     0..2^30
+ * sum and out must not overlap anything else, nor each other (rows of the same distance may lie side by side).  Everything is computed in fp32 from h as it
+ * is, not as `sum` holds it, and each result is rounded once.  A row with a number that is not finite gives what the formula gives; squares and
+ * sums beyond fp32 do no harm.  Rows do not depend on each other; the same call gives the same bits.
+ * Alignment, what lies between rows, streams, graphs, devices, checks, `why` and n_rows == 0 as for moe_ep_linear.
+ */
+int moe_ep_norm(const moe_ep_norm_config *cfg, const void *block, const void *residual, const void *gate, const void *after_weight,
+                const void *after_bias, const void *before_weight, const void *before_bias, int32_t n_rows, void *sum, void *out,
+                void *stream, const char **why);
+
+/*
  * Test / inspection surface: host copies of what the last forward computed for chunk
  * `chunk` (synchronises the context's streams; after moe_ep_forward_dep chunk = i * r_2 + j for
  * chunk j of micro-batch i).  Any pointer may be NULL.  With Tn the tokens of this chunk:

@@ -87,6 +87,8 @@ BF16, F32 = 0, 1
 SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 GROUP_MAX, GROUP_TOP2 = 0, 1
 ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = 0, 1, 2, 3, 4
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+GATE_AS_IS, GATE_SIGMOID, GATE_SILU = 0, 1, 2
 
 
 class _Fields(ctypes.Structure):
@@ -117,6 +119,20 @@ class LinearConfig(_Fields):
     _fields_ = [(n, ctypes.c_int32) for n in (
         "in_features", "out_features", "weight_type", "out_type", "activation", "device")] + [
         (n, ctypes.c_int64) for n in ("x_stride", "weight_stride", "residual_stride", "out_stride")]
+
+
+class NormConfig(_Fields):
+    """Mirror of ``moe_ep_norm_config``; fields that are not named are 0, but for eps of 1e-6 and scales of 1."""
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "features", "norm_after", "norm_before", "block_type", "stream_type", "out_type", "weight_type", "gate_type", "gate_form", "gate_per_row",
+        "device")] + [(n, ctypes.c_float) for n in ("eps", "block_scale", "residual_scale", "weight_offset")] + [
+        (n, ctypes.c_int64) for n in ("block_stride", "residual_stride", "gate_stride", "sum_stride", "out_stride")]
+
+    def __init__(self, *args, **kw):
+        for at, (name, value) in enumerate((("eps", 1e-6), ("block_scale", 1.0), ("residual_scale", 1.0)), start=11):
+            if len(args) <= at:
+                kw.setdefault(name, value)
+        super().__init__(*args, **kw)
 
 
 def lib_path() -> str:
@@ -190,6 +206,10 @@ def load_library() -> ctypes.CDLL:
     lib.moe_ep_get_stage_ms.restype = ctypes.c_int
     lib.moe_ep_get_stage_ms.argtypes = [vp, vp, i32]
     dp = ctypes.POINTER(ctypes.c_double)
+    lib.moe_ep_validate_norm.restype = ctypes.c_int
+    lib.moe_ep_validate_norm.argtypes = [ctypes.POINTER(NormConfig), whyp]
+    lib.moe_ep_norm.restype = ctypes.c_int
+    lib.moe_ep_norm.argtypes = [ctypes.POINTER(NormConfig), vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, whyp]
     lib.moe_ep_fit_linear.restype = ctypes.c_int
     lib.moe_ep_fit_linear.argtypes = [dp, dp, i32, dp, dp, dp]
     lib.moe_ep_pipeline_makespan.restype = ctypes.c_double
@@ -424,6 +444,55 @@ def linear(cfg: LinearConfig, x, weight, bias=None, residual=None, out=None, n_r
         ctypes.byref(cfg), _rows(x, "x", n_rows, K, cfg.x_stride or K, BF16, at), _rows(weight, "weight", N, K, cfg.weight_stride or K, F32 if cfg.weight_type else BF16, at),
         _vector(bias, "bias", N, F32, at), _rows(residual, "residual", n_rows, N, cfg.residual_stride or N, result, at), n_rows,
         _rows(out, "out", n_rows, N, cfg.out_stride or N, result, at), stream, ctypes.byref(why))
+    if rc != 0:
+        raise MoeEpError(rc, (why.value or b"").decode())
+    return rc
+
+
+def validate_norm(cfg: NormConfig) -> Tuple[int, str]:
+    why = ctypes.c_char_p()
+    rc = load_library().moe_ep_validate_norm(ctypes.byref(cfg), ctypes.byref(why))
+    return rc, (why.value or b"").decode()
+
+
+def _column(x, name: str, n_rows: int, stride: int, kind: int, device: int) -> Optional[int]:
+    """Address of one element a row, ``stride`` apart: a vector, or the first column of a matrix."""
+    if x is None:
+        return None
+    try:
+        have, apart = x.shape, x.stride()
+    except (AttributeError, TypeError):
+        return _ptr(x)
+    _check_type(x, name, kind)
+    _check_place(x, name, device)
+    if len(have) not in (1, 2) or have[0] < n_rows or have[-1] < 1:
+        raise ValueError(f"{name} must be at least {n_rows} elements, one a row, got {tuple(have)}")
+    if n_rows > 1 and apart[0] != stride:
+        raise ValueError(f"{name} has strides {apart}, the call reads elements {stride} apart")
+    return x.data_ptr()
+
+
+def norm(cfg: NormConfig, block, residual=None, gate=None, after_weight=None, after_bias=None, before_weight=None, before_bias=None, sum=None, out=None,
+         n_rows: Optional[int] = None, stream: Optional[int] = None) -> int:
+    """moe_ep_norm: sum = residual_scale residual + block_scale f(gate) N_after(block), out = N_before(sum as it is before it is rounded)."""
+    if n_rows is None:
+        n_rows = int(block.shape[0])
+    if not 0 <= n_rows <= _MOST_ROWS:
+        raise MoeEpError(-1, "n_rows must be in 0..2^30")
+    if stream is None:
+        stream = _current_stream(cfg.device)
+    M, at = cfg.features, cfg.device
+    flow, weights = F32 if cfg.stream_type else BF16, F32 if cfg.weight_type else BF16
+    gates = F32 if cfg.gate_type else BF16
+    if gate is not None:
+        gate = _column(gate, "gate", n_rows, cfg.gate_stride or 1, gates, at) if cfg.gate_per_row else _rows(gate, "gate", n_rows, M, cfg.gate_stride or M, gates, at)
+    why = ctypes.c_char_p()
+    rc = (_lib or load_library()).moe_ep_norm(
+        ctypes.byref(cfg), _rows(block, "block", n_rows, M, cfg.block_stride or M, F32 if cfg.block_type else BF16, at),
+        _rows(residual, "residual", n_rows, M, cfg.residual_stride or M, flow, at), gate, _vector(after_weight, "after_weight", M, weights, at),
+        _vector(after_bias, "after_bias", M, weights, at), _vector(before_weight, "before_weight", M, weights, at),
+        _vector(before_bias, "before_bias", M, weights, at), n_rows, _rows(sum, "sum", n_rows, M, cfg.sum_stride or M, flow, at),
+        _rows(out, "out", n_rows, M, cfg.out_stride or M, F32 if cfg.out_type else BF16, at), stream, ctypes.byref(why))
     if rc != 0:
         raise MoeEpError(rc, (why.value or b"").decode())
     return rc

@@ -245,6 +245,24 @@ enum {
 int linear_kernel(const LinearArgs& a, int n_cu);
 hipError_t launch_linear(const LinearArgs& a, int n_cu, hipStream_t s);
 
+// ---- norms around a block (norm.hip): the public struct's fields as the kernels read them
+enum { kNormNone = 0, kNormRms, kNormLayer, kNormCount };
+enum { kGateAsIs = 0, kGateSigmoid, kGateSilu, kGateCount };
+struct NormArgs {
+    const void *block, *residual, *gate;                                      // the last two may be NULL
+    const void *after_weight, *after_bias, *before_weight, *before_bias;      // each may be NULL
+    void *sum, *out;                                                          // one of them may be NULL
+    long long ldb, ldr, ldg, lds, ldo;
+    int R, M, after, before, gate_form;
+    bool block32, stream32, out32, weight32, gate32, gate_per_row;
+    float eps, block_scale, residual_scale, offset;
+};
+// What launch_norm launches (tests name it): wavefronts of a row x turns of 8 elements a lane
+enum { kNorm1x1 = 0, kNorm2x1, kNorm4x1, kNorm8x1, kNorm16x1, kNorm8x2, kNorm16x2, kNorm16x4 };
+constexpr int kNormMost = 16 * 64 * 8 * 4;   // elements of the longest row
+int norm_kernel_of(int R, int M, int n_cu);
+hipError_t launch_norm(const NormArgs& a, int n_cu, hipStream_t s);
+
 // What the kernels are about to read or write through a caller's pointer (moe_ep.hip): NULL where it is usable, else what is wrong.
 // device: the one that device memory has to be on, or -1
 const char* check_span(const void* p, size_t bytes, bool want_host, const void** dev_ptr, int device = -1);

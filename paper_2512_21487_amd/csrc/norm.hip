@@ -1,0 +1,303 @@
+// Norms behind and in front of a block, with the block's gate and the residual stream between them:
+//   h = residual_scale residual + block_scale f(gate) N_after(block);   sum = h,  out = N_before(h)
+// All of it is fp32 in registers, a row at a time: each operand is read once, each result rounded once and written once.
+#include "rows.h"
+
+namespace moe_ep {
+
+namespace {
+
+// 8 consecutive elements as they come from memory; WIDE: of either type, bf16 ones take the first half, else bf16
+template <bool WIDE> struct Raw8 { u32x4_t v[WIDE ? 2 : 1]; };
+
+// the `left` first of 8 elements, and zeros; cols: elements of the row
+template <bool WIDE>
+__device__ __forceinline__ Raw8<WIDE> load_raw(const char* row, int col, bool wide, int left, int cols)
+{
+    Raw8<WIDE> r;
+    if constexpr (WIDE) {
+        if (wide) {
+            const float* const p = reinterpret_cast<const float*>(row) + col;
+            r.v[0] = load_part<4>(p, left, cols);
+            r.v[1] = load_part<4>(p + 4, left - 4, cols);
+            return r;
+        }
+        r.v[1] = u32x4_t{0, 0, 0, 0};
+    }
+    r.v[0] = load_part<8>(reinterpret_cast<const uint16_t*>(row) + col, left, cols);
+    return r;
+}
+
+template <bool WIDE>
+__device__ __forceinline__ void to_float(const Raw8<WIDE>& r, bool wide, float (&f)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float narrow = (i & 1) ? bf16_hi(r.v[0][i >> 1]) : bf16_lo(r.v[0][i >> 1]);
+        if constexpr (WIDE) f[i] = wide ? __uint_as_float(r.v[i >> 2][i & 3]) : narrow;
+        else f[i] = narrow;
+    }
+}
+
+__device__ __forceinline__ void store8(char* row, int col, bool wide, int left, const float (&f)[8])
+{
+    if (left >= 8) {
+        if (wide) {
+            f32x4_any4* const p = reinterpret_cast<f32x4_any4*>(reinterpret_cast<float*>(row) + col);
+            p[0] = f32x4_t{f[0], f[1], f[2], f[3]};
+            p[1] = f32x4_t{f[4], f[5], f[6], f[7]};
+        } else
+            *reinterpret_cast<u32x4_any2*>(reinterpret_cast<uint16_t*>(row) + col) =
+                u32x4_t{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 7; ++i) {
+        if (i >= left) continue;
+        if (wide) reinterpret_cast<float*>(row)[col + i] = f[i];
+        else reinterpret_cast<uint16_t*>(row)[col + i] = (uint16_t)pack_bf16x2(f[i], 0.f);
+    }
+}
+
+struct Add { __device__ float operator()(float a, float b) const { return a + b; } };
+struct Larger { __device__ float operator()(float a, float b) const { return fmaxf(a, b); } };   // of two numbers where one is NaN, the other
+
+// over the WAVES wavefronts of a row, the same bits in every lane
+template <int WAVES, class Op>
+__device__ __forceinline__ float over_row(float v, float* lds, int& turn, Op op)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) v = op(v, __shfl_xor(v, d, 64));
+    if constexpr (WAVES > 1) {
+        // two places in turn: who is at the next reduction has left this one's barrier, which everybody reaches behind reading the last one's
+        float* const at = lds + (turn & 1) * WAVES;
+        ++turn;
+        if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = at[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) v = op(v, at[w]);
+    }
+    return v;
+}
+
+// x <- (x - mean) / sqrt(mean((x - mean)^2) + eps); RMS: without the mean.  The mean is taken out before the squares are summed, so that nothing cancels.
+// Where squares or sums leave fp32 while the row's numbers do not, its largest is between 2^56 (its square times 32768 is 2^127) and 2^128: times 2^-72 neither
+// they nor anything that counts beside them is lost, and eps, which does not count there, goes with it.  Such a row costs two or three reductions more.
+template <int WAVES, int V>
+__device__ __forceinline__ void normalise(float (&x)[V][8], const int (&left)[V], int cols, int kind, float eps, float* lds, int& turn)
+{
+    const float each = 1.0f / (float)cols;
+    for (int scaled = 0;; ++scaled) {
+        float mean = 0.f;
+        if (kind == kNormLayer) {
+            float s = 0.f;
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s += x[v][i];
+            mean = over_row<WAVES>(s, lds, turn, Add()) * each;
+        }
+        float q = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float d = i < left[v] ? x[v][i] - mean : 0.f;
+                q = fmaf(d, d, q);
+            }
+        const float power = over_row<WAVES>(q, lds, turn, Add()) * each;
+        if (scaled == 0 && !(power <= __FLT_MAX__)) {
+            float top = 0.f;
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[v][i]));
+            top = over_row<WAVES>(top, lds, turn, Larger());
+            // a number that is none, or infinite: as the formula has it
+            if (top <= __FLT_MAX__) {
+                constexpr float s = 0x1p-72f;
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[v][i] *= s;
+                eps = eps * s * s;
+                continue;
+            }
+        }
+        const float r = __builtin_amdgcn_rsqf(power + eps);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[v][i] = (x[v][i] - mean) * r;
+        return;
+    }
+}
+
+// A weight and a bias of 8 features
+struct Weights { Raw8<true> weight, bias; };
+__device__ __forceinline__ Weights load_weights(const NormArgs& a, const void* weight, const void* bias, int col, int left)
+{
+    Weights w;
+    if (weight) w.weight = load_raw<true>(static_cast<const char*>(weight), col, a.weight32, left, a.M);
+    if (bias) w.bias = load_raw<true>(static_cast<const char*>(bias), col, a.weight32, left, a.M);
+    return w;
+}
+// x <- x (weight + offset) + bias
+__device__ __forceinline__ void weigh(float (&x)[8], const NormArgs& a, const Weights& w, const void* weight, const void* bias)
+{
+    float f[8];
+    if (weight) {
+        to_float(w.weight, a.weight32, f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= f[i] + a.offset;
+    }
+    if (bias) {
+        to_float(w.bias, a.weight32, f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] += f[i];
+    }
+}
+
+__device__ __forceinline__ float gate_of(float g, int form)
+{
+    if (form == kGateAsIs) return g;
+    const float s = __builtin_amdgcn_rcpf(1.0f + exp_f(-g));
+    return form == kGateSigmoid ? s : g * s;
+}
+
+// WAVES wavefronts have a row, a lane 8 elements of it in each of V turns.  WIDE: the block, the stream or the gate is fp32.  EARLY: weights and biases are asked for
+// with the row, not behind the sums in front of them.
+// Of many rows memory bounds it: 16384 x 5120, bf16, residual and norm in front, 123 us for 671 MB, 5.5 TB/s (a copy of 1 GiB: 5.1); of few the chain of load, sum
+// over wavefronts, square root, store: 1 x 5120 3.8 us, 5.0 with norms on both sides and nothing in L2.
+template <int WAVES, int V, bool WIDE, bool EARLY>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(NormArgs a)
+{
+    constexpr int ROWS = WAVES == 1 ? 4 : 1;
+    __shared__ float lds[2 * WAVES];
+    int turn = 0;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+    const long long m = workgroup() * ROWS + (WAVES == 1 ? wave : 0);
+    if (m >= a.R) return;                                  // all of a row's wavefronts
+    int col[V], left[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        col[v] = (v * WAVES * 64 + lane) * 8;
+        left[v] = a.M - col[v];
+        if (left[v] <= 0) { left[v] = 0; col[v] = 0; }
+    }
+    const char* const block = static_cast<const char*>(a.block) + (size_t)m * a.ldb * (a.block32 ? 4 : 2);
+    const char* const residual = static_cast<const char*>(a.residual) + (size_t)m * a.ldr * (a.stream32 ? 4 : 2);
+    const char* const gate = static_cast<const char*>(a.gate) + (size_t)m * a.ldg * (a.gate32 ? 4 : 2);
+
+    Raw8<WIDE> b[V], r[V], g[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) b[v] = load_raw<WIDE>(block, col[v], a.block32, left[v], a.M);
+    if (a.residual)
+#pragma unroll
+        for (int v = 0; v < V; ++v) r[v] = load_raw<WIDE>(residual, col[v], a.stream32, left[v], a.M);
+    const bool of_elements = a.gate && !a.gate_per_row;
+    if (of_elements)
+#pragma unroll
+        for (int v = 0; v < V; ++v) g[v] = load_raw<WIDE>(gate, col[v], a.gate32, left[v], a.M);
+    Weights after[V], before[V];
+    if constexpr (EARLY)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            after[v] = load_weights(a, a.after_weight, a.after_bias, col[v], left[v]);
+            before[v] = load_weights(a, a.before_weight, a.before_bias, col[v], left[v]);
+        }
+    float one = a.block_scale;
+    if (a.gate && a.gate_per_row) one *= gate_of(a.gate32 ? *reinterpret_cast<const float*>(gate) : bf16_lo(*reinterpret_cast<const uint16_t*>(gate)), a.gate_form);
+
+    float x[V][8];
+#pragma unroll
+    for (int v = 0; v < V; ++v) to_float(b[v], a.block32, x[v]);
+    if (a.after != kNormNone) normalise<WAVES, V>(x, left, a.M, a.after, a.eps, lds, turn);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        if constexpr (!EARLY) after[v] = load_weights(a, a.after_weight, a.after_bias, col[v], left[v]);
+        weigh(x[v], a, after[v], a.after_weight, a.after_bias);
+    }
+    if (of_elements)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            float f[8];
+            to_float(g[v], a.gate32, f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[v][i] *= gate_of(f[i], a.gate_form);
+        }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        float f[8];
+        if (a.residual) to_float(r[v], a.stream32, f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[v][i] = a.residual ? fmaf(a.residual_scale, f[i], one * x[v][i]) : one * x[v][i];
+    }
+    if (a.sum) {
+        char* const sum = static_cast<char*>(a.sum) + (size_t)m * a.lds * (a.stream32 ? 4 : 2);
+#pragma unroll
+        for (int v = 0; v < V; ++v) store8(sum, col[v], a.stream32, left[v], x[v]);
+    }
+    if (!a.out) return;
+    // what is not there counts as zero
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[v][i] = i < left[v] ? x[v][i] : 0.f;
+    normalise<WAVES, V>(x, left, a.M, a.before, a.eps, lds, turn);
+    char* const out = static_cast<char*>(a.out) + (size_t)m * a.ldo * (a.out32 ? 4 : 2);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        if constexpr (!EARLY) before[v] = load_weights(a, a.before_weight, a.before_bias, col[v], left[v]);
+        weigh(x[v], a, before[v], a.before_weight, a.before_bias);
+        store8(out, col[v], a.out32, left[v], x[v]);
+    }
+}
+
+template <int WAVES, int V, bool EARLY>
+hipError_t launch_as(const NormArgs& a, hipStream_t s)
+{
+    const long long groups = WAVES == 1 ? ((long long)a.R + 3) / 4 : a.R;
+    const dim3 threads(WAVES == 1 ? 256 : WAVES * 64);
+    if (a.block32 || a.stream32 || (a.gate32 && !a.gate_per_row)) hipLaunchKernelGGL((norm_kernel<WAVES, V, true, EARLY>), grid_of(groups), threads, 0, s, a);
+    else hipLaunchKernelGGL((norm_kernel<WAVES, V, false, EARLY>), grid_of(groups), threads, 0, s, a);
+    return hipGetLastError();
+}
+
+template <int WAVES, int V>
+hipError_t launch_when(bool early, const NormArgs& a, hipStream_t s) { return early ? launch_as<WAVES, V, true>(a, s) : launch_as<WAVES, V, false>(a, s); }
+
+}  // namespace
+
+// The least that holds a row, in one turn up to 4096 elements.  Residual and norm of bf16 rows, turns x wavefronts, us: 1 / 1024 / 16384 x 2048 1 x 4 3.0 / 6.1 /
+// 47, 2 x 2 3.6 / 6.5 / 48, 4 x 1 5.0 / 8.2 / 53; x 4096 1 x 8 3.3 / 9.9 / 96, 2 x 4 3.7 / 9.8 / 94, 4 x 2 5.2 / 12 / 99.  Beyond 4096 the turns are two where compute units have
+// several rows: 1 x 16 / 2 x 8, of norms on both sides, operands not in L2, 1, 33, 256, 512 x 5120 5.0 / 5.3, 5.7 / 6.2, 7.0 / 7.5, 12 / 10, 256 x 8192 8.4 / 8.5; of one norm, 1024, 16384
+// x 5120 17 / 14, 183 / 123.
+int norm_kernel_of(int R, int M, int n_cu)
+{
+    if (M > 4096 && M <= 8192) return R <= n_cu ? kNorm16x1 : kNorm8x2;
+    return M <= 512 ? kNorm1x1 : M <= 1024 ? kNorm2x1 : M <= 2048 ? kNorm4x1 : M <= 4096 ? kNorm8x1 : M <= 16384 ? kNorm16x2 : kNorm16x4;
+}
+
+hipError_t launch_norm(const NormArgs& a, int n_cu, hipStream_t s)
+{
+    if (a.R <= 0) return hipSuccess;
+    if (a.M < 1 || a.M > kNormMost) return hipErrorInvalidValue;
+    // With a row for every compute unit, or fewer, nothing but the row's own loads hides those of the weights.  Weights asked for behind the sums / with the row, norms on
+    // both sides, operands not in L2, us: 1, 33, 256, 512 x 2048 4.1 / 3.6, 4.9 / 4.2, 5.6 / 4.8, 6.1 / 5.7; x 4096 4.5 / 4.0, 5.6 / 4.7, 6.5 / 5.8, 8.0 / 8.3; with more
+    // rows their registers cost wavefronts: 16384 x 2048 47 / 51, x 4096 96 / 101 (one norm).
+    const bool early = a.R <= n_cu;
+    switch (norm_kernel_of(a.R, a.M, n_cu)) {
+    case kNorm1x1: return launch_when<1, 1>(early, a, s);
+    case kNorm2x1: return launch_when<2, 1>(early, a, s);
+    case kNorm4x1: return launch_when<4, 1>(early, a, s);
+    case kNorm8x1: return launch_when<8, 1>(early, a, s);
+    case kNorm16x1: return launch_as<16, 1, true>(a, s);
+    case kNorm8x2: return launch_as<8, 2, false>(a, s);
+    case kNorm16x2: return launch_as<16, 2, false>(a, s);
+    default: return launch_as<16, 4, false>(a, s);
+    }
+}
+
+}  // namespace moe_ep

@@ -192,4 +192,95 @@ int moe_ep_linear(const moe_ep_linear_config* c, const void* x, const void* weig
     return e == hipSuccess ? MOE_EP_OK : hip_failed(why, "launch", e);
 }
 
+int moe_ep_validate_norm(const moe_ep_norm_config* c, const char** why)
+{
+    set_why(why, "ok");
+    if (!c) return refuse(why, "cfg is NULL");
+    if (c->features < 1 || c->features > kNormMost) return refuse(why, "features must be in 1..32768");
+    if (c->norm_after < 0 || c->norm_after >= kNormCount) return refuse(why, "unknown norm_after");
+    if (c->norm_before < 0 || c->norm_before >= kNormCount) return refuse(why, "unknown norm_before");
+    const auto type = [](int t) { return t == MOE_EP_BF16 || t == MOE_EP_F32; };
+    if (!type(c->block_type)) return refuse(why, "block_type must be MOE_EP_BF16 or MOE_EP_F32");
+    if (!type(c->stream_type)) return refuse(why, "stream_type must be MOE_EP_BF16 or MOE_EP_F32");
+    if (!type(c->out_type)) return refuse(why, "out_type must be MOE_EP_BF16 or MOE_EP_F32");
+    if (!type(c->weight_type)) return refuse(why, "weight_type must be MOE_EP_BF16 or MOE_EP_F32");
+    if (!type(c->gate_type)) return refuse(why, "gate_type must be MOE_EP_BF16 or MOE_EP_F32");
+    if (c->gate_form < 0 || c->gate_form >= kGateCount) return refuse(why, "unknown gate_form");
+    if (c->gate_per_row != 0 && c->gate_per_row != 1) return refuse(why, "gate_per_row must be 0 or 1");
+    const bool norms = c->norm_after != MOE_EP_NORM_NONE || c->norm_before != MOE_EP_NORM_NONE;
+    if (norms && !(c->eps >= 1e-20f && c->eps <= 1.0f)) return refuse(why, "eps must be in 1e-20..1");
+    const auto finite = [](float f) { return f >= -FLT_MAX && f <= FLT_MAX; };
+    if (!finite(c->block_scale)) return refuse(why, "block_scale must be finite");
+    if (!finite(c->residual_scale)) return refuse(why, "residual_scale must be finite");
+    if (!finite(c->weight_offset)) return refuse(why, "weight_offset must be finite");
+    const auto fits = [](long long stride, long long cols) { return stride == 0 || (stride >= cols && stride <= kMostStride); };
+    if (!fits(c->block_stride, c->features)) return refuse(why, "block_stride must be 0 or in features..2^22");
+    if (!fits(c->residual_stride, c->features)) return refuse(why, "residual_stride must be 0 or in features..2^22");
+    if (!fits(c->gate_stride, c->gate_per_row ? 1 : c->features)) return refuse(why, "gate_stride must be 0 or in features (of one gate a row: 1)..2^22");
+    if (!fits(c->sum_stride, c->features)) return refuse(why, "sum_stride must be 0 or in features..2^22");
+    if (!fits(c->out_stride, c->features)) return refuse(why, "out_stride must be 0 or in features..2^22");
+    if (c->device < 0) return refuse(why, "device must be >= 0");
+    return MOE_EP_OK;
+}
+
+int moe_ep_norm(const moe_ep_norm_config* c, const void* block, const void* residual, const void* gate, const void* after_weight, const void* after_bias,
+                const void* before_weight, const void* before_bias, int32_t n_rows, void* sum, void* out, void* stream, const char** why)
+{
+    if (moe_ep_validate_norm(c, why) != MOE_EP_OK) return MOE_EP_EINVAL;
+    if (n_rows < 0 || n_rows > kMostRows) return refuse(why, "n_rows must be in 0..2^30");
+    if (n_rows == 0) return MOE_EP_OK;
+    const bool before = c->norm_before != MOE_EP_NORM_NONE;
+    if (!block) return refuse(why, "block must not be NULL");
+    if (before != (out != nullptr)) return refuse(why, "out must be given exactly where there is a norm_before");
+    if (!before && (before_weight || before_bias)) return refuse(why, "before_weight and before_bias need a norm_before");
+    if (!sum && !out) return refuse(why, "sum and out must not both be NULL");
+    const int M = c->features;
+    const auto size = [](int type) { return type == MOE_EP_F32 ? 4 : 2; };
+    const int bs = size(c->block_type), ss = size(c->stream_type), os = size(c->out_type), ws = size(c->weight_type), gs = size(c->gate_type);
+    const auto apart = [](long long stride, int cols) { return stride ? stride : (long long)cols; };
+    const int gate_cols = c->gate_per_row ? 1 : M;
+    const long long ldb = apart(c->block_stride, M), ldr = apart(c->residual_stride, M), ldg = apart(c->gate_stride, gate_cols);
+    const long long lds = apart(c->sum_stride, M), ldo = apart(c->out_stride, M);
+    if (off_alignment(block, bs) || off_alignment(residual, ss) || off_alignment(gate, gs) || off_alignment(sum, ss) || off_alignment(out, os) ||
+        off_alignment(after_weight, ws) || off_alignment(after_bias, ws) || off_alignment(before_weight, ws) || off_alignment(before_bias, ws))
+        return refuse(why, "every pointer must be aligned to its elements");
+    // a lane reads its elements of a row before it writes in their place, and no other lane does either
+    const bool stream_in_place = residual == sum && ldr == lds, block_in_place = block == out && ldb == ldo && bs == os;
+    const size_t rows = (size_t)n_rows, vector = (size_t)M * ws;
+    const Span sp[] = {{block, rows, (size_t)ldb * bs, (size_t)M * bs, "block", false},
+                       {residual, rows, (size_t)ldr * ss, (size_t)M * ss, "residual", false},
+                       {gate, rows, (size_t)ldg * gs, (size_t)gate_cols * gs, "gate", false},
+                       {after_weight, 1, 0, vector, "after_weight", false},
+                       {after_bias, 1, 0, vector, "after_bias", false},
+                       {before_weight, 1, 0, vector, "before_weight", false},
+                       {before_bias, 1, 0, vector, "before_bias", false},
+                       {sum, rows, (size_t)lds * ss, (size_t)M * ss, "sum", true},
+                       {out, rows, (size_t)ldo * os, (size_t)M * os, "out", true}};
+    constexpr int kSpans = sizeof sp / sizeof *sp, kSum = kSpans - 2, kOut = kSpans - 1;
+    Span others[kSpans];
+    for (int i = 0; i < kSpans; ++i) others[i] = sp[i];
+    if (stream_in_place) others[1].p = nullptr;
+    others[kOut].written = false;
+    if (const char* bad = overlap(others, kSpans)) return refuse(why, bad);        // of sum with everything, out among it
+    others[1].p = residual;
+    others[kOut].written = true;
+    others[kSum].written = false;
+    if (block_in_place) others[0].p = nullptr;
+    if (const char* bad = overlap(others, kSpans)) return refuse(why, bad);        // and of out
+    DeviceScope device(c->device);
+    if (device.error != hipSuccess) return hip_failed(why, "selecting the device", device.error);
+    if (const char* bad = out_of_reach(sp, kSpans, c->device)) return refuse(why, bad);
+    NormArgs a{};
+    a.block = block; a.residual = residual; a.gate = gate; a.sum = sum; a.out = out;
+    a.after_weight = after_weight; a.after_bias = after_bias; a.before_weight = before_weight; a.before_bias = before_bias;
+    a.ldb = ldb; a.ldr = ldr; a.ldg = ldg; a.lds = lds; a.ldo = ldo;
+    a.R = n_rows; a.M = M; a.after = c->norm_after; a.before = c->norm_before; a.gate_form = c->gate_form;
+    a.block32 = bs == 4; a.stream32 = ss == 4; a.out32 = os == 4; a.weight32 = ws == 4; a.gate32 = gs == 4; a.gate_per_row = c->gate_per_row != 0;
+    a.eps = c->eps; a.block_scale = c->block_scale; a.residual_scale = c->residual_scale; a.offset = c->weight_offset;
+    int n_cu = 0;
+    hipError_t e = hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, c->device);
+    if (e == hipSuccess) e = launch_norm(a, n_cu, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? MOE_EP_OK : hip_failed(why, "launch", e);
+}
+
 }  // extern "C"
