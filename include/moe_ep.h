@@ -309,6 +309,40 @@ int moe_ep_linear(const moe_ep_linear_config *cfg, const void *x, const void *we
                   const void *residual, int32_t n_rows, void *out, void *stream, const char **why);
 
 /*
+ * The same product with low-rank adapters of many requests at once, each row with its own or none:
+ *   out = act(x W^T + bias + scale_a (x A_a^T) B_a^T) + residual,   a = index[row]
+ */
+typedef struct {
+    int32_t n_adapters; /* 1..2^20                                                                          */
+    int32_t rank;       /* 8..128, a multiple of 8; an adapter of lower rank has zeros in its last rows of A
+                           and columns of B                                                                 */
+} moe_ep_adapter_config;
+
+/* Pure host check of both, usable without a GPU; returns and `why` as for moe_ep_validate_config.  cfg as for moe_ep_linear, with weights in bf16. */
+int moe_ep_validate_linear_adapters(const moe_ep_linear_config *cfg, const moe_ep_adapter_config *adapters, const char **why);
+
+/* Bytes of workspace that a call of up to n_rows rows needs (0 if something is invalid, or without rows); never fewer for more rows. */
+size_t moe_ep_linear_adapters_workspace_bytes(const moe_ep_linear_config *cfg, const moe_ep_adapter_config *adapters, int32_t n_rows);
+
+/*
+ *   x, weight, bias, residual, out, n_rows   as for moe_ep_linear; weight_type MOE_EP_BF16
+ *   index      int32 [n_rows], device memory: a row's adapter; any number outside 0..n_adapters - 1: no adapter.  Rows in any order; rows of one adapter that
+ *              lie together (a prompt's, say) cost least: of up to 256 rows that share a tile, every adapter adds 64 elements or more to K
+ *   down, up   bf16 [n_adapters, rank, K] and [n_adapters, N, rank], A and B, without gaps; `up` on 16 bytes.  Of the adapters that `index` names they must
+ *              be finite: one that is not may give NaN in rows of others too
+ *   scale      fp32 [n_adapters], or NULL (1)
+ *   workspace  workspace_bytes bytes of device memory on 16 bytes, the call's own until `stream` has passed it: nothing in it has to be set, nothing is kept in it, and
+ *              two calls that may overlap (on two streams, or in two graphs) need one each
+ * x A^T is summed in fp32 and keeps 16 bits of mantissa on its way to B, 24 where out is fp32; the rest as for moe_ep_linear.  out and
+ * workspace must not overlap anything else, but out the residual in place.  The call enqueues two kernels.  A row without an adapter has the product's formula; its bits may differ from
+ * moe_ep_linear's, which may choose another kernel.
+ */
+int moe_ep_linear_adapters(const moe_ep_linear_config *cfg, const moe_ep_adapter_config *adapters, const void *x, const void *weight,
+                           const float *bias, const void *residual, const int32_t *index, const void *down, const void *up,
+                           const float *scale, int32_t n_rows, void *out, void *workspace, size_t workspace_bytes, void *stream,
+                           const char **why);
+
+/*
  * Norms behind a block and in front of the next one, with the block's gate and the residual stream between them:
  *   h = residual_scale * residual + block_scale * f(gate) * N_after(block);   sum = h;   out = N_before(h)
  *   N(x) = (x - mean) / sqrt(mean((x - mean)^2) + eps) * (weight + weight_offset) + bias   per row; MOE_EP_NORM_RMS: mean = 0 (the

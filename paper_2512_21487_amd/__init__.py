@@ -12,7 +12,7 @@ from .binding import (DEP_AASS, DEP_ASAS, DepConfig, DepModels, DepPrimitives, D
                       NOALLOC_SCRATCH_BYTES, BF16, F32, SCORE_SOFTMAX, SCORE_SIGMOID, GROUP_MAX, GROUP_TOP2, Routing,
                       validate_routing, route, ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH, LinearConfig,
                       validate_linear, linear, NORM_NONE, NORM_RMS, NORM_LAYER, GATE_AS_IS, GATE_SIGMOID, GATE_SILU, NormConfig,
-                      validate_norm, norm)
+                      validate_norm, norm, AdapterConfig, validate_linear_adapters, linear_adapters_workspace_bytes, linear_adapters)
 
 __all__ = ["MoeEp", "MoeEpConfig", "MoeEpError", "load_library", "load_probe_library", "lib_path", "validate_config",
            "validate_forward", "workspace_bytes", "prepared_weight_bytes", "ORDER_SHARED_FIRST", "ORDER_INTERLEAVED",
@@ -22,4 +22,5 @@ __all__ = ["MoeEp", "MoeEpConfig", "MoeEpError", "load_library", "load_probe_lib
            "dep_search", "routed_tile_rows", "probe_device", "forward_noalloc", "NOALLOC_SCRATCH_BYTES",
            "BF16", "F32", "SCORE_SOFTMAX", "SCORE_SIGMOID", "GROUP_MAX", "GROUP_TOP2", "Routing", "validate_routing", "route",
            "ACT_NONE", "ACT_RELU", "ACT_SILU", "ACT_GELU", "ACT_GELU_TANH", "LinearConfig", "validate_linear", "linear",
-           "NORM_NONE", "NORM_RMS", "NORM_LAYER", "GATE_AS_IS", "GATE_SIGMOID", "GATE_SILU", "NormConfig", "validate_norm", "norm"]
+           "NORM_NONE", "NORM_RMS", "NORM_LAYER", "GATE_AS_IS", "GATE_SIGMOID", "GATE_SILU", "NormConfig", "validate_norm", "norm",
+           "AdapterConfig", "validate_linear_adapters", "linear_adapters_workspace_bytes", "linear_adapters"]

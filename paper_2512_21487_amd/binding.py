@@ -121,6 +121,11 @@ class LinearConfig(_Fields):
         (n, ctypes.c_int64) for n in ("x_stride", "weight_stride", "residual_stride", "out_stride")]
 
 
+class AdapterConfig(_Fields):
+    """Mirror of ``moe_ep_adapter_config``."""
+    _fields_ = [("n_adapters", ctypes.c_int32), ("rank", ctypes.c_int32)]
+
+
 class NormConfig(_Fields):
     """Mirror of ``moe_ep_norm_config``; fields that are not named are 0, but for eps of 1e-6 and scales of 1."""
     _fields_ = [(n, ctypes.c_int32) for n in (
@@ -206,6 +211,13 @@ def load_library() -> ctypes.CDLL:
     lib.moe_ep_get_stage_ms.restype = ctypes.c_int
     lib.moe_ep_get_stage_ms.argtypes = [vp, vp, i32]
     dp = ctypes.POINTER(ctypes.c_double)
+    lib.moe_ep_validate_linear_adapters.restype = ctypes.c_int
+    lib.moe_ep_validate_linear_adapters.argtypes = [ctypes.POINTER(LinearConfig), ctypes.POINTER(AdapterConfig), whyp]
+    lib.moe_ep_linear_adapters_workspace_bytes.restype = ctypes.c_size_t
+    lib.moe_ep_linear_adapters_workspace_bytes.argtypes = [ctypes.POINTER(LinearConfig), ctypes.POINTER(AdapterConfig), i32]
+    lib.moe_ep_linear_adapters.restype = ctypes.c_int
+    lib.moe_ep_linear_adapters.argtypes = [ctypes.POINTER(LinearConfig), ctypes.POINTER(AdapterConfig), vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp,
+                                           ctypes.c_size_t, vp, whyp]
     lib.moe_ep_validate_norm.restype = ctypes.c_int
     lib.moe_ep_validate_norm.argtypes = [ctypes.POINTER(NormConfig), whyp]
     lib.moe_ep_norm.restype = ctypes.c_int
@@ -444,6 +456,54 @@ def linear(cfg: LinearConfig, x, weight, bias=None, residual=None, out=None, n_r
         ctypes.byref(cfg), _rows(x, "x", n_rows, K, cfg.x_stride or K, BF16, at), _rows(weight, "weight", N, K, cfg.weight_stride or K, F32 if cfg.weight_type else BF16, at),
         _vector(bias, "bias", N, F32, at), _rows(residual, "residual", n_rows, N, cfg.residual_stride or N, result, at), n_rows,
         _rows(out, "out", n_rows, N, cfg.out_stride or N, result, at), stream, ctypes.byref(why))
+    if rc != 0:
+        raise MoeEpError(rc, (why.value or b"").decode())
+    return rc
+
+
+def validate_linear_adapters(cfg: LinearConfig, adapters: AdapterConfig) -> Tuple[int, str]:
+    why = ctypes.c_char_p()
+    rc = load_library().moe_ep_validate_linear_adapters(ctypes.byref(cfg), ctypes.byref(adapters), ctypes.byref(why))
+    return rc, (why.value or b"").decode()
+
+
+def linear_adapters_workspace_bytes(cfg: LinearConfig, adapters: AdapterConfig, n_rows: int) -> int:
+    """moe_ep_linear_adapters_workspace_bytes: of a call of up to ``n_rows`` rows."""
+    if not 0 <= n_rows <= _MOST_ROWS:
+        return 0
+    return int(load_library().moe_ep_linear_adapters_workspace_bytes(ctypes.byref(cfg), ctypes.byref(adapters), n_rows))
+
+
+def linear_adapters(cfg: LinearConfig, adapters: AdapterConfig, x, weight, index, down, up, scale=None, bias=None, residual=None, out=None, workspace=None,
+                    n_rows: Optional[int] = None, workspace_bytes: Optional[int] = None, stream: Optional[int] = None) -> int:
+    """moe_ep_linear_adapters: out = act(x weight^T + bias + scale[a] (x down[a]^T) up[a]^T) + residual, a = index[row].
+
+    ``workspace`` is a contiguous tensor of at least ``linear_adapters_workspace_bytes`` bytes (a raw address comes with ``workspace_bytes``)."""
+    if n_rows is None:
+        n_rows = int(x.shape[0])
+    if not 0 <= n_rows <= _MOST_ROWS:
+        raise MoeEpError(-1, "n_rows must be in 0..2^30")
+    if stream is None:
+        stream = _current_stream(cfg.device)
+    K, N, at, n, rank = cfg.in_features, cfg.out_features, cfg.device, adapters.n_adapters, adapters.rank
+    result = F32 if cfg.out_type else BF16
+    if workspace is not None and workspace_bytes is None:
+        try:
+            workspace_bytes = workspace.numel() * workspace.element_size()
+        except AttributeError:
+            raise ValueError("workspace_bytes must be given with an address") from None
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        if workspace.get_device() != at:
+            _check_place(workspace, "workspace", at)
+        workspace = workspace.data_ptr()
+    why = ctypes.c_char_p()
+    rc = (_lib or load_library()).moe_ep_linear_adapters(
+        ctypes.byref(cfg), ctypes.byref(adapters), _rows(x, "x", n_rows, K, cfg.x_stride or K, BF16, at),
+        _rows(weight, "weight", N, K, cfg.weight_stride or K, F32 if cfg.weight_type else BF16, at), _vector(bias, "bias", N, F32, at),
+        _rows(residual, "residual", n_rows, N, cfg.residual_stride or N, result, at), _vector(index, "index", n_rows, _I32, at),
+        _vector(down, "down", n * rank * K, BF16, at), _vector(up, "up", n * rank * N, BF16, at), _vector(scale, "scale", n, F32, at), n_rows,
+        _rows(out, "out", n_rows, N, cfg.out_stride or N, result, at), _ptr(workspace), workspace_bytes or 0, stream, ctypes.byref(why))
     if rc != 0:
         raise MoeEpError(rc, (why.value or b"").decode())
     return rc

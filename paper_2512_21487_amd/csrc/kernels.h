@@ -245,6 +245,24 @@ enum {
 int linear_kernel(const LinearArgs& a, int n_cu);
 hipError_t launch_linear(const LinearArgs& a, int n_cu, hipStream_t s);
 
+// ---- the same product with low-rank adapters (adapters.hip, and the product's kernels): act(x W^T + bias + scale_a (x A_a^T) B_a^T) + residual
+struct NoAdapters { static constexpr bool on = false; };
+struct AdapterArgs {
+    static constexpr bool on = true;
+    const int32_t* index;               // of every row; one that is not in 0..n-1: none
+    const uint16_t *down, *up;          // A [n, rank, K], B [n, N, rank]
+    const float* scale;                 // [n] or NULL
+    uint16_t* low;                      // workspace [R, width]: scale_a x A_a^T as `parts` bf16 numbers that add up to it, [parts, rank] and a rest; rows with an adapter only
+    int32_t* lists;                     // workspace: of every tile of `tile` rows, tile + 1 numbers: how many adapters its rows have, and which
+    int n, rank, parts, width, tile;
+};
+// reduction steps of 64 that an adapter adds to a tile
+inline int adapter_width(int rank, int parts) { return (rank * parts + 63) / 64 * 64; }
+constexpr int kRankMost = 128;
+int linear_tile_rows(int kernel);       // of what linear_kernel chose; 0: no tiles
+hipError_t launch_adapters_down(const LinearArgs& a, const AdapterArgs& x, int n_cu, hipStream_t s);
+hipError_t launch_linear_adapters(const LinearArgs& a, const AdapterArgs& x, int n_cu, hipStream_t s);
+
 // ---- norms around a block (norm.hip): the public struct's fields as the kernels read them
 enum { kNormNone = 0, kNormRms, kNormLayer, kNormCount };
 enum { kGateAsIs = 0, kGateSigmoid, kGateSilu, kGateCount };

@@ -73,27 +73,23 @@ int linear_kernel(const LinearArgs& a, int n_cu)
     return split_kernel(a, n_cu);
 }
 
+int linear_tile_rows(int kernel)
+{
+    if (kernel < kLinearTiled) return 0;
+    if (kernel < kLinearStaged128x64) return kTilings[kernel - kLinearTiled].rows;
+    switch (kernel) {
+    case kLinearStaged128x64: return 128;
+    case kLinearSplit32x16: return 32;
+    case kLinearSplit16x16: return 16;
+    default: return 64;
+    }
+}
+
 hipError_t launch_linear(const LinearArgs& a, int n_cu, hipStream_t s)
 {
     if (a.R <= 0) return hipSuccess;
     if (a.N < 1 || a.K < 1) return hipErrorInvalidValue;
-    switch (linear_kernel(a, n_cu)) {
-    case kLinearRows1x1: return launch_rows<1, 1>(a, s);
-    case kLinearRows4x1: return launch_rows<4, 1>(a, s);
-    case kLinearRows4x2: return launch_rows<4, 2>(a, s);
-    case kLinearTiled + 0: return launch_tiled<256, 256, 2, 1>(a, n_cu, s);
-    case kLinearTiled + 1: return launch_tiled<256, 192, 2, 1>(a, n_cu, s);
-    case kLinearTiled + 2: return launch_tiled<192, 256, 2, 1>(a, n_cu, s);
-    case kLinearTiled + 3: return launch_tiled<128, 128, 4, 1>(a, n_cu, s);
-    case kLinearTiled + 4: return launch_tiled<64, 64, 4, 2>(a, n_cu, s);
-    case kLinearStaged128x64: return launch_tiled<128, 64, 2, 2, true>(a, n_cu, s);
-    case kLinearStaged64x64: return launch_tiled<64, 64, 2, 3, true>(a, n_cu, s);
-    case kLinearSplit64x32by4: return launch_split<4, 2, 4>(a, s);
-    case kLinearSplit64x32: return launch_split<4, 2, 8>(a, s);
-    case kLinearSplit64x16: return launch_split<4, 1, 8>(a, s);
-    case kLinearSplit32x16: return launch_split<2, 1, 16>(a, s);
-    default: return launch_split<1, 1, 16>(a, s);
-    }
+    return launch_chosen(linear_kernel(a, n_cu), a, NoAdapters{}, n_cu, s);
 }
 
 }  // namespace moe_ep

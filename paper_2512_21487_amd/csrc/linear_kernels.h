@@ -17,6 +17,31 @@ namespace {
 
 #define SB() __builtin_amdgcn_sched_barrier(0)
 
+// The kernels take adapters, or NoAdapters.  A row tile's reduction goes on behind K with `width` elements for every adapter that its rows have: on the
+// side of the rows their x A_a^T, zero in rows of another adapter or none, on the side of the weights B_a, once for each part.
+__device__ __forceinline__ int adapter_of(const AdapterArgs& x, int row)
+{
+    const int a = x.index[row];
+    return (unsigned)a < (unsigned)x.n ? a : -1;
+}
+// the adapters of a tile's rows
+struct TileAdapters {
+    const __attribute__((address_space(4))) int32_t* list;   // read as constants: another launch has written it
+    int count;
+    __device__ __forceinline__ void aim(const AdapterArgs& x, int tile)
+    {
+        list = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)(x.lists + (size_t)tile * (x.tile + 1));
+        count = list[0];
+    }
+    __device__ __forceinline__ int operator[](int i) const { return list[1 + i]; }
+};
+// where the 8 elements of chunk c of an adapter's width are in a row of B, or -1 beyond the last part
+__device__ __forceinline__ int rank_of_chunk(const AdapterArgs& x, int c)
+{
+    const int per = x.rank >> 3;
+    return c < per * x.parts ? (c - per * (c / per)) * 8 : -1;
+}
+
 // 0.5 z (1 + erf(z / sqrt 2)).  1 - erf(x) for x >= 0 is a polynomial in 1 / (1 + p x) times exp(-x^2) to 1.5e-7 (Abramowitz and Stegun,
 // Handbook of Mathematical Functions, 7.1.26), so that nothing cancels where z is negative.  Of z from N(0, 1) it is off by 8.4e-8 (RMS, of the result's)
 // and 3.3e-7 at most, the formula in fp32 by 3.8e-8 and 3.8e-7; half a step of bf16 is 3.9e-3, and sums of a few products are off by more.
@@ -193,8 +218,8 @@ hipError_t allow_lds(K* kernel, int bytes, std::atomic<uint64_t>& told)
 // A workgroup has C columns and up to RB rows: its threads take 8 elements of the reduction in turn, which reads the weights in whole
 // 4 or 8 KB, and their sums are added up through the wavefronts and LDS.  Latency bounds it: 1 x 160 x 5120 with fp32 weights 3.1 us (with 16
 // rows of a matrix instruction, 15 of them empty, 8.6), of which reading 3.3 MB is 0.6.
-template <int RB, int C, bool W32>
-__global__ __launch_bounds__(256) void linear_rows_kernel(LinearArgs a)
+template <int RB, int C, bool W32, class X>
+__global__ __launch_bounds__(256) void linear_rows_kernel(LinearArgs a, X x)
 {
     __shared__ float s_sum[4][C * RB];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -210,11 +235,11 @@ __global__ __launch_bounds__(256) void linear_rows_kernel(LinearArgs a)
     for (int k = tid * 8; k < a.K; k += 256 * 8) {
         const int left = a.K - k;
         Weight8 w[C];
-        u32x4_t x[RB];
+        u32x4_t xs[RB];
 #pragma unroll
         for (int c = 0; c < C; ++c) w[c] = load8(static_cast<const Weight*>(a.w) + (size_t)min(n0 + c, a.N - 1) * a.ldw + k, left);
 #pragma unroll
-        for (int r = 0; r < RB; ++r) x[r] = load8(a.x + (size_t)min(m0 + r, a.R - 1) * a.ldx + k, left);
+        for (int r = 0; r < RB; ++r) xs[r] = load8(a.x + (size_t)min(m0 + r, a.R - 1) * a.ldx + k, left);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             float f[8];
@@ -226,7 +251,29 @@ __global__ __launch_bounds__(256) void linear_rows_kernel(LinearArgs a)
 #pragma unroll
             for (int r = 0; r < RB; ++r)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) acc[c][r] = fmaf(f[i], (i & 1) ? bf16_hi(x[r][i >> 1]) : bf16_lo(x[r][i >> 1]), acc[c][r]);
+                for (int i = 0; i < 8; ++i) acc[c][r] = fmaf(f[i], (i & 1) ? bf16_hi(xs[r][i >> 1]) : bf16_lo(xs[r][i >> 1]), acc[c][r]);
+        }
+    }
+    if constexpr (X::on) {
+        // 16 lanes have a row's adapter, 8 of its rank each
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            if (tid >> 4 != r || (tid & 15) * 8 >= x.rank || m0 + r >= a.R) continue;
+            const int ad = adapter_of(x, m0 + r), j = (tid & 15) * 8;
+            if (ad < 0) continue;
+            const uint16_t* const low = x.low + (size_t)(m0 + r) * x.width + j;
+            float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            for (int p = x.parts - 1; p >= 0; --p) {          // the smallest first
+                const u32x4_t u = *reinterpret_cast<const u32x4_t*>(low + p * x.rank);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] += (i & 1) ? bf16_hi(u[i >> 1]) : bf16_lo(u[i >> 1]);
+            }
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const u32x4_t u = *reinterpret_cast<const u32x4_t*>(x.up + ((size_t)ad * a.N + min(n0 + c, a.N - 1)) * x.rank + j);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[c][r] = fmaf((i & 1) ? bf16_hi(u[i >> 1]) : bf16_lo(u[i >> 1]), v[i], acc[c][r]);
+            }
         }
     }
 #pragma unroll
@@ -253,13 +300,17 @@ __global__ __launch_bounds__(256) void linear_rows_kernel(LinearArgs a)
     }
 }
 
-template <int RB, int C>
-hipError_t launch_rows(const LinearArgs& a, hipStream_t s)
+template <int RB, int C, class X>
+hipError_t launch_rows(const LinearArgs& a, const X& x, hipStream_t s)
 {
     const long long grid = (long long)((a.N + C - 1) / C) * ((a.R + RB - 1) / RB);
     if (grid > 0x7fffffffll) return hipErrorInvalidValue;
-    if (a.w32) hipLaunchKernelGGL((linear_rows_kernel<RB, C, true>), dim3((unsigned)grid), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((linear_rows_kernel<RB, C, false>), dim3((unsigned)grid), dim3(256), 0, s, a);
+    if constexpr (!X::on)
+        if (a.w32) {
+            hipLaunchKernelGGL((linear_rows_kernel<RB, C, true, X>), dim3((unsigned)grid), dim3(256), 0, s, a, x);
+            return hipGetLastError();
+        }
+    hipLaunchKernelGGL((linear_rows_kernel<RB, C, false, X>), dim3((unsigned)grid), dim3(256), 0, s, a, x);
     return hipGetLastError();
 }
 
@@ -295,8 +346,8 @@ struct SplitCfg {
     static_assert(MB * NB * 1024 <= BYTES, "the sums take the place of the operands");
 };
 
-template <int MB, int NB, int WAVES, bool W32>
-__global__ __launch_bounds__(WAVES * 64) void linear_split_kernel(LinearArgs a)
+template <int MB, int NB, int WAVES, bool W32, class X>
+__global__ __launch_bounds__(WAVES * 64) void linear_split_kernel(LinearArgs a, X x)
 {
     using C = SplitCfg<MB, NB, W32>;
     constexpr int KS = C::KS;
@@ -322,8 +373,34 @@ __global__ __launch_bounds__(WAVES * 64) void linear_split_kernel(LinearArgs a)
 #pragma unroll
     for (int i = 0; i < C::WL; ++i) wo[i] = (uint32_t)min(i * (64 / (C::WROW / 16)) + wr, a.N - 1 - n0) * (uint32_t)a.ldw + wc * PER;
     struct Step { u32x4_t x[C::XL], w[C::WL]; } f;
+    const int k_steps = (a.K + KS - 1) / KS, whole = a.K / KS;
+    int steps = k_steps, adapter[C::XL];
+    TileAdapters tile;
+    if constexpr (X::on) {
+        tile.aim(x, m0 / (MB * 16));
+        steps += tile.count * (x.width / KS);
+#pragma unroll
+        for (int i = 0; i < C::XL; ++i) adapter[i] = m0 + i * 8 + xr < a.R ? adapter_of(x, m0 + i * 8 + xr) : -1;
+    }
     // whole: all 64 elements are there
     const auto load = [&](int step, bool whole) __attribute__((always_inline)) {
+        if constexpr (X::on)
+            if (step >= k_steps) {
+                const int per = x.width / KS, at = step - k_steps, i0 = at / per, ad = tile[i0], c = (at - i0 * per) * 8;
+                const int wk = rank_of_chunk(x, c + wc), xk = rank_of_chunk(x, c + xc);
+                const uint16_t* const up = x.up + ((size_t)ad * a.N + n0) * x.rank + wk;
+#pragma unroll
+                for (int i = 0; i < C::WL; ++i) {
+                    f.w[i] = u32x4_t{0, 0, 0, 0};
+                    if (wk >= 0) f.w[i] = *reinterpret_cast<const u32x4_t*>(up + (size_t)min(i * (64 / (C::WROW / 16)) + wr, a.N - 1 - n0) * x.rank);
+                }
+#pragma unroll
+                for (int i = 0; i < C::XL; ++i) {
+                    f.x[i] = u32x4_t{0, 0, 0, 0};
+                    if (xk >= 0 && adapter[i] == ad) f.x[i] = *reinterpret_cast<const u32x4_t*>(x.low + (size_t)(m0 + i * 8 + xr) * x.width + (c + xc) * 8);
+                }
+                return;
+            }
         const int left = a.K - step * KS;
 #pragma unroll
         for (int i = 0; i < C::WL; ++i) {
@@ -356,9 +433,9 @@ __global__ __launch_bounds__(WAVES * 64) void linear_split_kernel(LinearArgs a)
     const auto multiply = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            bf16x8_t x[MB];
+            bf16x8_t xs[MB];
 #pragma unroll
-            for (int i = 0; i < MB; ++i) x[i] = *reinterpret_cast<const bf16x8_t*>(own + (i * 16 + row) * 128 + ((h * 4 + kh) ^ sw) * 16);
+            for (int i = 0; i < MB; ++i) xs[i] = *reinterpret_cast<const bf16x8_t*>(own + (i * 16 + row) * 128 + ((h * 4 + kh) ^ sw) * 16);
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
                 const char* const at = own + C::X_BYTES + (j * 16 + row) * C::WROW;
@@ -371,16 +448,15 @@ __global__ __launch_bounds__(WAVES * 64) void linear_split_kernel(LinearArgs a)
 #pragma unroll
                     for (int p = 0; p < 3; ++p)
 #pragma unroll
-                        for (int i = 0; i < MB; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part[p], x[i], acc[i][j], 0, 0, 0);
+                        for (int i = 0; i < MB; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part[p], xs[i], acc[i][j], 0, 0, 0);
                 } else {
                     const bf16x8_t w = *reinterpret_cast<const bf16x8_t*>(at + ((h * 4 + kh) ^ sw) * 16);
 #pragma unroll
-                    for (int i = 0; i < MB; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x[i], acc[i][j], 0, 0, 0);
+                    for (int i = 0; i < MB; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, xs[i], acc[i][j], 0, 0, 0);
                 }
             }
         }
     };
-    const int steps = (a.K + KS - 1) / KS, whole = a.K / KS;
     if (wave < steps) load(wave, wave < whole);
     for (int st = wave; st < steps; st += WAVES) {
         to_lds();
@@ -415,25 +491,27 @@ __global__ __launch_bounds__(WAVES * 64) void linear_split_kernel(LinearArgs a)
     }
 }
 
-template <int MB, int NB, int WAVES, bool W32>
-hipError_t launch_split_as(const LinearArgs& a, long long workgroups, hipStream_t s)
+template <int MB, int NB, int WAVES, bool W32, class X>
+hipError_t launch_split_as(const LinearArgs& a, const X& x, long long workgroups, hipStream_t s)
 {
     constexpr int bytes = WAVES * SplitCfg<MB, NB, W32>::BYTES;
     static_assert(bytes <= 160 * 1024, "LDS of a compute unit");
     static std::atomic<uint64_t> told{0};
-    const hipError_t e = allow_lds(&linear_split_kernel<MB, NB, WAVES, W32>, bytes, told);
+    const hipError_t e = allow_lds(&linear_split_kernel<MB, NB, WAVES, W32, X>, bytes, told);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((linear_split_kernel<MB, NB, WAVES, W32>), grid_of(workgroups), dim3(WAVES * 64), bytes, s, a);
+    hipLaunchKernelGGL((linear_split_kernel<MB, NB, WAVES, W32, X>), grid_of(workgroups), dim3(WAVES * 64), bytes, s, a, x);
     return hipGetLastError();
 }
 
-template <int MB, int NB, int WAVES>
-hipError_t launch_split(LinearArgs a, hipStream_t s)
+template <int MB, int NB, int WAVES, class X>
+hipError_t launch_split(LinearArgs a, const X& x, hipStream_t s)
 {
     const long long mt = (a.R + MB * 16 - 1) / (MB * 16), nt = (a.N + NB * 16 - 1) / (NB * 16), per = (mt * nt + 7) / 8;
     // an XCD's tiles share the rows of the larger operand through its L2
     a.rows_first = (double)a.N * a.K * (a.w32 ? 4 : 2) > (double)a.R * a.K * 2;
-    return a.w32 ? launch_split_as<MB, NB, WAVES, true>(a, per * 8, s) : launch_split_as<MB, NB, WAVES, false>(a, per * 8, s);
+    if constexpr (!X::on)
+        if (a.w32) return launch_split_as<MB, NB, WAVES, true>(a, x, per * 8, s);
+    return launch_split_as<MB, NB, WAVES, false>(a, x, per * 8, s);
 }
 
 // ---- many rows and columns
@@ -585,8 +663,8 @@ __device__ __forceinline__ void row_of_blocks(int mb, const f32x4_t (&acc)[MB][N
 // STAGED: operands that are not on 16 bytes come in through registers, a K step ahead, and are written to the next slot in front of its hand-over.
 // RAGGED: the last K step is not whole.  ACT: there is an activation; a launch without one does not fetch the code of all of them (256 x 256
 // tiles: 3 us of 19)
-template <int BM, int BN, int SLOTS, int OCC, bool RAGGED, bool ACT, bool STAGED>
-__global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a)
+template <int BM, int BN, int SLOTS, int OCC, bool RAGGED, bool ACT, bool STAGED, class X>
+__global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a, X x)
 {
     using C = TileCfg<BM, BN, SLOTS>;
     constexpr int MB = C::MB, NB = C::NB, RPW = C::RPW, RX = C::RX;
@@ -610,7 +688,19 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a)
     const int ld_row = lane >> 3, ld_c = (lane & 7) ^ (lane >> 4);      // chunk of an even region's row; an odd one's is ld_c ^ 4
     const char *xi = nullptr, *wi = nullptr;
     uint32_t off[RPW];
+    // adapters: of the tile that is loaded its adapters, its first row and column, the K steps it has, the adapter of each row a lane loads; of the step that is
+    // loaded the adapter, its first chunk in `low`, and where the lane's even and odd regions' chunk is in a row of B
+    TileAdapters tile;
+    int tm = 0, tn = 0, steps = KT, adapter[X::on ? RX : 1], ad = 0, c0 = 0, at_rank[2] = {0, 0};
     const auto aim = [&](int m0, int n0) __attribute__((always_inline)) {
+        if constexpr (X::on) {
+            tm = m0;
+            tn = n0;
+            tile.aim(x, m0 / BM);
+            steps = KT + tile.count * (x.width / C::KS);
+#pragma unroll
+            for (int i = 0; i < RX; ++i) adapter[i] = adapter_of(x, min(m0 + (wave + C::NW * i) * 8 + ld_row, a.R - 1));
+        }
         xi = reinterpret_cast<const char*>(a.x + (size_t)m0 * a.ldx);
         wi = reinterpret_cast<const char*>(static_cast<const uint16_t*>(a.w) + (size_t)n0 * a.ldw);
 #pragma unroll
@@ -625,6 +715,17 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a)
     u32x4_t staged[STAGED ? RPW : 1];
     const auto issue = [&](int ks, int ring, int i) __attribute__((always_inline)) {
         const int j = wave + C::NW * (i < RX ? i : i - RX);
+        if constexpr (X::on)
+            if (ks >= KT) {
+                const int c = c0 + ((j & 1) ? ld_c ^ 4 : ld_c), k = at_rank[j & 1];
+                const char* src = reinterpret_cast<const char*>(kZeros);
+                if (i < RX) {
+                    if (k >= 0 && adapter[i < RX ? i : 0] == ad) src = reinterpret_cast<const char*>(x.low + (size_t)min(tm + j * 8 + ld_row, a.R - 1) * x.width + c * 8);
+                } else if (k >= 0) src = reinterpret_cast<const char*>(x.up + ((size_t)ad * a.N + min(tn + j * 8 + ld_row, a.N - 1)) * x.rank + k);
+                if constexpr (STAGED) staged[i] = *reinterpret_cast<const u32x4_t*>(src);
+                else load_to_lds(lds_base + (uint32_t)(ring * C::SLOT_BYTES + (i < RX ? 0 : BM * 128) + j * 1024), src);
+                return;
+            }
         if constexpr (STAGED) {
             const uint16_t* const p = reinterpret_cast<const uint16_t*>((i < RX ? xi : wi) + ks * (C::KS * 2) + off[i]);
             if (RAGGED && ks == KT - 1) staged[i] = load_part<8>(p, a.K - ks * C::KS - ((j & 1) ? ld_c ^ 4 : ld_c) * 8, a.K);
@@ -673,12 +774,21 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a)
     aim(m0, n0);
     int ring = 0, ki = 0, next_m0 = m0, next_n0 = n0;   // ki: the K step whose loads start at the next hand-over
     bool more = true;                                    // there is a tile behind the one that is multiplied
+    int tile_steps = steps;                              // of the tile that is multiplied
     const auto advance = [&]() __attribute__((always_inline)) {
-        if (ki == KT) {
+        if (ki == steps) {
             more = tile_at(it + 1, next_m0, next_n0);
             if (more) aim(next_m0, next_n0);     // the last tile's loads go round to its own first K steps, and are not used
             ki = 0;
         }
+        if constexpr (X::on)
+            if (ki >= KT) {
+                const int per = x.width / C::KS, at = ki - KT, i = at / per;
+                ad = tile[i];
+                c0 = (at - i * per) * 8;
+                at_rank[0] = rank_of_chunk(x, c0 + ld_c);
+                at_rank[1] = rank_of_chunk(x, c0 + (ld_c ^ 4));
+            }
     };
 #pragma unroll
     for (int st = 0; st < SLOTS - 1; ++st) {
@@ -704,7 +814,7 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a)
         SB();
         asm volatile("s_nop 7");
         SB();
-        for (int kt = 0; kt < KT; ++kt) {
+        for (int kt = 0; kt < (X::on ? tile_steps : KT); ++kt) {
             const int other = ring == SLOTS - 1 ? 0 : ring + 1, last = ring == 0 ? SLOTS - 1 : ring - 1;
 #pragma unroll
             for (int p = 0; p < C::M; ++p) {
@@ -748,37 +858,61 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a)
         if (!more) break;
         m0 = next_m0;
         n0 = next_n0;
+        if constexpr (X::on) tile_steps = steps;
         ++it;
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);   // no load may land in LDS that is another workgroup's by then
 }
 
-template <int BM, int BN, int SLOTS, int OCC, bool RAGGED, bool ACT, bool STAGED>
-hipError_t launch_tiled_as(const LinearArgs& a, int n_cu, hipStream_t s)
+template <int BM, int BN, int SLOTS, int OCC, bool RAGGED, bool ACT, bool STAGED, class X>
+hipError_t launch_tiled_as(const LinearArgs& a, const X& x, int n_cu, hipStream_t s)
 {
     using C = TileCfg<BM, BN, SLOTS>;
     static_assert(C::LDS_BYTES * OCC <= 160 * 1024, "LDS of a compute unit");
     static std::atomic<uint64_t> told{0};
-    const hipError_t e = allow_lds(&linear_tiled_kernel<BM, BN, SLOTS, OCC, RAGGED, ACT, STAGED>, C::LDS_BYTES, told);
+    const hipError_t e = allow_lds(&linear_tiled_kernel<BM, BN, SLOTS, OCC, RAGGED, ACT, STAGED, X>, C::LDS_BYTES, told);
     if (e != hipSuccess) return e;
     const long long total = (long long)((a.R + BM - 1) / BM) * ((a.N + BN - 1) / BN);
     if (total > 0x3fffffffll) return hipErrorInvalidValue;
     // as few workgroups as it takes for as many rounds, the same number on every XCD
     const long long wgs = (long long)n_cu * OCC, rounds = (total + wgs - 1) / wgs;
     const int grid = (int)(((total + rounds - 1) / rounds + 7) / 8 * 8);
-    hipLaunchKernelGGL((linear_tiled_kernel<BM, BN, SLOTS, OCC, RAGGED, ACT, STAGED>), dim3(grid), dim3(256), C::LDS_BYTES, s, a);
+    hipLaunchKernelGGL((linear_tiled_kernel<BM, BN, SLOTS, OCC, RAGGED, ACT, STAGED, X>), dim3(grid), dim3(256), C::LDS_BYTES, s, a, x);
     return hipGetLastError();
 }
 
-template <int BM, int BN, int SLOTS, int OCC, bool STAGED = false>
-hipError_t launch_tiled(const LinearArgs& a, int n_cu, hipStream_t s)
+template <int BM, int BN, int SLOTS, int OCC, bool STAGED, class X>
+hipError_t launch_tiled(const LinearArgs& a, const X& x, int n_cu, hipStream_t s)
 {
     // (staged: K is seldom whole)
     if constexpr (!STAGED) {
-        if (a.act == kActNone && a.K % 64 == 0) return launch_tiled_as<BM, BN, SLOTS, OCC, false, false, false>(a, n_cu, s);
-        if (a.K % 64 == 0) return launch_tiled_as<BM, BN, SLOTS, OCC, false, true, false>(a, n_cu, s);
+        if (a.act == kActNone && a.K % 64 == 0) return launch_tiled_as<BM, BN, SLOTS, OCC, false, false, false>(a, x, n_cu, s);
+        if (a.K % 64 == 0) return launch_tiled_as<BM, BN, SLOTS, OCC, false, true, false>(a, x, n_cu, s);
     }
-    return a.act == kActNone ? launch_tiled_as<BM, BN, SLOTS, OCC, true, false, STAGED>(a, n_cu, s) : launch_tiled_as<BM, BN, SLOTS, OCC, true, true, STAGED>(a, n_cu, s);
+    return a.act == kActNone ? launch_tiled_as<BM, BN, SLOTS, OCC, true, false, STAGED>(a, x, n_cu, s) : launch_tiled_as<BM, BN, SLOTS, OCC, true, true, STAGED>(a, x, n_cu, s);
+}
+
+// a kernel that linear_kernel chose
+template <class X>
+hipError_t launch_chosen(int kernel, const LinearArgs& a, const X& x, int n_cu, hipStream_t s)
+{
+    switch (kernel) {
+    case kLinearRows1x1: return launch_rows<1, 1>(a, x, s);
+    case kLinearRows4x1: return launch_rows<4, 1>(a, x, s);
+    case kLinearRows4x2: return launch_rows<4, 2>(a, x, s);
+    case kLinearTiled + 0: return launch_tiled<256, 256, 2, 1, false>(a, x, n_cu, s);
+    case kLinearTiled + 1: return launch_tiled<256, 192, 2, 1, false>(a, x, n_cu, s);
+    case kLinearTiled + 2: return launch_tiled<192, 256, 2, 1, false>(a, x, n_cu, s);
+    case kLinearTiled + 3: return launch_tiled<128, 128, 4, 1, false>(a, x, n_cu, s);
+    case kLinearTiled + 4: return launch_tiled<64, 64, 4, 2, false>(a, x, n_cu, s);
+    case kLinearStaged128x64: return launch_tiled<128, 64, 2, 2, true>(a, x, n_cu, s);
+    case kLinearStaged64x64: return launch_tiled<64, 64, 2, 3, true>(a, x, n_cu, s);
+    case kLinearSplit64x32by4: return launch_split<4, 2, 4>(a, x, s);
+    case kLinearSplit64x32: return launch_split<4, 2, 8>(a, x, s);
+    case kLinearSplit64x16: return launch_split<4, 1, 8>(a, x, s);
+    case kLinearSplit32x16: return launch_split<2, 1, 16>(a, x, s);
+    default: return launch_split<1, 1, 16>(a, x, s);
+    }
 }
 
 }  // namespace

@@ -84,7 +84,41 @@ const char* out_of_reach(const Span* sp, int n, int device)
 
 bool off_alignment(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) != 0; }
 
-constexpr long long kMostStride = 1ll << 22, kMostFeatures = 1 << 20, kMostRows = 1 << 30;
+constexpr long long kMostStride = 1ll << 22, kMostFeatures = 1 << 20, kMostRows = 1 << 30, kMostAdapters = 1 << 20;
+
+// A product's arguments as its kernels read them, and what it reads and writes
+struct Product {
+    static constexpr int kSpans = 5;
+    LinearArgs args{};
+    Span spans[kSpans];
+    bool aligned;
+    Product(const moe_ep_linear_config& c, const void* x, const void* weight, const float* bias, const void* residual, int32_t n_rows, void* out)
+    {
+        const int K = c.in_features, N = c.out_features;
+        const int ws = c.weight_type == MOE_EP_F32 ? 4 : 2, os = c.out_type == MOE_EP_F32 ? 4 : 2;
+        const long long ldx = c.x_stride ? c.x_stride : K, ldw = c.weight_stride ? c.weight_stride : K;
+        const long long ldr = c.residual_stride ? c.residual_stride : N, ldo = c.out_stride ? c.out_stride : N;
+        aligned = !off_alignment(x, 2) && !off_alignment(weight, ws) && !off_alignment(bias, 4) && !off_alignment(residual, os) && !off_alignment(out, os);
+        // an element of the residual is read by the lane that writes the result in its place: the same buffer may be both
+        const bool in_place = residual == out && ldr == ldo;
+        const size_t rows = (size_t)n_rows;
+        spans[0] = {x, rows, (size_t)ldx * 2, (size_t)K * 2, "x", false};
+        spans[1] = {weight, (size_t)N, (size_t)ldw * ws, (size_t)K * ws, "weight", false};
+        spans[2] = {bias, 1, 0, (size_t)N * 4, "bias", false};
+        spans[3] = {in_place ? nullptr : residual, rows, (size_t)ldr * os, (size_t)N * os, "residual", false};
+        spans[4] = {out, rows, (size_t)ldo * os, (size_t)N * os, "out", true};
+        args.x = static_cast<const uint16_t*>(x); args.w = weight; args.bias = bias; args.residual = residual; args.out = out;
+        args.ldx = ldx; args.ldw = ldw; args.ldr = ldr; args.ldo = ldo;
+        args.R = n_rows; args.N = N; args.K = K; args.act = c.activation;
+        args.w32 = ws == 4; args.out32 = os == 4;
+    }
+};
+
+// bf16 numbers that stand for one of x A^T, and what the workspace holds: of every row its own, then the lists of the row tiles, which are 16 rows at least and
+// hold a number more than rows
+int parts_of(const moe_ep_linear_config& c) { return c.out_type == MOE_EP_F32 ? 3 : 2; }
+size_t low_bytes(const moe_ep_linear_config& c, const moe_ep_adapter_config& ad, int32_t n_rows) { return (size_t)n_rows * adapter_width(ad.rank, parts_of(c)) * 2; }
+size_t lists_bytes(int32_t n_rows) { return ((size_t)n_rows + n_rows / 16 + 272) * 4; }
 
 }  // namespace
 
@@ -163,32 +197,76 @@ int moe_ep_linear(const moe_ep_linear_config* c, const void* x, const void* weig
     if (n_rows < 0 || n_rows > kMostRows) return refuse(why, "n_rows must be in 0..2^30");
     if (n_rows == 0) return MOE_EP_OK;
     if (!x || !weight || !out) return refuse(why, "x, weight and out must not be NULL");
-    const int K = c->in_features, N = c->out_features;
-    const int ws = c->weight_type == MOE_EP_F32 ? 4 : 2, os = c->out_type == MOE_EP_F32 ? 4 : 2;
-    const long long ldx = c->x_stride ? c->x_stride : K, ldw = c->weight_stride ? c->weight_stride : K;
-    const long long ldr = c->residual_stride ? c->residual_stride : N, ldo = c->out_stride ? c->out_stride : N;
-    if (off_alignment(x, 2) || off_alignment(weight, ws) || off_alignment(bias, 4) || off_alignment(residual, os) || off_alignment(out, os))
-        return refuse(why, "x, weight, bias, residual and out must be aligned to their elements");
-    // an element of the residual is read by the lane that writes the result in its place: the same buffer may be both
-    const bool in_place = residual == out && ldr == ldo;
-    const size_t rows = (size_t)n_rows;
-    const Span sp[] = {{x, rows, (size_t)ldx * 2, (size_t)K * 2, "x", false},
-                       {weight, (size_t)N, (size_t)ldw * ws, (size_t)K * ws, "weight", false},
-                       {bias, 1, 0, (size_t)N * 4, "bias", false},
-                       {in_place ? nullptr : residual, rows, (size_t)ldr * os, (size_t)N * os, "residual", false},
-                       {out, rows, (size_t)ldo * os, (size_t)N * os, "out", true}};
-    if (const char* bad = overlap(sp, 5)) return refuse(why, bad);
+    const Product p(*c, x, weight, bias, residual, n_rows, out);
+    if (!p.aligned) return refuse(why, "x, weight, bias, residual and out must be aligned to their elements");
+    if (const char* bad = overlap(p.spans, Product::kSpans)) return refuse(why, bad);
     DeviceScope device(c->device);
     if (device.error != hipSuccess) return hip_failed(why, "selecting the device", device.error);
-    if (const char* bad = out_of_reach(sp, 5, c->device)) return refuse(why, bad);
-    LinearArgs a{};
-    a.x = static_cast<const uint16_t*>(x); a.w = weight; a.bias = bias; a.residual = residual; a.out = out;
-    a.ldx = ldx; a.ldw = ldw; a.ldr = ldr; a.ldo = ldo;
-    a.R = n_rows; a.N = N; a.K = K; a.act = c->activation;
-    a.w32 = ws == 4; a.out32 = os == 4;
+    if (const char* bad = out_of_reach(p.spans, Product::kSpans, c->device)) return refuse(why, bad);
     int n_cu = 0;
     hipError_t e = hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, c->device);
-    if (e == hipSuccess) e = launch_linear(a, n_cu, static_cast<hipStream_t>(stream));
+    if (e == hipSuccess) e = launch_linear(p.args, n_cu, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? MOE_EP_OK : hip_failed(why, "launch", e);
+}
+
+int moe_ep_validate_linear_adapters(const moe_ep_linear_config* c, const moe_ep_adapter_config* ad, const char** why)
+{
+    if (moe_ep_validate_linear(c, why) != MOE_EP_OK) return MOE_EP_EINVAL;
+    if (c->weight_type != MOE_EP_BF16) return refuse(why, "weight_type must be MOE_EP_BF16 beside adapters");
+    if (!ad) return refuse(why, "adapters is NULL");
+    if (ad->n_adapters < 1 || ad->n_adapters > kMostAdapters) return refuse(why, "n_adapters must be in 1..2^20");
+    if (ad->rank < 8 || ad->rank > kRankMost || ad->rank % 8) return refuse(why, "rank must be a multiple of 8 in 8..128");
+    return MOE_EP_OK;
+}
+
+size_t moe_ep_linear_adapters_workspace_bytes(const moe_ep_linear_config* c, const moe_ep_adapter_config* ad, int32_t n_rows)
+{
+    if (moe_ep_validate_linear_adapters(c, ad, nullptr) != MOE_EP_OK || n_rows < 1 || n_rows > kMostRows) return 0;
+    return low_bytes(*c, *ad, n_rows) + lists_bytes(n_rows);
+}
+
+int moe_ep_linear_adapters(const moe_ep_linear_config* c, const moe_ep_adapter_config* ad, const void* x, const void* weight, const float* bias,
+                           const void* residual, const int32_t* index, const void* down, const void* up, const float* scale, int32_t n_rows, void* out,
+                           void* workspace, size_t workspace_bytes, void* stream, const char** why)
+{
+    if (moe_ep_validate_linear_adapters(c, ad, why) != MOE_EP_OK) return MOE_EP_EINVAL;
+    if (n_rows < 0 || n_rows > kMostRows) return refuse(why, "n_rows must be in 0..2^30");
+    if (n_rows == 0) return MOE_EP_OK;
+    if (!x || !weight || !out) return refuse(why, "x, weight and out must not be NULL");
+    if (!index || !down || !up || !workspace) return refuse(why, "index, down, up and workspace must not be NULL");
+    const Product p(*c, x, weight, bias, residual, n_rows, out);
+    if (!p.aligned || off_alignment(index, 4) || off_alignment(down, 2) || off_alignment(scale, 4))
+        return refuse(why, "x, weight, bias, residual, index, down, scale and out must be aligned to their elements");
+    if (off_alignment(up, 16) || off_alignment(workspace, 16)) return refuse(why, "up and workspace must be aligned to 16 bytes");
+    const size_t need = moe_ep_linear_adapters_workspace_bytes(c, ad, n_rows);
+    if (workspace_bytes < need) {
+        snprintf(t_text, sizeof t_text, "workspace has %zu bytes, the call needs %zu", workspace_bytes, need);
+        return refuse(why, t_text);
+    }
+    const size_t n = (size_t)ad->n_adapters, each = (size_t)ad->rank * 2;
+    constexpr int kSpans = Product::kSpans + 5;
+    Span sp[kSpans];
+    for (int i = 0; i < Product::kSpans; ++i) sp[i] = p.spans[i];
+    Span* const mine = sp + Product::kSpans;
+    mine[0] = {index, 1, 0, (size_t)n_rows * 4, "index", false};
+    mine[1] = {down, 1, 0, n * each * (size_t)c->in_features, "down", false};
+    mine[2] = {up, 1, 0, n * each * (size_t)c->out_features, "up", false};
+    mine[3] = {scale, 1, 0, n * 4, "scale", false};
+    mine[4] = {workspace, 1, 0, need, "workspace", true};
+    if (const char* bad = overlap(sp, kSpans)) return refuse(why, bad);
+    DeviceScope device(c->device);
+    if (device.error != hipSuccess) return hip_failed(why, "selecting the device", device.error);
+    if (const char* bad = out_of_reach(sp, kSpans, c->device)) return refuse(why, bad);
+    int n_cu = 0;
+    hipError_t e = hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, c->device);
+    if (e != hipSuccess) return hip_failed(why, "launch", e);
+    AdapterArgs a{};
+    a.index = index; a.down = static_cast<const uint16_t*>(down); a.up = static_cast<const uint16_t*>(up); a.scale = scale;
+    a.low = static_cast<uint16_t*>(workspace);
+    a.lists = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + low_bytes(*c, *ad, n_rows));
+    a.n = ad->n_adapters; a.rank = ad->rank; a.parts = parts_of(*c); a.width = adapter_width(a.rank, a.parts);
+    a.tile = linear_tile_rows(linear_kernel(p.args, n_cu));
+    e = launch_linear_adapters(p.args, a, n_cu, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? MOE_EP_OK : hip_failed(why, "launch", e);
 }
 
