@@ -26,7 +26,8 @@ struct Distinct {
 // the list of a tile of up to 256 rows, by one wavefront
 __device__ __forceinline__ void make_list(const LinearArgs& a, const AdapterArgs& x, long long tile, int lane)
 {
-    int32_t* const list = x.lists + tile * (x.tile + 1);
+    int32_t* const list = x.lists + tile * adapter_list(x.tile);
+    const int masks = (x.tile + 31) / 32;
     int mine[4], count = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -37,12 +38,19 @@ __device__ __forceinline__ void make_list(const LinearArgs& a, const AdapterArgs
     for (int i = 0; i < 4; ++i) {
         Distinct d(mine[i]);
         int adapter;
-        unsigned long long who;
-        while (d.next(adapter, who)) {
+        unsigned long long who[4] = {0, 0, 0, 0};
+        while (d.next(adapter, who[i])) {
 #pragma unroll
-            for (int j = i + 1; j < 4; ++j)
+            for (int j = i + 1; j < 4; ++j) {
+                who[j] = __ballot(mine[j] == adapter);
                 if (mine[j] == adapter) mine[j] = -1;
-            if (lane == 0) list[1 + count] = adapter;
+            }
+            // lane 0 writes the number, lane 1 + m the rows 32 m ..
+            uint32_t v = (uint32_t)adapter;
+#pragma unroll
+            for (int m = 0; m < 8; ++m)
+                if (lane == 1 + m) v = (uint32_t)(who[m >> 1] >> (m & 1) * 32);
+            if (lane <= masks) list[1 + count * (1 + masks) + lane] = (int32_t)v;
             ++count;
         }
     }
@@ -53,7 +61,7 @@ __device__ __forceinline__ void make_list(const LinearArgs& a, const AdapterArgs
 // time and the last rounded: two leave 2^-17 of the sum, which is 2^-8 of what rounding the result to bf16 leaves, three 2^-25 (results in fp32).
 __device__ __forceinline__ void store_low(const AdapterArgs& x, long long row, int r, f32x4_t v)
 {
-    uint16_t* const to = x.low + row * x.width + r;
+    uint16_t* const to = x.low + row * adapter_pitch(x.width) + r;
     for (int p = 0; p < x.parts; ++p) {
         u32x2_t u;
         if (p + 1 == x.parts) u = u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
@@ -86,6 +94,9 @@ __global__ __launch_bounds__(WAVES * 64) void adapters_down_kernel(LinearArgs a,
     if (m0 >= a.R) return;
     char* const own = reinterpret_cast<char*>(lds4) + wave * C::BYTES;
     const int xr = lane >> 3, xc = lane & 7, row = lane & 15, kh = lane >> 4, sw = (row >> 1) & 7;
+    // the zeros behind every row, one with an adapter or not
+    if (b % blocks == 0 && group == 0 && wave == 0 && lane < MB * 16 && m0 + lane < a.R)
+        *reinterpret_cast<u32x4_t*>(x.low + (m0 + lane) * adapter_pitch(x.width) + x.width) = u32x4_t{0, 0, 0, 0};
     Distinct tile(lane < MB * 16 && m0 + lane < a.R ? adapter_of(x, (int)(m0 + lane)) : -1);
     int adapter;
     unsigned long long who;

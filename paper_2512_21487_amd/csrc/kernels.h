@@ -252,12 +252,15 @@ struct AdapterArgs {
     const int32_t* index;               // of every row; one that is not in 0..n-1: none
     const uint16_t *down, *up;          // A [n, rank, K], B [n, N, rank]
     const float* scale;                 // [n] or NULL
-    uint16_t* low;                      // workspace [R, width]: scale_a x A_a^T as `parts` bf16 numbers that add up to it, [parts, rank] and a rest; rows with an adapter only
-    int32_t* lists;                     // workspace: of every tile of `tile` rows, tile + 1 numbers: how many adapters its rows have, and which
+    uint16_t* low;                      // workspace [R, adapter_pitch(width)]: scale_a x A_a^T as `parts` bf16 numbers that add up to it, [parts, rank], of rows with an adapter; behind
+                                        // `width` elements of every row 8 zeros
+    int32_t* lists;                     // workspace: of every tile of `tile` rows, adapter_list(tile) numbers: how many adapters its rows have, each one's number and a bit for every row
     int n, rank, parts, width, tile;
 };
 // reduction steps of 64 that an adapter adds to a tile
 inline int adapter_width(int rank, int parts) { return (rank * parts + 63) / 64 * 64; }
+__host__ __device__ constexpr int adapter_pitch(int width) { return width + 8; }
+__host__ __device__ constexpr int adapter_list(int tile) { return 1 + tile * (1 + (tile + 31) / 32); }
 constexpr int kRankMost = 128;
 int linear_tile_rows(int kernel);       // of what linear_kernel chose; 0: no tiles
 hipError_t launch_adapters_down(const LinearArgs& a, const AdapterArgs& x, int n_cu, hipStream_t s);

@@ -24,16 +24,19 @@ __device__ __forceinline__ int adapter_of(const AdapterArgs& x, int row)
     const int a = x.index[row];
     return (unsigned)a < (unsigned)x.n ? a : -1;
 }
-// the adapters of a tile's rows
+// The adapters of a tile of TILE rows: how many, and for each its number and a bit for every row
+template <int TILE>
 struct TileAdapters {
+    static constexpr int MASKS = (TILE + 31) / 32, ENTRY = 1 + MASKS;
     const __attribute__((address_space(4))) int32_t* list;   // read as constants: another launch has written it
     int count;
     __device__ __forceinline__ void aim(const AdapterArgs& x, int tile)
     {
-        list = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)(x.lists + (size_t)tile * (x.tile + 1));
+        list = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)(x.lists + (size_t)tile * adapter_list(TILE));
         count = list[0];
     }
-    __device__ __forceinline__ int operator[](int i) const { return list[1 + i]; }
+    __device__ __forceinline__ int adapter(int i) const { return list[1 + i * ENTRY]; }
+    __device__ __forceinline__ uint32_t rows(int i, int m) const { return (uint32_t)list[2 + i * ENTRY + m]; }   // 32 m ..
 };
 // where the 8 elements of chunk c of an adapter's width are in a row of B, or -1 beyond the last part
 __device__ __forceinline__ int rank_of_chunk(const AdapterArgs& x, int c)
@@ -261,7 +264,7 @@ __global__ __launch_bounds__(256) void linear_rows_kernel(LinearArgs a, X x)
             if (tid >> 4 != r || (tid & 15) * 8 >= x.rank || m0 + r >= a.R) continue;
             const int ad = adapter_of(x, m0 + r), j = (tid & 15) * 8;
             if (ad < 0) continue;
-            const uint16_t* const low = x.low + (size_t)(m0 + r) * x.width + j;
+            const uint16_t* const low = x.low + (size_t)(m0 + r) * adapter_pitch(x.width) + j;
             float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             for (int p = x.parts - 1; p >= 0; --p) {          // the smallest first
                 const u32x4_t u = *reinterpret_cast<const u32x4_t*>(low + p * x.rank);
@@ -374,19 +377,17 @@ __global__ __launch_bounds__(WAVES * 64) void linear_split_kernel(LinearArgs a, 
     for (int i = 0; i < C::WL; ++i) wo[i] = (uint32_t)min(i * (64 / (C::WROW / 16)) + wr, a.N - 1 - n0) * (uint32_t)a.ldw + wc * PER;
     struct Step { u32x4_t x[C::XL], w[C::WL]; } f;
     const int k_steps = (a.K + KS - 1) / KS, whole = a.K / KS;
-    int steps = k_steps, adapter[C::XL];
-    TileAdapters tile;
+    int steps = k_steps;
+    TileAdapters<MB * 16> tile;
     if constexpr (X::on) {
         tile.aim(x, m0 / (MB * 16));
         steps += tile.count * (x.width / KS);
-#pragma unroll
-        for (int i = 0; i < C::XL; ++i) adapter[i] = m0 + i * 8 + xr < a.R ? adapter_of(x, m0 + i * 8 + xr) : -1;
     }
     // whole: all 64 elements are there
     const auto load = [&](int step, bool whole) __attribute__((always_inline)) {
         if constexpr (X::on)
             if (step >= k_steps) {
-                const int per = x.width / KS, at = step - k_steps, i0 = at / per, ad = tile[i0], c = (at - i0 * per) * 8;
+                const int per = x.width / KS, at = step - k_steps, i0 = at / per, ad = tile.adapter(i0), c = (at - i0 * per) * 8;
                 const int wk = rank_of_chunk(x, c + wc), xk = rank_of_chunk(x, c + xc);
                 const uint16_t* const up = x.up + ((size_t)ad * a.N + n0) * x.rank + wk;
 #pragma unroll
@@ -397,7 +398,8 @@ __global__ __launch_bounds__(WAVES * 64) void linear_split_kernel(LinearArgs a, 
 #pragma unroll
                 for (int i = 0; i < C::XL; ++i) {
                     f.x[i] = u32x4_t{0, 0, 0, 0};
-                    if (xk >= 0 && adapter[i] == ad) f.x[i] = *reinterpret_cast<const u32x4_t*>(x.low + (size_t)(m0 + i * 8 + xr) * x.width + (c + xc) * 8);
+                    if (xk >= 0 && (tile.rows(i0, i >> 2) >> ((i & 3) * 8 + xr) & 1))
+                        f.x[i] = *reinterpret_cast<const u32x4_t*>(x.low + (size_t)(m0 + i * 8 + xr) * adapter_pitch(x.width) + (c + xc) * 8);
                 }
                 return;
             }
@@ -688,18 +690,15 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a, X 
     const int ld_row = lane >> 3, ld_c = (lane & 7) ^ (lane >> 4);      // chunk of an even region's row; an odd one's is ld_c ^ 4
     const char *xi = nullptr, *wi = nullptr;
     uint32_t off[RPW];
-    // adapters: of the tile that is loaded its adapters, its first row and column, the K steps it has, the adapter of each row a lane loads; of the step that is
-    // loaded the adapter, its first chunk in `low`, and where the lane's even and odd regions' chunk is in a row of B
-    TileAdapters tile;
-    int tm = 0, tn = 0, steps = KT, adapter[X::on ? RX : 1], ad = 0, c0 = 0, at_rank[2] = {0, 0};
+    // adapters of the tile that is loaded, its first row and column, and the K steps it has
+    TileAdapters<BM> tile;
+    int tm = 0, tn = 0, steps = KT;
     const auto aim = [&](int m0, int n0) __attribute__((always_inline)) {
         if constexpr (X::on) {
             tm = m0;
             tn = n0;
             tile.aim(x, m0 / BM);
             steps = KT + tile.count * (x.width / C::KS);
-#pragma unroll
-            for (int i = 0; i < RX; ++i) adapter[i] = adapter_of(x, min(m0 + (wave + C::NW * i) * 8 + ld_row, a.R - 1));
         }
         xi = reinterpret_cast<const char*>(a.x + (size_t)m0 * a.ldx);
         wi = reinterpret_cast<const char*>(static_cast<const uint16_t*>(a.w) + (size_t)n0 * a.ldw);
@@ -710,22 +709,30 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a, X 
             off[i] = ((uint32_t)row * (uint32_t)(i < RX ? a.ldx : a.ldw) + c * 8) * 2u;
         }
     };
+    // Step ks, behind K, is one of an adapter's: the loads go on as they are, from other places.  Rows of another adapter or none, and what is beyond the last part, read the
+    // zeros behind a row of `low`; what they are multiplied with, B's rows and columns that are there, is finite.
+    const auto aim_adapter = [&](int ks) __attribute__((always_inline)) {
+        if constexpr (X::on) {
+            static_assert(C::NW == 4, "a wavefront's regions are 32 rows apart, all even or all odd");
+            const int per = x.width / C::KS, at = ks - KT, i0 = at / per, ad = tile.adapter(i0), c = (at - i0 * per) * 8 + ((wave & 1) ? ld_c ^ 4 : ld_c);
+            const int k = rank_of_chunk(x, c), row0 = wave * 8 + ld_row;
+            const uint32_t pitch = (uint32_t)adapter_pitch(x.width) * 2u;
+            xi = reinterpret_cast<const char*>(x.low) + (size_t)tm * pitch - (size_t)ks * (C::KS * 2);
+            wi = reinterpret_cast<const char*>(x.up + ((size_t)ad * a.N + tn) * x.rank) - (size_t)ks * (C::KS * 2);
+#pragma unroll
+            for (int i = 0; i < RX; ++i) {
+                const bool its = k >= 0 && (tile.rows(i0, i) >> row0 & 1);
+                off[i] = (uint32_t)min(row0 + i * 32, a.R - 1 - tm) * pitch + (its ? c * 16u : (uint32_t)x.width * 2u);
+            }
+#pragma unroll
+            for (int i = RX; i < RPW; ++i) off[i] = ((uint32_t)min(row0 + (i - RX) * 32, a.N - 1 - tn) * (uint32_t)x.rank + (k < 0 ? 0 : k)) * 2u;
+        }
+    };
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
     static_assert(!STAGED || SLOTS == 2, "one K step in registers");
     u32x4_t staged[STAGED ? RPW : 1];
     const auto issue = [&](int ks, int ring, int i) __attribute__((always_inline)) {
         const int j = wave + C::NW * (i < RX ? i : i - RX);
-        if constexpr (X::on)
-            if (ks >= KT) {
-                const int c = c0 + ((j & 1) ? ld_c ^ 4 : ld_c), k = at_rank[j & 1];
-                const char* src = reinterpret_cast<const char*>(kZeros);
-                if (i < RX) {
-                    if (k >= 0 && adapter[i < RX ? i : 0] == ad) src = reinterpret_cast<const char*>(x.low + (size_t)min(tm + j * 8 + ld_row, a.R - 1) * x.width + c * 8);
-                } else if (k >= 0) src = reinterpret_cast<const char*>(x.up + ((size_t)ad * a.N + min(tn + j * 8 + ld_row, a.N - 1)) * x.rank + k);
-                if constexpr (STAGED) staged[i] = *reinterpret_cast<const u32x4_t*>(src);
-                else load_to_lds(lds_base + (uint32_t)(ring * C::SLOT_BYTES + (i < RX ? 0 : BM * 128) + j * 1024), src);
-                return;
-            }
         if constexpr (STAGED) {
             const uint16_t* const p = reinterpret_cast<const uint16_t*>((i < RX ? xi : wi) + ks * (C::KS * 2) + off[i]);
             if (RAGGED && ks == KT - 1) staged[i] = load_part<8>(p, a.K - ks * C::KS - ((j & 1) ? ld_c ^ 4 : ld_c) * 8, a.K);
@@ -778,17 +785,11 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a, X 
     const auto advance = [&]() __attribute__((always_inline)) {
         if (ki == steps) {
             more = tile_at(it + 1, next_m0, next_n0);
-            if (more) aim(next_m0, next_n0);     // the last tile's loads go round to its own first K steps, and are not used
+            if (more || X::on) aim(next_m0, next_n0);   // the last tile's loads go round to its own first K steps, and are not used
             ki = 0;
         }
         if constexpr (X::on)
-            if (ki >= KT) {
-                const int per = x.width / C::KS, at = ki - KT, i = at / per;
-                ad = tile[i];
-                c0 = (at - i * per) * 8;
-                at_rank[0] = rank_of_chunk(x, c0 + ld_c);
-                at_rank[1] = rank_of_chunk(x, c0 + (ld_c ^ 4));
-            }
+            if (ki >= KT) aim_adapter(ki);
     };
 #pragma unroll
     for (int st = 0; st < SLOTS - 1; ++st) {

@@ -114,11 +114,11 @@ struct Product {
     }
 };
 
-// bf16 numbers that stand for one of x A^T, and what the workspace holds: of every row its own, then the lists of the row tiles, which are 16 rows at least and
-// hold a number more than rows
+// bf16 numbers that stand for one of x A^T, and what the workspace holds: of every row its own, then the lists of the row tiles (adapter_list), of 16 to 256 rows: (R / t + 1)
+// (1 + t (1 + t / 32)) numbers are at most those of t = 256 and one more for 16 rows
 int parts_of(const moe_ep_linear_config& c) { return c.out_type == MOE_EP_F32 ? 3 : 2; }
-size_t low_bytes(const moe_ep_linear_config& c, const moe_ep_adapter_config& ad, int32_t n_rows) { return (size_t)n_rows * adapter_width(ad.rank, parts_of(c)) * 2; }
-size_t lists_bytes(int32_t n_rows) { return ((size_t)n_rows + n_rows / 16 + 272) * 4; }
+size_t low_bytes(const moe_ep_linear_config& c, const moe_ep_adapter_config& ad, int32_t n_rows) { return (size_t)n_rows * adapter_pitch(adapter_width(ad.rank, parts_of(c))) * 2; }
+size_t lists_bytes(int32_t n_rows) { return ((size_t)n_rows * 9 + n_rows / 16 + adapter_list(256) + 1) * 4; }
 
 }  // namespace
 
