@@ -1,0 +1,89 @@
+// Adapters of up to kGathered rows, a decode step of many requests: the product and x A_a^T in one launch, x A_a^T B_a^T and the epilogue in another.  The rows of such a
+// batch have their adapters in no order, so that a tile of the product would meet most of them; groups of rows of one adapter meet one.
+#include "linear_kernels.h"
+
+namespace moe_ep {
+
+namespace {
+
+// A wavefront has a group of up to 16 rows and NB * 16 columns: x W^T of them, as the product left it, and the product of their x A^T (as `parts` bf16 numbers) with B, straight
+// from memory in the order that the matrix instruction wants: 64 bytes of a row, 16 rows at a time.
+template <int NB>
+__global__ __launch_bounds__(256) void adapters_up_kernel(LinearArgs a, AdapterArgs x, const float* wide, const int32_t* table, int slices)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = blockIdx.x / slices;
+    const int n0 = ((int)(blockIdx.x % slices) * 4 + wave) * (NB * 16);
+    const int32_t* const entry = table + group * kGroupEntry;
+    const int adapter = entry[0], row = lane & 15, kh = lane >> 4, m = entry[1 + row];
+    if (adapter < -1 || n0 >= a.N) return;
+    const Epilogue<NB> e(a, n0, kh);
+    typename Epilogue<NB>::Residual res;
+    const bool there = m >= 0;
+    if (a.residual && there) e.fetch(m, res);
+    f32x4_t v[NB];
+    const float* const from = wide + (size_t)(there ? m : 0) * a.N + n0 + kh * 4;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        v[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if (e.group(b)) v[b] = *reinterpret_cast<const f32x4_any4*>(from + b * 16);
+        else
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (n0 + kh * 4 + b * 16 + i < a.N) v[b][i] = from[b * 16 + i];
+    }
+    if (adapter >= 0) {
+        const uint16_t* const low = x.low + (size_t)(there ? m : 0) * adapter_pitch(x.width);
+        const uint16_t* const up = x.up + (size_t)adapter * a.N * x.rank;
+        const int chunks = x.parts * (x.rank >> 3);
+#pragma unroll 2
+        for (int c = kh; c - kh < chunks; c += 4) {
+            const int k = rank_of_chunk(x, c);
+            u32x4_t l = {0, 0, 0, 0}, u[NB];
+            if (k >= 0 && there) l = *reinterpret_cast<const u32x4_t*>(low + c * 8);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                u[b] = u32x4_t{0, 0, 0, 0};
+                if (k >= 0) u[b] = *reinterpret_cast<const u32x4_t*>(up + (size_t)min(n0 + b * 16 + row, a.N - 1) * x.rank + k);
+            }
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+                v[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, u[b]), __builtin_bit_cast(bf16x8_t, l), v[b], 0, 0, 0);
+        }
+    }
+    e.store(m, there, v, res);
+}
+
+template <int NB>
+hipError_t launch_up(const LinearArgs& a, const AdapterArgs& x, const float* wide, const int32_t* table, int groups, hipStream_t s)
+{
+    const long long slices = ((long long)a.N + NB * 64 - 1) / (NB * 64), grid = groups * slices;
+    if (grid > 0x7fffffffll / 256) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((adapters_up_kernel<NB>), dim3((unsigned)grid), dim3(256), 0, s, a, x, wide, table, (int)slices);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_linear_grouped(const LinearArgs& a, const AdapterArgs& x, float* wide, int32_t* table, int n_cu, hipStream_t s)
+{
+    if (a.R <= 0) return hipSuccess;
+    if (a.R > kGathered || a.N < 1 || a.K < 1 || a.w32 || x.n < 1 || x.rank < 8 || x.rank > kRankMost || x.rank % 8) return hipErrorInvalidValue;
+    LinearArgs product = a;
+    product.out = wide;
+    product.ldo = a.N;
+    product.out32 = true;
+    product.bias = nullptr;
+    product.residual = nullptr;
+    product.act = kActNone;
+    GroupArgs g{};
+    g.adapters = x;
+    g.table = table;
+    g.groups = adapter_groups(a.R, x.n);
+    const int blocks = (x.rank + 15) / 16;
+    g.shares = blocks;
+    g.workgroups = (g.groups * g.shares + 7) / 8 * 8;
+    const hipError_t e = launch_chosen(linear_kernel(product, n_cu), product, g, n_cu, s);
+    return e == hipSuccess ? launch_up<2>(a, x, wide, table, g.groups, s) : e;
+}
+
+}  // namespace moe_ep

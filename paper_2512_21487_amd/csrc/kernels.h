@@ -246,9 +246,9 @@ int linear_kernel(const LinearArgs& a, int n_cu);
 hipError_t launch_linear(const LinearArgs& a, int n_cu, hipStream_t s);
 
 // ---- the same product with low-rank adapters (adapters.hip, and the product's kernels): act(x W^T + bias + scale_a (x A_a^T) B_a^T) + residual
-struct NoAdapters { static constexpr bool on = false; };
+struct NoAdapters { static constexpr bool on = false, beside = false; };
 struct AdapterArgs {
-    static constexpr bool on = true;
+    static constexpr bool on = true, beside = false;   // the product's reduction goes on with B
     const int32_t* index;               // of every row; one that is not in 0..n-1: none
     const uint16_t *down, *up;          // A [n, rank, K], B [n, N, rank]
     const float* scale;                 // [n] or NULL
@@ -263,8 +263,20 @@ __host__ __device__ constexpr int adapter_pitch(int width) { return width + 8; }
 __host__ __device__ constexpr int adapter_list(int tile) { return 1 + tile * (1 + (tile + 31) / 32); }
 constexpr int kRankMost = 128;
 int linear_tile_rows(int kernel);       // of what linear_kernel chose; 0: no tiles
+// Few rows, of many adapters maybe: the product's launch leaves x W^T in fp32, and other workgroups of it make `low`, of groups of up to 16 rows of one adapter (or of none); another
+// launch adds the groups' low B_a^T and has the epilogue.
+constexpr int kGathered = 512, kGroupEntry = 1 + 16;
+struct GroupArgs {
+    static constexpr bool on = false, beside = true;
+    AdapterArgs adapters;
+    int32_t* table;                     // workspace: of every group its adapter (-1: none; -2: no group) and its rows (-1: none)
+    int groups, shares, workgroups;     // groups there may be; workgroups that share one's ranks; of all, a multiple of the XCDs
+};
+inline int adapter_groups(int R, int n) { return R / 16 + (n + 1 < R ? n + 1 : R); }   // full ones, and one that is not for every adapter and for none
+constexpr int adapter_kernel(int linear) { return linear < kLinearTiled ? kLinearSplit16x16 : linear; }   // whose reduction can go on
 hipError_t launch_adapters_down(const LinearArgs& a, const AdapterArgs& x, int n_cu, hipStream_t s);
 hipError_t launch_linear_adapters(const LinearArgs& a, const AdapterArgs& x, int n_cu, hipStream_t s);
+hipError_t launch_linear_grouped(const LinearArgs& a, const AdapterArgs& x, float* wide, int32_t* table, int n_cu, hipStream_t s);
 
 // ---- norms around a block (norm.hip): the public struct's fields as the kernels read them
 enum { kNormNone = 0, kNormRms, kNormLayer, kNormCount };

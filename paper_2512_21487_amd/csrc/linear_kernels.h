@@ -216,6 +216,192 @@ hipError_t allow_lds(K* kernel, int bytes, std::atomic<uint64_t>& told)
     return e;
 }
 
+// What a wavefront that takes K steps of MB x NB blocks of 16 rows x 16 columns has in LDS
+template <int MB, int NB, bool W32>
+struct SplitCfg {
+    static constexpr int KS = 64, WROW = W32 ? 256 : 128;                    // bytes of a row of weights
+    static constexpr int XL = MB * 2, WL = NB * 16 * WROW / 1024;             // loads of 1 KB
+    static constexpr int X_BYTES = MB * 16 * 128, W_BYTES = NB * 16 * WROW, BYTES = X_BYTES + W_BYTES;
+    static_assert(MB * NB * 1024 <= BYTES, "the sums take the place of the operands");
+};
+
+// ---- rows times A: what adapters' workgroups do in front of a product's
+
+// the upper halves of two words, of `a` in the low half
+__device__ __forceinline__ uint32_t upper_halves(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
+
+// A wavefront's 16 rows x 16 ranks of sums: a lane has 4 consecutive ranks of its row, r the first.  They are written as `parts` bf16 numbers each, 8 bits cut off the top at a
+// time and the last rounded: two leave 2^-17 of the sum, which is 2^-8 of what rounding the result to bf16 leaves, three 2^-25 (results in fp32).
+__device__ __forceinline__ void store_low(const AdapterArgs& x, long long row, int r, f32x4_t v)
+{
+    uint16_t* const to = x.low + row * adapter_pitch(x.width) + r;
+    for (int p = 0; p < x.parts; ++p) {
+        u32x2_t u;
+        if (p + 1 == x.parts) u = u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+        else {
+            u = u32x2_t{upper_halves(v[0], v[1]), upper_halves(v[2], v[3])};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] -= __uint_as_float(__float_as_uint(v[i]) & 0xffff0000u);
+        }
+        *reinterpret_cast<u32x2_t*>(to + p * x.rank) = u;
+    }
+}
+
+// x A_a^T of up to MB * 16 rows, which `row_of` names (-1: none), and NB * 16 ranks from r0 on.  The wavefronts take K steps of 64 in turn, as in linear_split_kernel, DEPTH of
+// them on their way in registers; their sums are added up in LDS, in the order of the wavefronts.
+template <int MB, int NB, int WAVES, int DEPTH, class Rows>
+__device__ __forceinline__ void down(const LinearArgs& a, const AdapterArgs& x, uint4* lds4, int lane, int wave, int adapter, int r0, long long first,
+                                     const Rows& row_of)
+{
+    using C = SplitCfg<MB, NB, false>;
+    constexpr int KS = C::KS;
+    char* const own = reinterpret_cast<char*>(lds4) + wave * C::BYTES;
+    const int xr = lane >> 3, xc = lane & 7, row = lane & 15, kh = lane >> 4, sw = (row >> 1) & 7;
+    // in place of a row that is not there the first one, of a rank the last: what comes of them is not stored
+    const uint16_t *xp[C::XL], *wp[C::WL];
+#pragma unroll
+    for (int i = 0; i < C::XL; ++i) {
+        const long long m = row_of(i * 8 + xr);
+        xp[i] = a.x + (m < 0 ? first : m) * a.ldx + xc * 8;
+    }
+#pragma unroll
+    for (int i = 0; i < C::WL; ++i) wp[i] = x.down + ((size_t)adapter * x.rank + min(r0 + i * 8 + xr, x.rank - 1)) * a.K + xc * 8;
+    struct Step { u32x4_t x[C::XL], w[C::WL]; } f[DEPTH];
+    const int steps = (a.K + KS - 1) / KS, whole = a.K / KS;
+    const auto load = [&](Step& to, int step) __attribute__((always_inline)) {
+        if (step < whole) {
+#pragma unroll
+            for (int i = 0; i < C::WL; ++i) to.w[i] = *reinterpret_cast<const u32x4_any2*>(wp[i] + step * KS);
+#pragma unroll
+            for (int i = 0; i < C::XL; ++i) to.x[i] = *reinterpret_cast<const u32x4_any2*>(xp[i] + step * KS);
+            return;
+        }
+        const int left = a.K - step * KS - xc * 8;
+#pragma unroll
+        for (int i = 0; i < C::WL; ++i) to.w[i] = load_part<8>(wp[i] + step * KS, left, a.K);
+#pragma unroll
+        for (int i = 0; i < C::XL; ++i) to.x[i] = load_part<8>(xp[i] + step * KS, left, a.K);
+    };
+    f32x4_t acc[MB][NB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d)
+        if (wave + d * WAVES < steps) load(f[d], wave + d * WAVES);
+    for (int st = wave; st < steps; st += WAVES * DEPTH) {
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            if (st + d * WAVES >= steps) break;
+#pragma unroll
+            for (int i = 0; i < C::WL; ++i) *reinterpret_cast<u32x4_t*>(own + C::X_BYTES + xr * 128 + i * 1024 + (xc ^ (((i * 8 + xr) >> 1) & 7)) * 16) = f[d].w[i];
+#pragma unroll
+            for (int i = 0; i < C::XL; ++i) *reinterpret_cast<u32x4_t*>(own + xr * 128 + i * 1024 + (xc ^ (((i * 8 + xr) >> 1) & 7)) * 16) = f[d].x[i];
+            wavefront_lds_order();
+            if (st + (d + DEPTH) * WAVES < steps) load(f[d], st + (d + DEPTH) * WAVES);
+            SB();   // or the compiler moves loads behind the products
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                bf16x8_t xs[MB];
+#pragma unroll
+                for (int i = 0; i < MB; ++i) xs[i] = *reinterpret_cast<const bf16x8_t*>(own + (i * 16 + row) * 128 + ((h * 4 + kh) ^ sw) * 16);
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    const bf16x8_t w = *reinterpret_cast<const bf16x8_t*>(own + C::X_BYTES + (j * 16 + row) * 128 + ((h * 4 + kh) ^ sw) * 16);
+#pragma unroll
+                    for (int i = 0; i < MB; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, xs[i], acc[i][j], 0, 0, 0);
+                }
+            }
+            wavefront_lds_order();
+        }
+    }
+    // a wavefront's operands make room for its sums
+    f32x4_t* const sums = reinterpret_cast<f32x4_t*>(own) + lane;
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) sums[(i * NB + j) * 64] = acc[i][j];
+    __syncthreads();
+    const float scale = x.scale ? x.scale[adapter] : 1.0f;
+    for (int ij = wave; ij < MB * NB; ij += WAVES) {
+        const f32x4_t* const from = reinterpret_cast<const f32x4_t*>(lds4) + ij * 64 + lane;
+        f32x4_t v = from[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) v += from[w * (C::BYTES / 16)];
+        const int r = r0 + ij % NB * 16 + kh * 4;
+        const long long m = row_of(ij / NB * 16 + row);
+        if (m >= 0 && r < x.rank) store_low(x, m, r, v * scale);
+    }
+    __syncthreads();
+}
+
+// Up to kGathered rows in any order, in groups: an adapter's rows, and those without one, are taken 16 at a time.  Of every row a thread counts those in front of it with the same
+// adapter; each row whose count is a multiple of 16 begins a group, and a workgroup has the group of its number and some of its ranks.  So A is read once for 16 of its rows, and
+// however many rows have the same adapter, no workgroup has more to do than another.  The workgroup of a group's first ranks writes down its rows.
+template <int WAVES, int DEPTH>
+__device__ __forceinline__ void down_group(const LinearArgs& a, const GroupArgs& g, uint4* lds4, int number)
+{
+    const AdapterArgs& x = g.adapters;
+    __shared__ int s_rows[16];
+    __shared__ unsigned long long s_begin[kGathered / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int group = number / g.shares, share = number % g.shares;
+    if (group >= g.groups) return;
+    int* const all = reinterpret_cast<int*>(lds4);
+    int* const in_front = all + kGathered;
+    for (int row = tid; row < kGathered; row += WAVES * 64) all[row] = row < a.R ? adapter_of(x, row) : -2;
+    if (tid < 16) s_rows[tid] = -1;
+    __syncthreads();
+#pragma unroll 1
+    for (int row = tid; row < kGathered; row += WAVES * 64) {
+        const int mine = all[row];
+        int n = 0;
+        if ((row & ~63) < a.R)                               // whole wavefronts
+            for (int i = 0; i < a.R; i += 4) {
+                const int4 other = *reinterpret_cast<const int4*>(all + i);
+                n += (other.x == mine && i < row) + (other.y == mine && i + 1 < row) + (other.z == mine && i + 2 < row) + (other.w == mine && i + 3 < row);
+            }
+        in_front[row] = n;
+        const unsigned long long begin = __ballot(mine > -2 && n % 16 == 0);
+        if (lane == 0) s_begin[row >> 6] = begin;
+    }
+    __syncthreads();
+    int left = group, begin = -1;
+#pragma unroll
+    for (int w = 0; w < kGathered / 64; ++w) {
+        unsigned long long bits = s_begin[w];
+        const int n = __popcll(bits);
+        if (begin < 0 && left < n) {
+            for (; left > 0; --left) bits &= bits - 1;
+            begin = w * 64 + __builtin_ctzll(bits);
+        }
+        left -= n;
+    }
+    begin = __builtin_amdgcn_readfirstlane(begin);
+    int32_t* const entry = g.table + group * kGroupEntry;
+    if (begin < 0) {
+        if (share == 0 && tid == 0) entry[0] = -2;
+        return;
+    }
+    const int adapter = __builtin_amdgcn_readfirstlane(all[begin]), from = in_front[begin];
+    for (int row = tid; row < a.R; row += WAVES * 64)
+        if (all[row] == adapter && in_front[row] >= from && in_front[row] < from + 16) s_rows[in_front[row] - from] = row;
+    __syncthreads();
+    if (share == 0 && tid < kGroupEntry) entry[tid] = tid == 0 ? adapter : s_rows[tid - 1];
+    if (adapter < 0) return;
+    for (int r0 = share * 16; r0 < x.rank; r0 += g.shares * 16)
+        down<1, 1, WAVES, DEPTH>(a, x, lds4, lane, wave, adapter, r0, begin, [&](int i) { return (long long)s_rows[i]; });
+}
+
+// how many workgroups of a launch are in front of the product's
+template <class X>
+__host__ __device__ __forceinline__ int in_front_of(const X& x)
+{
+    if constexpr (X::beside) return x.workgroups;
+    else return 0;
+}
+
 // ---- a few rows: no matrix instruction is full
 
 // A workgroup has C columns and up to RB rows: its threads take 8 elements of the reduction in turn, which reads the weights in whole
@@ -225,8 +411,15 @@ template <int RB, int C, bool W32, class X>
 __global__ __launch_bounds__(256) void linear_rows_kernel(LinearArgs a, X x)
 {
     __shared__ float s_sum[4][C * RB];
+    static_assert(!X::on, "no more of a reduction");
+    if constexpr (X::beside)
+        if ((int)blockIdx.x < x.workgroups) {
+            extern __shared__ uint4 lds4[];
+            down_group<4, 4>(a, x, lds4, blockIdx.x);
+            return;
+        }
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int nt = (a.N + C - 1) / C, n0 = (int)(blockIdx.x % nt) * C, m0 = (int)(blockIdx.x / nt) * RB;
+    const int at = (int)blockIdx.x - in_front_of(x), nt = (a.N + C - 1) / C, n0 = at % nt * C, m0 = at / nt * RB;
     float acc[C][RB];
 #pragma unroll
     for (int c = 0; c < C; ++c)
@@ -257,28 +450,6 @@ __global__ __launch_bounds__(256) void linear_rows_kernel(LinearArgs a, X x)
                 for (int i = 0; i < 8; ++i) acc[c][r] = fmaf(f[i], (i & 1) ? bf16_hi(xs[r][i >> 1]) : bf16_lo(xs[r][i >> 1]), acc[c][r]);
         }
     }
-    if constexpr (X::on) {
-        // 16 lanes have a row's adapter, 8 of its rank each
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            if (tid >> 4 != r || (tid & 15) * 8 >= x.rank || m0 + r >= a.R) continue;
-            const int ad = adapter_of(x, m0 + r), j = (tid & 15) * 8;
-            if (ad < 0) continue;
-            const uint16_t* const low = x.low + (size_t)(m0 + r) * adapter_pitch(x.width) + j;
-            float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            for (int p = x.parts - 1; p >= 0; --p) {          // the smallest first
-                const u32x4_t u = *reinterpret_cast<const u32x4_t*>(low + p * x.rank);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] += (i & 1) ? bf16_hi(u[i >> 1]) : bf16_lo(u[i >> 1]);
-            }
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                const u32x4_t u = *reinterpret_cast<const u32x4_t*>(x.up + ((size_t)ad * a.N + min(n0 + c, a.N - 1)) * x.rank + j);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) acc[c][r] = fmaf((i & 1) ? bf16_hi(u[i >> 1]) : bf16_lo(u[i >> 1]), v[i], acc[c][r]);
-            }
-        }
-    }
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -306,21 +477,19 @@ __global__ __launch_bounds__(256) void linear_rows_kernel(LinearArgs a, X x)
 template <int RB, int C, class X>
 hipError_t launch_rows(const LinearArgs& a, const X& x, hipStream_t s)
 {
-    const long long grid = (long long)((a.N + C - 1) / C) * ((a.R + RB - 1) / RB);
+    const long long grid = (long long)((a.N + C - 1) / C) * ((a.R + RB - 1) / RB) + in_front_of(x);
     if (grid > 0x7fffffffll) return hipErrorInvalidValue;
-    if constexpr (!X::on)
+    if constexpr (!X::beside)
         if (a.w32) {
             hipLaunchKernelGGL((linear_rows_kernel<RB, C, true, X>), dim3((unsigned)grid), dim3(256), 0, s, a, x);
             return hipGetLastError();
         }
-    hipLaunchKernelGGL((linear_rows_kernel<RB, C, false, X>), dim3((unsigned)grid), dim3(256), 0, s, a, x);
+    constexpr int bytes = X::beside ? 4 * SplitCfg<1, 1, false>::BYTES : 0;
+    hipLaunchKernelGGL((linear_rows_kernel<RB, C, false, X>), dim3((unsigned)grid), dim3(256), bytes, s, a, x);
     return hipGetLastError();
 }
 
 // ---- some rows, weights in fp32, or operands that are not on 16 bytes
-
-// the upper halves of two words, of `a` in the low half
-__device__ __forceinline__ uint32_t upper_halves(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
 
 // 8 fp32 numbers as the sum of three times 8 bf16 numbers
 __device__ __forceinline__ void split3(const f32x8_t& w, bf16x8_t part[3])
@@ -341,14 +510,6 @@ __device__ __forceinline__ void split3(const f32x8_t& w, bf16x8_t part[3])
 // those lanes, 16 rows' bytes at a time, a load took the memory path four times as long (4096 x 128 x 4096, fp32 weights: 33 us against 22).
 // Those 22 us are 1.6 TB/s of operands; the matrix unit is busy 16 % of them.  What bounds it is a step's chain in each wavefront, LDS write, read,
 // cutting the weights up, products, with only two wavefronts per SIMD to fill one another's gaps (eight slices of 16 KB are most of the LDS).
-template <int MB, int NB, bool W32>
-struct SplitCfg {
-    static constexpr int KS = 64, WROW = W32 ? 256 : 128;                    // bytes of a row of weights
-    static constexpr int XL = MB * 2, WL = NB * 16 * WROW / 1024;             // loads of 1 KB
-    static constexpr int X_BYTES = MB * 16 * 128, W_BYTES = NB * 16 * WROW, BYTES = X_BYTES + W_BYTES;
-    static_assert(MB * NB * 1024 <= BYTES, "the sums take the place of the operands");
-};
-
 template <int MB, int NB, int WAVES, bool W32, class X>
 __global__ __launch_bounds__(WAVES * 64) void linear_split_kernel(LinearArgs a, X x)
 {
@@ -359,7 +520,12 @@ __global__ __launch_bounds__(WAVES * 64) void linear_split_kernel(LinearArgs a, 
     char* const own = reinterpret_cast<char*>(lds4) + wave * C::BYTES;
     // tiles of one XCD (workgroup number mod 8) are consecutive ones
     const int mt = (a.R + MB * 16 - 1) / (MB * 16), nt = (a.N + NB * 16 - 1) / (NB * 16);
-    const long long total = (long long)mt * nt, per = (total + 7) / 8, at = workgroup(), L = (at & 7) * per + (at >> 3);
+    if constexpr (X::beside)
+        if (workgroup() < x.workgroups) {
+            down_group<WAVES, WAVES == 16 ? 2 : 4>(a, x, lds4, (int)workgroup());
+            return;
+        }
+    const long long total = (long long)mt * nt, per = (total + 7) / 8, at = workgroup() - in_front_of(x), L = (at & 7) * per + (at >> 3);
     if ((at >> 3) >= per || L >= total) return;
     const int m0 = (int)(a.rows_first ? L % mt : L / nt) * (MB * 16), n0 = (int)(a.rows_first ? L / mt : L % nt) * (NB * 16);
 
@@ -501,7 +667,7 @@ hipError_t launch_split_as(const LinearArgs& a, const X& x, long long workgroups
     static std::atomic<uint64_t> told{0};
     const hipError_t e = allow_lds(&linear_split_kernel<MB, NB, WAVES, W32, X>, bytes, told);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((linear_split_kernel<MB, NB, WAVES, W32, X>), grid_of(workgroups), dim3(WAVES * 64), bytes, s, a, x);
+    hipLaunchKernelGGL((linear_split_kernel<MB, NB, WAVES, W32, X>), grid_of(workgroups + in_front_of(x)), dim3(WAVES * 64), bytes, s, a, x);
     return hipGetLastError();
 }
 
@@ -511,7 +677,7 @@ hipError_t launch_split(LinearArgs a, const X& x, hipStream_t s)
     const long long mt = (a.R + MB * 16 - 1) / (MB * 16), nt = (a.N + NB * 16 - 1) / (NB * 16), per = (mt * nt + 7) / 8;
     // an XCD's tiles share the rows of the larger operand through its L2
     a.rows_first = (double)a.N * a.K * (a.w32 ? 4 : 2) > (double)a.R * a.K * 2;
-    if constexpr (!X::on)
+    if constexpr (!X::on && !X::beside)
         if (a.w32) return launch_split_as<MB, NB, WAVES, true>(a, x, per * 8, s);
     return launch_split_as<MB, NB, WAVES, false>(a, x, per * 8, s);
 }
@@ -674,8 +840,13 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a, X 
     char* const lds = reinterpret_cast<char*>(lds4);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1;
     const int mt = (a.R + BM - 1) / BM, nt = (a.N + BN - 1) / BN, total = mt * nt, KT = (a.K + C::KS - 1) / C::KS;
+    if constexpr (X::beside)
+        if ((int)blockIdx.x < x.workgroups) {
+            down_group<4, 4>(a, x, lds4, blockIdx.x);
+            return;
+        }
     // workgroup b runs on XCD b mod 8: an XCD's tiles are consecutive ones, in bands of 8 row tiles, inside a band row tiles first
-    const int per = gridDim.x >> 3, xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
+    const int at = (int)blockIdx.x - in_front_of(x), per = ((int)gridDim.x - in_front_of(x)) >> 3, xcd = at & 7, slot = at >> 3;
     const auto tile_at = [&](int it, int& m0, int& n0) -> bool {
         const int L = (it * 8 + xcd) * per + slot;
         if (L >= total) return false;
@@ -877,7 +1048,7 @@ hipError_t launch_tiled_as(const LinearArgs& a, const X& x, int n_cu, hipStream_
     if (total > 0x3fffffffll) return hipErrorInvalidValue;
     // as few workgroups as it takes for as many rounds, the same number on every XCD
     const long long wgs = (long long)n_cu * OCC, rounds = (total + wgs - 1) / wgs;
-    const int grid = (int)(((total + rounds - 1) / rounds + 7) / 8 * 8);
+    const int grid = (int)(((total + rounds - 1) / rounds + 7) / 8 * 8) + in_front_of(x);
     hipLaunchKernelGGL((linear_tiled_kernel<BM, BN, SLOTS, OCC, RAGGED, ACT, STAGED, X>), dim3(grid), dim3(256), C::LDS_BYTES, s, a, x);
     return hipGetLastError();
 }
@@ -888,19 +1059,24 @@ hipError_t launch_tiled(const LinearArgs& a, const X& x, int n_cu, hipStream_t s
     // (staged: K is seldom whole)
     if constexpr (!STAGED) {
         if (a.act == kActNone && a.K % 64 == 0) return launch_tiled_as<BM, BN, SLOTS, OCC, false, false, false>(a, x, n_cu, s);
-        if (a.K % 64 == 0) return launch_tiled_as<BM, BN, SLOTS, OCC, false, true, false>(a, x, n_cu, s);
+        if constexpr (!X::beside)
+            if (a.K % 64 == 0) return launch_tiled_as<BM, BN, SLOTS, OCC, false, true, false>(a, x, n_cu, s);
     }
-    return a.act == kActNone ? launch_tiled_as<BM, BN, SLOTS, OCC, true, false, STAGED>(a, x, n_cu, s) : launch_tiled_as<BM, BN, SLOTS, OCC, true, true, STAGED>(a, x, n_cu, s);
+    if constexpr (!X::beside)
+        if (a.act != kActNone) return launch_tiled_as<BM, BN, SLOTS, OCC, true, true, STAGED>(a, x, n_cu, s);
+    return a.act == kActNone ? launch_tiled_as<BM, BN, SLOTS, OCC, true, false, STAGED>(a, x, n_cu, s) : hipErrorInvalidValue;
 }
 
 // a kernel that linear_kernel chose
 template <class X>
 hipError_t launch_chosen(int kernel, const LinearArgs& a, const X& x, int n_cu, hipStream_t s)
 {
+    if constexpr (!X::on) {
+        if (kernel == kLinearRows1x1) return launch_rows<1, 1>(a, x, s);
+        if (kernel == kLinearRows4x1) return launch_rows<4, 1>(a, x, s);
+        if (kernel == kLinearRows4x2) return launch_rows<4, 2>(a, x, s);
+    }
     switch (kernel) {
-    case kLinearRows1x1: return launch_rows<1, 1>(a, x, s);
-    case kLinearRows4x1: return launch_rows<4, 1>(a, x, s);
-    case kLinearRows4x2: return launch_rows<4, 2>(a, x, s);
     case kLinearTiled + 0: return launch_tiled<256, 256, 2, 1, false>(a, x, n_cu, s);
     case kLinearTiled + 1: return launch_tiled<256, 192, 2, 1, false>(a, x, n_cu, s);
     case kLinearTiled + 2: return launch_tiled<192, 256, 2, 1, false>(a, x, n_cu, s);

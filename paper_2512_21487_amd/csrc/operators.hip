@@ -114,11 +114,23 @@ struct Product {
     }
 };
 
-// bf16 numbers that stand for one of x A^T, and what the workspace holds: of every row its own, then the lists of the row tiles (adapter_list), of 16 to 256 rows: (R / t + 1)
-// (1 + t (1 + t / 32)) numbers are at most those of t = 256 and one more for 16 rows
+// bf16 numbers that stand for one of x A^T
 int parts_of(const moe_ep_linear_config& c) { return c.out_type == MOE_EP_F32 ? 3 : 2; }
-size_t low_bytes(const moe_ep_linear_config& c, const moe_ep_adapter_config& ad, int32_t n_rows) { return (size_t)n_rows * adapter_pitch(adapter_width(ad.rank, parts_of(c))) * 2; }
-size_t lists_bytes(int32_t n_rows) { return ((size_t)n_rows * 9 + n_rows / 16 + adapter_list(256) + 1) * 4; }
+
+// What the workspace holds: x A^T of every row; behind it, of up to kGathered rows, x W^T in fp32 and the groups' table, of more the lists of the row tiles, of 16 to 256 rows: (R / t + 1)
+// (1 + t (1 + t / 32)) numbers are at most those of t = 256 and one more for 16 rows.
+struct AdapterWorkspace {
+    size_t low, wide, table, lists;
+    AdapterWorkspace(const moe_ep_linear_config& c, const moe_ep_adapter_config& ad, int32_t n_rows)
+    {
+        const int few = n_rows < kGathered ? n_rows : kGathered;
+        low = (size_t)n_rows * adapter_pitch(adapter_width(ad.rank, parts_of(c))) * 2;
+        wide = ((size_t)few * c.out_features * 4 + 15) / 16 * 16;
+        table = (size_t)adapter_groups(few, ad.n_adapters) * kGroupEntry * 4;
+        lists = ((size_t)n_rows * 9 + n_rows / 16 + adapter_list(256) + 1) * 4;
+    }
+    size_t bytes() const { return low + (wide + table > lists ? wide + table : lists); }   // of more rows not fewer: that holds of each
+};
 
 }  // namespace
 
@@ -222,7 +234,7 @@ int moe_ep_validate_linear_adapters(const moe_ep_linear_config* c, const moe_ep_
 size_t moe_ep_linear_adapters_workspace_bytes(const moe_ep_linear_config* c, const moe_ep_adapter_config* ad, int32_t n_rows)
 {
     if (moe_ep_validate_linear_adapters(c, ad, nullptr) != MOE_EP_OK || n_rows < 1 || n_rows > kMostRows) return 0;
-    return low_bytes(*c, *ad, n_rows) + lists_bytes(n_rows);
+    return AdapterWorkspace(*c, *ad, n_rows).bytes();
 }
 
 int moe_ep_linear_adapters(const moe_ep_linear_config* c, const moe_ep_adapter_config* ad, const void* x, const void* weight, const float* bias,
@@ -263,10 +275,16 @@ int moe_ep_linear_adapters(const moe_ep_linear_config* c, const moe_ep_adapter_c
     AdapterArgs a{};
     a.index = index; a.down = static_cast<const uint16_t*>(down); a.up = static_cast<const uint16_t*>(up); a.scale = scale;
     a.low = static_cast<uint16_t*>(workspace);
-    a.lists = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + low_bytes(*c, *ad, n_rows));
     a.n = ad->n_adapters; a.rank = ad->rank; a.parts = parts_of(*c); a.width = adapter_width(a.rank, a.parts);
-    a.tile = linear_tile_rows(linear_kernel(p.args, n_cu));
-    e = launch_linear_adapters(p.args, a, n_cu, static_cast<hipStream_t>(stream));
+    const AdapterWorkspace parts(*c, *ad, n_rows);
+    char* const behind = static_cast<char*>(workspace) + parts.low;
+    if (n_rows <= kGathered)
+        e = launch_linear_grouped(p.args, a, reinterpret_cast<float*>(behind), reinterpret_cast<int32_t*>(behind + parts.wide), n_cu, static_cast<hipStream_t>(stream));
+    else {
+        a.lists = reinterpret_cast<int32_t*>(behind);
+        a.tile = linear_tile_rows(adapter_kernel(linear_kernel(p.args, n_cu)));
+        e = launch_linear_adapters(p.args, a, n_cu, static_cast<hipStream_t>(stream));
+    }
     return e == hipSuccess ? MOE_EP_OK : hip_failed(why, "launch", e);
 }
 
