@@ -2,7 +2,6 @@
 // Two launches.  The first makes scale_a x A_a^T of every row with an adapter, and for every row tile of the second the list of its rows' adapters.  The
 // second is the product's own kernel (linear_kernels.h), whose reduction goes on behind K with these products and B_a: the
 // wide result is neither written twice nor read again.
-#include <cstdlib>
 #include "linear_kernels.h"
 
 namespace moe_ep {
@@ -107,29 +106,15 @@ hipError_t launch_tiles(const LinearArgs& a, const AdapterArgs& x, int groups, h
 
 }  // namespace
 
-hipError_t launch_adapters_down(const LinearArgs& a, const AdapterArgs& x, int, hipStream_t s)
+// Tiles of few rows spread a few hundred of them over the compute units, tall ones read A less often.  16 rows x 16 ranks (a), two workgroups with 16 x 32 (b), two with 32 x 64 (c), 32 x
+// 64 (d), 64 x 64 (e, not kept): the whole call of R x 1024 x 4096, 16 prompts, us: rank 16, R 600 30 / 31 / 40 / - / -, 4096 49 / 56 / 55 / - / -, 16384 157 / - / 170 / 159 / 161; rank 64, 1024 34 / 32 /
+// 42 / - / -, 2048 51 / 51 / 47 / 50 / -, 4096 71 / - / 59 / 66 / -, 8192 - / - / 110 / 108 / 116, 16384 - / - / 186 / 170 / 167; rank 128, 4096 - / - / 77 / 71 / 85, 16384 - / - / 253 / 206 / 207.
+hipError_t launch_adapters_down(const LinearArgs& a, const AdapterArgs& x, hipStream_t s)
 {
-    if (const char* k = getenv("DOWN_K")) switch (atoi(k)) {
-    case 10: return launch_tiles<1, 1, 16, 1>(a, x, 16, s);
-    case 11: return launch_tiles<1, 1, 16, 2>(a, x, 1, s);
-    case 12: return launch_tiles<1, 2, 8, 2>(a, x, 1, s);
-    case 13: return launch_tiles<1, 4, 8, 2>(a, x, 1, s);
-    case 14: return launch_tiles<2, 2, 8, 2>(a, x, 1, s);
-    case 15: return launch_tiles<2, 4, 8, 1>(a, x, 1, s);
-    case 16: return launch_tiles<2, 4, 8, 2>(a, x, 1, s);
-    case 17: return launch_tiles<4, 4, 8, 1>(a, x, 1, s);
-    case 18: return launch_tiles<4, 2, 8, 2>(a, x, 1, s);
-    case 19: return launch_tiles<1, 2, 16, 2>(a, x, 1, s);
-    case 20: return launch_tiles<1, 4, 8, 2>(a, x, 2, s);
-    case 21: return launch_tiles<2, 4, 8, 2>(a, x, 2, s);
-    case 22: return launch_tiles<1, 2, 8, 4>(a, x, 2, s);
-    case 23: return launch_tiles<4, 4, 8, 1>(a, x, 2, s);
-    case 24: return launch_tiles<1, 2, 4, 4>(a, x, 2, s);
-    case 25: return launch_tiles<2, 2, 4, 4>(a, x, 2, s);
-    case 26: return launch_tiles<2, 4, 4, 2>(a, x, 2, s);
-    case 27: return launch_tiles<4, 4, 4, 1>(a, x, 2, s);
-    }
-    return launch_tiles<4, 4, 8, 1>(a, x, 1, s);
+    if (x.rank <= 16) return launch_tiles<1, 1, 16, 2>(a, x, 1, s);
+    if (a.R < 2048) return launch_tiles<1, 2, 8, 4>(a, x, 2, s);
+    if (a.R < 8192) return launch_tiles<2, 4, 8, 2>(a, x, 2, s);
+    return launch_tiles<2, 4, 8, 1>(a, x, 1, s);
 }
 
 hipError_t launch_linear_adapters(const LinearArgs& a, const AdapterArgs& x, int n_cu, hipStream_t s)
@@ -138,7 +123,7 @@ hipError_t launch_linear_adapters(const LinearArgs& a, const AdapterArgs& x, int
     if (a.N < 1 || a.K < 1 || a.w32 || x.n < 1 || x.rank < 8 || x.rank > kRankMost || x.rank % 8) return hipErrorInvalidValue;
     const int kernel = adapter_kernel(linear_kernel(a, n_cu));
     if (x.tile != linear_tile_rows(kernel)) return hipErrorInvalidValue;
-    const hipError_t e = launch_adapters_down(a, x, n_cu, s);
+    const hipError_t e = launch_adapters_down(a, x, s);
     return e == hipSuccess ? launch_chosen(kernel, a, x, n_cu, s) : e;
 }
 

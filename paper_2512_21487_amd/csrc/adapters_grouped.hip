@@ -34,20 +34,27 @@ __global__ __launch_bounds__(256) void adapters_up_kernel(LinearArgs a, AdapterA
     if (adapter >= 0) {
         const uint16_t* const low = x.low + (size_t)(there ? m : 0) * adapter_pitch(x.width);
         const uint16_t* const up = x.up + (size_t)adapter * a.N * x.rank;
-        const int chunks = x.parts * (x.rank >> 3);
-#pragma unroll 2
-        for (int c = kh; c - kh < chunks; c += 4) {
-            const int k = rank_of_chunk(x, c);
-            u32x4_t l = {0, 0, 0, 0}, u[NB];
-            if (k >= 0 && there) l = *reinterpret_cast<const u32x4_t*>(low + c * 8);
+#pragma unroll 4
+        for (int k = kh * 8; k - kh * 8 < x.rank; k += 32) {
+            const bool in = k < x.rank;
+            u32x4_t u[NB], l[3];
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 u[b] = u32x4_t{0, 0, 0, 0};
-                if (k >= 0) u[b] = *reinterpret_cast<const u32x4_t*>(up + (size_t)min(n0 + b * 16 + row, a.N - 1) * x.rank + k);
+                if (in) u[b] = *reinterpret_cast<const u32x4_t*>(up + (size_t)min(n0 + b * 16 + row, a.N - 1) * x.rank + k);
             }
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
-                v[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, u[b]), __builtin_bit_cast(bf16x8_t, l), v[b], 0, 0, 0);
+            for (int p = 0; p < 3; ++p) {
+                l[p] = u32x4_t{0, 0, 0, 0};
+                if (in && there && p < x.parts) l[p] = *reinterpret_cast<const u32x4_t*>(low + p * x.rank + k);
+            }
+#pragma unroll
+            for (int p = 2; p >= 0; --p) {
+                if (p >= x.parts) continue;
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+                    v[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, u[b]), __builtin_bit_cast(bf16x8_t, l[p]), v[b], 0, 0, 0);
+            }
         }
     }
     e.store(m, there, v, res);
@@ -80,7 +87,8 @@ hipError_t launch_linear_grouped(const LinearArgs& a, const AdapterArgs& x, floa
     g.table = table;
     g.groups = adapter_groups(a.R, x.n);
     const int blocks = (x.rank + 15) / 16;
-    g.shares = blocks;
+    // two workgroups for a compute unit, beside the product's own (512 x 4096 x 4096, 400 adapters of rank 32, one / two / four 84 / 90 / 91 us, of rank 128 169 / 187 / 161)
+    g.shares = g.groups * blocks <= 2 * n_cu ? blocks : 2 * n_cu / g.groups > 1 ? 2 * n_cu / g.groups : 1;
     g.workgroups = (g.groups * g.shares + 7) / 8 * 8;
     const hipError_t e = launch_chosen(linear_kernel(product, n_cu), product, g, n_cu, s);
     return e == hipSuccess ? launch_up<2>(a, x, wide, table, g.groups, s) : e;

@@ -274,7 +274,7 @@ struct GroupArgs {
 };
 inline int adapter_groups(int R, int n) { return R / 16 + (n + 1 < R ? n + 1 : R); }   // full ones, and one that is not for every adapter and for none
 constexpr int adapter_kernel(int linear) { return linear < kLinearTiled ? kLinearSplit16x16 : linear; }   // whose reduction can go on
-hipError_t launch_adapters_down(const LinearArgs& a, const AdapterArgs& x, int n_cu, hipStream_t s);
+hipError_t launch_adapters_down(const LinearArgs& a, const AdapterArgs& x, hipStream_t s);
 hipError_t launch_linear_adapters(const LinearArgs& a, const AdapterArgs& x, int n_cu, hipStream_t s);
 hipError_t launch_linear_grouped(const LinearArgs& a, const AdapterArgs& x, float* wide, int32_t* table, int n_cu, hipStream_t s);
 

@@ -350,21 +350,37 @@ __device__ __forceinline__ void down_group(const LinearArgs& a, const GroupArgs&
     if (group >= g.groups) return;
     int* const all = reinterpret_cast<int*>(lds4);
     int* const in_front = all + kGathered;
-    for (int row = tid; row < kGathered; row += WAVES * 64) all[row] = row < a.R ? adapter_of(x, row) : -2;
     if (tid < 16) s_rows[tid] = -1;
-    __syncthreads();
+    // Every wavefront has all rows, 64 to a register, and counts for some 64 of them: of each adapter among these how many rows of the 64s in front have it.  (A thread that
+    // compares its row with all in front took 4 us for 512 rows.)
+    constexpr int WORDS = kGathered / 64;
+    int of[WORDS];
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) of[i] = i * 64 + lane < a.R ? adapter_of(x, i * 64 + lane) : -2;
+    static_assert(WAVES >= WORDS / 2, "a wavefront counts for 64 rows, or for 64 from the beginning and 64 from the end");
 #pragma unroll 1
-    for (int row = tid; row < kGathered; row += WAVES * 64) {
-        const int mine = all[row];
+    for (int own = wave; own < WORDS; own = WAVES < WORDS && own < WAVES ? WORDS - 1 - own : WORDS) {
+        const int row = own * 64 + lane, mine = row < a.R ? adapter_of(x, row) : -2;
         int n = 0;
-        if ((row & ~63) < a.R)                               // whole wavefronts
-            for (int i = 0; i < a.R; i += 4) {
-                const int4 other = *reinterpret_cast<const int4*>(all + i);
-                n += (other.x == mine && i < row) + (other.y == mine && i + 1 < row) + (other.z == mine && i + 2 < row) + (other.w == mine && i + 3 < row);
-            }
+        unsigned long long left = __ballot(mine > -2);
+#pragma unroll 1
+        while (left) {
+            const int adapter = __builtin_amdgcn_readlane(mine, __builtin_ctzll(left));
+            const unsigned long long who = __ballot(mine == adapter);
+            left &= ~who;
+            int before = 0;
+            if (own)
+#pragma unroll
+                for (int j = 0; j + 1 < WORDS; ++j) {
+                    const int there = __popcll(__ballot(of[j] == adapter));
+                    before += j < own ? there : 0;
+                }
+            n = mine == adapter ? before + __popcll(who & ((1ull << lane) - 1)) : n;
+        }
+        all[row] = mine;
         in_front[row] = n;
         const unsigned long long begin = __ballot(mine > -2 && n % 16 == 0);
-        if (lane == 0) s_begin[row >> 6] = begin;
+        if (lane == 0) s_begin[own] = begin;
     }
     __syncthreads();
     int left = group, begin = -1;
