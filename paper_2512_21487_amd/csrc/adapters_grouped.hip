@@ -90,7 +90,7 @@ hipError_t launch_linear_grouped(const LinearArgs& a, const AdapterArgs& x, floa
     // two workgroups for a compute unit, beside the product's own (512 x 4096 x 4096, 400 adapters of rank 32, one / two / four 84 / 90 / 91 us, of rank 128 169 / 187 / 161)
     g.shares = g.groups * blocks <= 2 * n_cu ? blocks : 2 * n_cu / g.groups > 1 ? 2 * n_cu / g.groups : 1;
     g.workgroups = (g.groups * g.shares + 7) / 8 * 8;
-    const hipError_t e = launch_chosen(linear_kernel(product, n_cu), product, g, n_cu, s);
+    const hipError_t e = launch_chosen(adapter_kernel(linear_kernel(product, n_cu)), product, g, n_cu, s);
     return e == hipSuccess ? launch_up<2>(a, x, wide, table, g.groups, s) : e;
 }
 

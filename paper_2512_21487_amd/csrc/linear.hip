@@ -89,7 +89,12 @@ hipError_t launch_linear(const LinearArgs& a, int n_cu, hipStream_t s)
 {
     if (a.R <= 0) return hipSuccess;
     if (a.N < 1 || a.K < 1) return hipErrorInvalidValue;
-    return launch_chosen(linear_kernel(a, n_cu), a, NoAdapters{}, n_cu, s);
+    switch (const int kernel = linear_kernel(a, n_cu)) {
+    case kLinearRows1x1: return launch_rows<1, 1>(a, s);
+    case kLinearRows4x1: return launch_rows<4, 1>(a, s);
+    case kLinearRows4x2: return launch_rows<4, 2>(a, s);
+    default: return launch_chosen(kernel, a, NoAdapters{}, n_cu, s);
+    }
 }
 
 }  // namespace moe_ep

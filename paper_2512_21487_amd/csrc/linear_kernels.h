@@ -343,8 +343,8 @@ template <int WAVES, int DEPTH>
 __device__ __forceinline__ void down_group(const LinearArgs& a, const GroupArgs& g, uint4* lds4, int number)
 {
     const AdapterArgs& x = g.adapters;
-    __shared__ int s_rows[16];
-    __shared__ unsigned long long s_begin[kGathered / 64];
+    int* const s_rows = reinterpret_cast<int*>(reinterpret_cast<char*>(lds4) + WAVES * SplitCfg<1, 1, false>::BYTES);   // behind what down() takes
+    unsigned long long* const s_begin = reinterpret_cast<unsigned long long*>(s_rows + 16);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int group = number / g.shares, share = number % g.shares;
     if (group >= g.groups) return;
@@ -410,6 +410,9 @@ __device__ __forceinline__ void down_group(const LinearArgs& a, const GroupArgs&
         down<1, 1, WAVES, DEPTH>(a, x, lds4, lane, wave, adapter, r0, begin, [&](int i) { return (long long)s_rows[i]; });
 }
 
+constexpr int group_lds(int waves) { return waves * SplitCfg<1, 1, false>::BYTES + 16 * 4 + kGathered / 64 * 8; }
+static_assert(2 * kGathered * 4 <= 4 * SplitCfg<1, 1, false>::BYTES, "the rows' adapters and counts are where down()'s operands come");
+
 // how many workgroups of a launch are in front of the product's
 template <class X>
 __host__ __device__ __forceinline__ int in_front_of(const X& x)
@@ -423,19 +426,12 @@ __host__ __device__ __forceinline__ int in_front_of(const X& x)
 // A workgroup has C columns and up to RB rows: its threads take 8 elements of the reduction in turn, which reads the weights in whole
 // 4 or 8 KB, and their sums are added up through the wavefronts and LDS.  Latency bounds it: 1 x 160 x 5120 with fp32 weights 3.1 us (with 16
 // rows of a matrix instruction, 15 of them empty, 8.6), of which reading 3.3 MB is 0.6.
-template <int RB, int C, bool W32, class X>
-__global__ __launch_bounds__(256) void linear_rows_kernel(LinearArgs a, X x)
+template <int RB, int C, bool W32>
+__global__ __launch_bounds__(256) void linear_rows_kernel(LinearArgs a)
 {
     __shared__ float s_sum[4][C * RB];
-    static_assert(!X::on, "no more of a reduction");
-    if constexpr (X::beside)
-        if ((int)blockIdx.x < x.workgroups) {
-            extern __shared__ uint4 lds4[];
-            down_group<4, 4>(a, x, lds4, blockIdx.x);
-            return;
-        }
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int at = (int)blockIdx.x - in_front_of(x), nt = (a.N + C - 1) / C, n0 = at % nt * C, m0 = at / nt * RB;
+    const int nt = (a.N + C - 1) / C, n0 = (int)(blockIdx.x % nt) * C, m0 = (int)(blockIdx.x / nt) * RB;
     float acc[C][RB];
 #pragma unroll
     for (int c = 0; c < C; ++c)
@@ -447,11 +443,11 @@ __global__ __launch_bounds__(256) void linear_rows_kernel(LinearArgs a, X x)
     for (int k = tid * 8; k < a.K; k += 256 * 8) {
         const int left = a.K - k;
         Weight8 w[C];
-        u32x4_t xs[RB];
+        u32x4_t x[RB];
 #pragma unroll
         for (int c = 0; c < C; ++c) w[c] = load8(static_cast<const Weight*>(a.w) + (size_t)min(n0 + c, a.N - 1) * a.ldw + k, left);
 #pragma unroll
-        for (int r = 0; r < RB; ++r) xs[r] = load8(a.x + (size_t)min(m0 + r, a.R - 1) * a.ldx + k, left);
+        for (int r = 0; r < RB; ++r) x[r] = load8(a.x + (size_t)min(m0 + r, a.R - 1) * a.ldx + k, left);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             float f[8];
@@ -463,7 +459,7 @@ __global__ __launch_bounds__(256) void linear_rows_kernel(LinearArgs a, X x)
 #pragma unroll
             for (int r = 0; r < RB; ++r)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) acc[c][r] = fmaf(f[i], (i & 1) ? bf16_hi(xs[r][i >> 1]) : bf16_lo(xs[r][i >> 1]), acc[c][r]);
+                for (int i = 0; i < 8; ++i) acc[c][r] = fmaf(f[i], (i & 1) ? bf16_hi(x[r][i >> 1]) : bf16_lo(x[r][i >> 1]), acc[c][r]);
         }
     }
 #pragma unroll
@@ -490,18 +486,13 @@ __global__ __launch_bounds__(256) void linear_rows_kernel(LinearArgs a, X x)
     }
 }
 
-template <int RB, int C, class X>
-hipError_t launch_rows(const LinearArgs& a, const X& x, hipStream_t s)
+template <int RB, int C>
+hipError_t launch_rows(const LinearArgs& a, hipStream_t s)
 {
-    const long long grid = (long long)((a.N + C - 1) / C) * ((a.R + RB - 1) / RB) + in_front_of(x);
+    const long long grid = (long long)((a.N + C - 1) / C) * ((a.R + RB - 1) / RB);
     if (grid > 0x7fffffffll) return hipErrorInvalidValue;
-    if constexpr (!X::beside)
-        if (a.w32) {
-            hipLaunchKernelGGL((linear_rows_kernel<RB, C, true, X>), dim3((unsigned)grid), dim3(256), 0, s, a, x);
-            return hipGetLastError();
-        }
-    constexpr int bytes = X::beside ? 4 * SplitCfg<1, 1, false>::BYTES : 0;
-    hipLaunchKernelGGL((linear_rows_kernel<RB, C, false, X>), dim3((unsigned)grid), dim3(256), bytes, s, a, x);
+    if (a.w32) hipLaunchKernelGGL((linear_rows_kernel<RB, C, true>), dim3((unsigned)grid), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((linear_rows_kernel<RB, C, false>), dim3((unsigned)grid), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
@@ -678,7 +669,7 @@ __global__ __launch_bounds__(WAVES * 64) void linear_split_kernel(LinearArgs a, 
 template <int MB, int NB, int WAVES, bool W32, class X>
 hipError_t launch_split_as(const LinearArgs& a, const X& x, long long workgroups, hipStream_t s)
 {
-    constexpr int bytes = WAVES * SplitCfg<MB, NB, W32>::BYTES;
+    constexpr int own = WAVES * SplitCfg<MB, NB, W32>::BYTES, bytes = X::beside && group_lds(WAVES) > own ? group_lds(WAVES) : own;
     static_assert(bytes <= 160 * 1024, "LDS of a compute unit");
     static std::atomic<uint64_t> told{0};
     const hipError_t e = allow_lds(&linear_split_kernel<MB, NB, WAVES, W32, X>, bytes, told);
@@ -1056,7 +1047,7 @@ template <int BM, int BN, int SLOTS, int OCC, bool RAGGED, bool ACT, bool STAGED
 hipError_t launch_tiled_as(const LinearArgs& a, const X& x, int n_cu, hipStream_t s)
 {
     using C = TileCfg<BM, BN, SLOTS>;
-    static_assert(C::LDS_BYTES * OCC <= 160 * 1024, "LDS of a compute unit");
+    static_assert(C::LDS_BYTES * OCC <= 160 * 1024 && (!X::beside || group_lds(4) <= C::LDS_BYTES), "LDS of a compute unit");
     static std::atomic<uint64_t> told{0};
     const hipError_t e = allow_lds(&linear_tiled_kernel<BM, BN, SLOTS, OCC, RAGGED, ACT, STAGED, X>, C::LDS_BYTES, told);
     if (e != hipSuccess) return e;
@@ -1083,15 +1074,10 @@ hipError_t launch_tiled(const LinearArgs& a, const X& x, int n_cu, hipStream_t s
     return a.act == kActNone ? launch_tiled_as<BM, BN, SLOTS, OCC, true, false, STAGED>(a, x, n_cu, s) : hipErrorInvalidValue;
 }
 
-// a kernel that linear_kernel chose
+// a kernel that linear_kernel chose, but for dot products
 template <class X>
 hipError_t launch_chosen(int kernel, const LinearArgs& a, const X& x, int n_cu, hipStream_t s)
 {
-    if constexpr (!X::on) {
-        if (kernel == kLinearRows1x1) return launch_rows<1, 1>(a, x, s);
-        if (kernel == kLinearRows4x1) return launch_rows<4, 1>(a, x, s);
-        if (kernel == kLinearRows4x2) return launch_rows<4, 2>(a, x, s);
-    }
     switch (kernel) {
     case kLinearTiled + 0: return launch_tiled<256, 256, 2, 1, false>(a, x, n_cu, s);
     case kLinearTiled + 1: return launch_tiled<256, 192, 2, 1, false>(a, x, n_cu, s);

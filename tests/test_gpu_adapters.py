@@ -111,6 +111,34 @@ def test_every_kernel(name, R, N, K, pattern):
         c.check()
 
 
+# up to 512 rows are grouped, beside the product on each of its kernels
+GROUPED = {"rows 1x1": (5, 96, 200), "rows 4x2": (66, 16, 65), "split 16x16": (207, 151, 96), "split 32x16": (66, 707, 65), "split 64x16": (66, 1034, 65), "split 64x32": (65, 2051, 65),
+           "split 64x32 by 4": (66, 8294, 65), "staged 128x64": (130, 32886, 65), "staged 64x64": (65, 12304, 65), "tiles 128x128": (67, 32395, 576),
+           "tiles 192x256": (66, 2100, 72), "tiles 256x192": (193, 33747, 72), "tiles 256x256": (512, 24719, 128), "tiles 64x64": (300, 2046, 256)}
+
+
+@pytest.mark.parametrize("name", sorted(GROUPED))
+@pytest.mark.parametrize("pattern", ["random", "some", "own"])
+def test_grouped_beside_every_kernel(name, pattern):
+    R, N, K = GROUPED[name]
+    if torch.cuda.get_device_properties(0).multi_processor_count == 256:
+        assert kernel_of(R, N, K) == name
+    for n, out32 in ((7, False), (300, True)):
+        c = Adapted(R, N, K, 24, n, pattern, out32=out32, bias=True, residual=out32, name="gelu_tanh")
+        c.run()
+        c.check()
+
+
+@pytest.mark.parametrize("R", [1, 15, 16, 17, 31, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 400, 449, 511, 512, 513, 600])
+@pytest.mark.parametrize("n", [1, 2, 20, 1000])
+def test_groups_of_every_number_of_rows(R, n):
+    """Groups that are full, one row short or over, of rows in any order, on kernels of four, eight and sixteen wavefronts."""
+    for N, K, pattern in ((48, 64, "random"), (2050, 72, "some"), (1100, 65, "runs"), (640, 192, "own")):
+        c = Adapted(R, N, K, 8, n, pattern, residual=True)
+        c.run()
+        c.check()
+
+
 @pytest.mark.parametrize("rank", [8, 16, 24, 32, 40, 56, 64, 72, 96, 120, 128])
 @pytest.mark.parametrize("out32", [False, True])
 @pytest.mark.parametrize("R,N,K", [(3, 40, 130), (70, 520, 320), (300, 640, 192), (700, 513, 136)])
