@@ -397,12 +397,13 @@ def _vector(x, name: str, n: int, kind: int, device: int) -> Optional[int]:
     if x is None:
         return None
     try:
+        if x.numel() >= n and x.dtype in _kinds[kind] and x.is_contiguous() and x.get_device() == device:
+            return x.data_ptr()
         if x.numel() < n or x.element_size() != _SIZES[kind] or not x.is_contiguous():
             raise ValueError(f"{name} must be {n} contiguous elements of {_SIZES[kind]} bytes")
     except AttributeError:
         return _ptr(x)
-    if x.dtype not in _kinds[kind]:
-        _check_type(x, name, kind)
+    _check_type(x, name, kind)
     if x.get_device() != device:
         _check_place(x, name, device)
     return x.data_ptr()

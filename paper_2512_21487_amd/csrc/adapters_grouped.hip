@@ -90,7 +90,12 @@ hipError_t launch_linear_grouped(const LinearArgs& a, const AdapterArgs& x, floa
     // two workgroups for a compute unit, beside the product's own (512 x 4096 x 4096, 400 adapters of rank 32, one / two / four 84 / 90 / 91 us, of rank 128 169 / 187 / 161)
     g.shares = g.groups * blocks <= 2 * n_cu ? blocks : 2 * n_cu / g.groups > 1 ? 2 * n_cu / g.groups : 1;
     g.workgroups = (g.groups * g.shares + 7) / 8 * 8;
-    const hipError_t e = launch_chosen(adapter_kernel(linear_kernel(product, n_cu)), product, g, n_cu, s);
+    // Of up to 32 rows the weights bound it, and what is on its way from memory: 32 columns a workgroup and two K steps ahead, eight wavefronts, so that compute units have two workgroups
+    // or more, x A^T beside the product among them.  The product's own kernel / this, rank 16, us: 1, 12 x 5120 x 5120 20.8 / 18.1, 22.6 / 19.6, 2 x 4096 x 4096 17.0 / 14.0,
+    // 4 x 5120 x 1536 12.0 / 10.4, 17 x 4096 x 4096 21.0 / 16.9, 32 x 5120 x 5120 30 / 24; of few columns both are as fast, 1 x 160 x 5120 11.2 / 11.4.
+    const hipError_t e = a.R <= 16   ? launch_split<1, 2, 8, 2>(product, g, s)
+                         : a.R <= 32 ? launch_split<2, 2, 8, 2>(product, g, s)
+                                     : launch_chosen(adapter_kernel(linear_kernel(product, n_cu)), product, g, n_cu, s);
     return e == hipSuccess ? launch_up<2>(a, x, wide, table, g.groups, s) : e;
 }
 

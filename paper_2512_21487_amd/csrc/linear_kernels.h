@@ -517,7 +517,7 @@ __device__ __forceinline__ void split3(const f32x8_t& w, bf16x8_t part[3])
 // those lanes, 16 rows' bytes at a time, a load took the memory path four times as long (4096 x 128 x 4096, fp32 weights: 33 us against 22).
 // Those 22 us are 1.6 TB/s of operands; the matrix unit is busy 16 % of them.  What bounds it is a step's chain in each wavefront, LDS write, read,
 // cutting the weights up, products, with only two wavefronts per SIMD to fill one another's gaps (eight slices of 16 KB are most of the LDS).
-template <int MB, int NB, int WAVES, bool W32, class X>
+template <int MB, int NB, int WAVES, bool W32, int DEPTH, class X>
 __global__ __launch_bounds__(WAVES * 64) void linear_split_kernel(LinearArgs a, X x)
 {
     using C = SplitCfg<MB, NB, W32>;
@@ -548,7 +548,7 @@ __global__ __launch_bounds__(WAVES * 64) void linear_split_kernel(LinearArgs a, 
     for (int i = 0; i < C::XL; ++i) xo[i] = (uint32_t)min(i * 8 + xr, a.R - 1 - m0) * (uint32_t)a.ldx + xc * 8;
 #pragma unroll
     for (int i = 0; i < C::WL; ++i) wo[i] = (uint32_t)min(i * (64 / (C::WROW / 16)) + wr, a.N - 1 - n0) * (uint32_t)a.ldw + wc * PER;
-    struct Step { u32x4_t x[C::XL], w[C::WL]; } f;
+    struct Step { u32x4_t x[C::XL], w[C::WL]; } f[DEPTH];                     // steps on their way
     const int k_steps = (a.K + KS - 1) / KS, whole = a.K / KS;
     int steps = k_steps;
     TileAdapters<MB * 16> tile;
@@ -557,7 +557,7 @@ __global__ __launch_bounds__(WAVES * 64) void linear_split_kernel(LinearArgs a, 
         steps += tile.count * (x.width / KS);
     }
     // whole: all 64 elements are there
-    const auto load = [&](int step, bool whole) __attribute__((always_inline)) {
+    const auto load = [&](Step& f, int step, bool whole) __attribute__((always_inline)) {
         if constexpr (X::on)
             if (step >= k_steps) {
                 const int per = x.width / KS, at = step - k_steps, i0 = at / per, ad = tile.adapter(i0), c = (at - i0 * per) * 8;
@@ -589,7 +589,7 @@ __global__ __launch_bounds__(WAVES * 64) void linear_split_kernel(LinearArgs a, 
         }
     };
     const uint32_t xw = xr * 128, ww = C::X_BYTES + wr * C::WROW;
-    const auto to_lds = [&]() __attribute__((always_inline)) {
+    const auto to_lds = [&](const Step& f) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < C::WL; ++i) {
             const int r = i * (64 / (C::WROW / 16)) + wr, sw = W32 ? r & 15 : (r >> 1) & 7;
@@ -632,14 +632,25 @@ __global__ __launch_bounds__(WAVES * 64) void linear_split_kernel(LinearArgs a, 
             }
         }
     };
-    if (wave < steps) load(wave, wave < whole);
-    for (int st = wave; st < steps; st += WAVES) {
-        to_lds();
+    const auto take = [&](Step& f, int next) __attribute__((always_inline)) {
+        to_lds(f);
         wavefront_lds_order();
-        if (st + WAVES < steps) load(st + WAVES, st + WAVES < whole);
+        if (next < steps) load(f, next, next < whole);
         SB();   // or the compiler moves loads behind the products
         multiply();
         wavefront_lds_order();
+    };
+    if constexpr (DEPTH == 1) {
+        if (wave < steps) load(f[0], wave, wave < whole);
+        for (int st = wave; st < steps; st += WAVES) take(f[0], st + WAVES);
+    } else {
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d)
+            if (wave + d * WAVES < steps) load(f[d], wave + d * WAVES, wave + d * WAVES < whole);
+        for (int st = wave; st < steps; st += WAVES * DEPTH)
+#pragma unroll
+            for (int d = 0; d < DEPTH; ++d)
+                if (d == 0 || st + d * WAVES < steps) take(f[d], st + (d + DEPTH) * WAVES);
     }
     // a wavefront's operands make room for its sums
     f32x4_t* const sums = reinterpret_cast<f32x4_t*>(own) + lane;
@@ -666,27 +677,27 @@ __global__ __launch_bounds__(WAVES * 64) void linear_split_kernel(LinearArgs a, 
     }
 }
 
-template <int MB, int NB, int WAVES, bool W32, class X>
+template <int MB, int NB, int WAVES, bool W32, int DEPTH, class X>
 hipError_t launch_split_as(const LinearArgs& a, const X& x, long long workgroups, hipStream_t s)
 {
     constexpr int own = WAVES * SplitCfg<MB, NB, W32>::BYTES, bytes = X::beside && group_lds(WAVES) > own ? group_lds(WAVES) : own;
     static_assert(bytes <= 160 * 1024, "LDS of a compute unit");
     static std::atomic<uint64_t> told{0};
-    const hipError_t e = allow_lds(&linear_split_kernel<MB, NB, WAVES, W32, X>, bytes, told);
+    const hipError_t e = allow_lds(&linear_split_kernel<MB, NB, WAVES, W32, DEPTH, X>, bytes, told);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((linear_split_kernel<MB, NB, WAVES, W32, X>), grid_of(workgroups + in_front_of(x)), dim3(WAVES * 64), bytes, s, a, x);
+    hipLaunchKernelGGL((linear_split_kernel<MB, NB, WAVES, W32, DEPTH, X>), grid_of(workgroups + in_front_of(x)), dim3(WAVES * 64), bytes, s, a, x);
     return hipGetLastError();
 }
 
-template <int MB, int NB, int WAVES, class X>
+template <int MB, int NB, int WAVES, int DEPTH = 1, class X>
 hipError_t launch_split(LinearArgs a, const X& x, hipStream_t s)
 {
     const long long mt = (a.R + MB * 16 - 1) / (MB * 16), nt = (a.N + NB * 16 - 1) / (NB * 16), per = (mt * nt + 7) / 8;
     // an XCD's tiles share the rows of the larger operand through its L2
     a.rows_first = (double)a.N * a.K * (a.w32 ? 4 : 2) > (double)a.R * a.K * 2;
     if constexpr (!X::on && !X::beside)
-        if (a.w32) return launch_split_as<MB, NB, WAVES, true>(a, x, per * 8, s);
-    return launch_split_as<MB, NB, WAVES, false>(a, x, per * 8, s);
+        if (a.w32) return launch_split_as<MB, NB, WAVES, true, DEPTH>(a, x, per * 8, s);
+    return launch_split_as<MB, NB, WAVES, false, DEPTH>(a, x, per * 8, s);
 }
 
 // ---- many rows and columns
