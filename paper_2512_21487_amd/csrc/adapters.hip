@@ -107,14 +107,16 @@ hipError_t launch_tiles(const LinearArgs& a, const AdapterArgs& x, int groups, h
 }  // namespace
 
 // Tiles of few rows spread a few hundred of them over the compute units, tall ones read A less often.  16 rows x 16 ranks (a), two workgroups with 16 x 32 (b), two with 32 x 64 (c), 32 x
-// 64 (d), 64 x 64 (e, not kept): the whole call of R x 1024 x 4096, 16 prompts, us: rank 16, R 600 30 / 31 / 40 / - / -, 4096 49 / 56 / 55 / - / -, 16384 157 / - / 170 / 159 / 161; rank 64, 1024 34 / 32 /
-// 42 / - / -, 2048 51 / 51 / 47 / 50 / -, 4096 71 / - / 59 / 66 / -, 8192 - / - / 110 / 108 / 116, 16384 - / - / 186 / 170 / 167; rank 128, 4096 - / - / 77 / 71 / 85, 16384 - / - / 253 / 206 / 207.
-hipError_t launch_adapters_down(const LinearArgs& a, const AdapterArgs& x, hipStream_t s)
+// 64 (d), 64 x 64 (e): the whole call of R x 1024 x 4096, 16 prompts, us: rank 16, R 600 30 / 31 / 40 / - / -, 4096 49 / 56 / 55 / - / -, 16384 157 / - / 170 / 159 / 161; rank 64, 1024 34 / 32 /
+// 42 / - / -, 2048 51 / 51 / 47 / 50 / -, 4096 71 / - / 59 / 66 / -, 8192 - / - / 110 / 108 / 116, 16384 - / - / 186 / 170 / 167; rank 128, 4096 - / - / 77 / 71 / 85, 16384 - / - / 253 / 206 / 207; of
+// 16384 x 5120 x 5120, rank 64, (d) 718, (e) 692.  Tiles of 64 x 64 filled by direct loads into a ring took as long as (e) (693), and longer of fewer rows.
+hipError_t launch_adapters_down(const LinearArgs& a, const AdapterArgs& x, int n_cu, hipStream_t s)
 {
     if (x.rank <= 16) return launch_tiles<1, 1, 16, 2>(a, x, 1, s);
     if (a.R < 2048) return launch_tiles<1, 2, 8, 4>(a, x, 2, s);
     if (a.R < 8192) return launch_tiles<2, 4, 8, 2>(a, x, 2, s);
-    return launch_tiles<2, 4, 8, 1>(a, x, 1, s);
+    if (a.R < 64 * n_cu) return launch_tiles<2, 4, 8, 1>(a, x, 1, s);
+    return launch_tiles<4, 4, 8, 1>(a, x, 1, s);
 }
 
 hipError_t launch_linear_adapters(const LinearArgs& a, const AdapterArgs& x, int n_cu, hipStream_t s)
@@ -123,7 +125,7 @@ hipError_t launch_linear_adapters(const LinearArgs& a, const AdapterArgs& x, int
     if (a.N < 1 || a.K < 1 || a.w32 || x.n < 1 || x.rank < 8 || x.rank > kRankMost || x.rank % 8) return hipErrorInvalidValue;
     const int kernel = adapter_kernel(linear_kernel(a, n_cu));
     if (x.tile != linear_tile_rows(kernel)) return hipErrorInvalidValue;
-    const hipError_t e = launch_adapters_down(a, x, s);
+    const hipError_t e = launch_adapters_down(a, x, n_cu, s);
     return e == hipSuccess ? launch_chosen(kernel, a, x, n_cu, s) : e;
 }
 

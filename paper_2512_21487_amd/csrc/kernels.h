@@ -276,7 +276,7 @@ inline int adapter_groups(int R, int n) { return R / 16 + (n + 1 < R ? n + 1 : R
 // The product's kernel with adapters: dot products have no reduction that could go on, and too few wavefronts to make x A^T beside them: rows / split, us: 8 x 1024 x 4096 21 / 12, 1 x
 // 160 x 5120 11.4 / 10.7, rank 16.
 constexpr int adapter_kernel(int linear) { return linear < kLinearTiled ? kLinearSplit16x16 : linear; }
-hipError_t launch_adapters_down(const LinearArgs& a, const AdapterArgs& x, hipStream_t s);
+hipError_t launch_adapters_down(const LinearArgs& a, const AdapterArgs& x, int n_cu, hipStream_t s);
 hipError_t launch_linear_adapters(const LinearArgs& a, const AdapterArgs& x, int n_cu, hipStream_t s);
 hipError_t launch_linear_grouped(const LinearArgs& a, const AdapterArgs& x, float* wide, int32_t* table, int n_cu, hipStream_t s);
 

@@ -148,6 +148,17 @@ def test_ranks(rank, out32, R, N, K):
     c.check()
 
 
+@pytest.mark.parametrize("R", [513, 1100, 2048, 5000, 8200, 16384, 16500])
+@pytest.mark.parametrize("rank", [8, 16, 24, 64, 72, 128])
+@pytest.mark.parametrize("K", [63, 200])
+def test_every_tile_of_x_a(R, rank, K):
+    """x A^T of many rows, by each of its tiles: ranks that fill them or not, a reduction with and without a whole step, adapters that change inside tiles."""
+    for pattern in ("runs", "some"):
+        c = Adapted(R, 40, K, rank, 9, pattern, out32=rank == 24, bias=True)
+        c.run()
+        c.check()
+
+
 @pytest.mark.parametrize("R", [256, 300, 1100])
 @pytest.mark.parametrize("N,K", [(2048, 512), (1544, 328)])
 def test_an_adapter_for_every_row(R, N, K):

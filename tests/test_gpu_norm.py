@@ -319,6 +319,21 @@ def test_offsets_beyond_32_bits():
     assert not bool(wide[:, 512:600].any())
 
 
+def test_more_rows_than_a_grid_has_rows_of_threads():
+    """2^32 threads are a grid dimension's; a wavefront has a row."""
+    import paper_2512_21487_amd as pkg
+    R, M = 2 ** 26 + 5, 8
+    x = torch.randint(-3, 4, (R, M), device="cuda", dtype=torch.int8).to(torch.bfloat16)
+    out = torch.full((R + 1, M), 9.0, dtype=torch.bfloat16, device="cuda")
+    pkg.norm(pkg.NormConfig(features=M, norm_before=pkg.NORM_RMS), x, out=out, n_rows=R)
+    torch.cuda.synchronize()
+    for rows in (slice(0, 1000), slice(R // 2, R // 2 + 1000), slice(R - 1000, R)):
+        v = x[rows].double()
+        want = v / torch.sqrt(v.square().mean(dim=1, keepdim=True) + 1e-6)
+        assert bool(((out[rows].double() - want).abs() <= 1.01 * 2.0 ** -8 * want.abs()).all())   # a rounding to bf16
+    assert bool(torch.isfinite(out).all()) and bool((out[R] == 9.0).all())
+
+
 def test_no_rows_and_refused_memory():
     import paper_2512_21487_amd as pkg
     cfg = pkg.NormConfig(features=64, norm_before=pkg.NORM_RMS)
