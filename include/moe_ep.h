@@ -326,14 +326,15 @@ size_t moe_ep_linear_adapters_workspace_bytes(const moe_ep_linear_config *cfg, c
 
 /*
  *   x, weight, bias, residual, out, n_rows   as for moe_ep_linear; weight_type MOE_EP_BF16
- *   index      int32 [n_rows], device memory: a row's adapter; any number outside 0..n_adapters - 1: no adapter.  Rows in any order; rows of one adapter that
- *              lie together (a prompt's, say) cost least: of up to 256 rows that share a tile, every adapter adds 64 elements or more to K
+ *   index      int32 [n_rows], device memory: a row's adapter; any number outside 0..n_adapters - 1: no adapter.  Rows in any order.  Up to 512 rows are
+ *              grouped by adapter; of more, those of one adapter that lie together (a prompt's, say) cost least: of up to 256 rows that share a tile, every adapter adds 64
+ *              elements or more to K
  *   down, up   bf16 [n_adapters, rank, K] and [n_adapters, N, rank], A and B, without gaps; `up` on 16 bytes.  Of the adapters that `index` names they must
  *              be finite: one that is not may give NaN in rows of others too
  *   scale      fp32 [n_adapters], or NULL (1)
  *   workspace  workspace_bytes bytes of device memory on 16 bytes, the call's own until `stream` has passed it: nothing in it has to be set, nothing is kept in it, and
  *              two calls that may overlap (on two streams, or in two graphs) need one each
- * x A^T is summed in fp32 and keeps 16 bits of mantissa on its way to B, 24 where out is fp32; the rest as for moe_ep_linear.  out and
+ * x A^T is summed in fp32 and keeps 16 bits of mantissa on its way to B, 24 where out is fp32 (a row of x that is not finite may give NaN where the formula gives an infinity); the rest as for moe_ep_linear.  out and
  * workspace must not overlap anything else, but out the residual in place.  The call enqueues two kernels.  A row without an adapter has the product's formula; its bits may differ from
  * moe_ep_linear's, which may choose another kernel.
  */
@@ -385,8 +386,8 @@ int moe_ep_validate_norm(const moe_ep_norm_config *cfg, const char **why);
  *   out        out_type [n_rows, M], exactly where norm_before is not MOE_EP_NORM_NONE; may be the block itself (same type and stride)
  *   n_rows     0..2^30
  * sum and out must not overlap anything else, nor each other (rows of the same distance may lie side by side).  Everything is computed in fp32 from h as it
- * is, not as `sum` holds it, and each result is rounded once.  A row with a number that is not finite gives what the formula gives; squares and
- * sums beyond fp32 do no harm.  Rows do not depend on each other; the same call gives the same bits.
+ * is, not as `sum` holds it, and each result is rounded once.  A row with a number that is not finite gives what the formula gives in fp32; in a
+ * norm, squares and sums beyond fp32 do no harm.  Rows do not depend on each other; the same call gives the same bits.
  * Alignment, what lies between rows, streams, graphs, devices, checks, `why` and n_rows == 0 as for moe_ep_linear.
  */
 int moe_ep_norm(const moe_ep_norm_config *cfg, const void *block, const void *residual, const void *gate, const void *after_weight,
