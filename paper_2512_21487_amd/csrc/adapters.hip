@@ -1,4 +1,4 @@
-// Low-rank adapters of many requests beside a shared projection: act(x W^T + bias + scale_a (x A_a^T) B_a^T) + residual, a = index[row].
+// Low-rank adapters of many requests beside a shared projection: act(x W^T + bias + scale_a (x A_a^T) B_a^T) + residual, a = index[row], of more than kGathered rows.
 // Two launches.  The first makes scale_a x A_a^T of every row with an adapter, and for every row tile of the second the list of its rows' adapters.  The
 // second is the product's own kernel (linear_kernels.h), whose reduction goes on behind K with these products and B_a: the
 // wide result is neither written twice nor read again.
@@ -97,7 +97,7 @@ hipError_t launch_tiles(const LinearArgs& a, const AdapterArgs& x, int groups, h
     static std::atomic<uint64_t> told{0};
     const hipError_t e = allow_lds(&adapters_down_tiles_kernel<MB, NB, WAVES, DEPTH>, bytes, told);
     if (e != hipSuccess) return e;
-    const long long list_tiles = x.tile ? ((long long)a.R + x.tile - 1) / x.tile : 0;
+    const long long list_tiles = ((long long)a.R + x.tile - 1) / x.tile;
     const long long tiles = ((long long)a.R + MB * 16 - 1) / (MB * 16), blocks = (x.rank + NB * 16 - 1) / (NB * 16);
     const long long grid = (list_tiles + WAVES - 1) / WAVES + tiles * blocks * groups;
     hipLaunchKernelGGL((adapters_down_tiles_kernel<MB, NB, WAVES, DEPTH>), grid_of(grid), dim3(WAVES * 64), bytes, s, a, x, (int)list_tiles, groups);

@@ -231,7 +231,8 @@ struct SplitCfg {
 __device__ __forceinline__ uint32_t upper_halves(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
 
 // A wavefront's 16 rows x 16 ranks of sums: a lane has 4 consecutive ranks of its row, r the first.  They are written as `parts` bf16 numbers each, 8 bits cut off the top at a
-// time and the last rounded: two leave 2^-17 of the sum, which is 2^-8 of what rounding the result to bf16 leaves, three 2^-25 (results in fp32).
+// time and the last rounded.  Of a sum in 1..2 the first leaves less than 2^-7, what rounds that to 8 bits half a step, 2^-16 at most: 2^-8 of what rounding the result to bf16
+// leaves.  With one cut more 2^-24 are left (results in fp32).
 __device__ __forceinline__ void store_low(const AdapterArgs& x, long long row, int r, f32x4_t v)
 {
     uint16_t* const to = x.low + row * adapter_pitch(x.width) + r;

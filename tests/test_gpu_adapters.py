@@ -63,7 +63,8 @@ class Adapted(Case):
         u = 2.0 ** -24
         x, w = self.x.double(), self.w.double()
         z, size, off = x @ w.t(), x.abs() @ w.abs().t(), torch.zeros((self.R, self.N), dtype=torch.float64, device="cuda")
-        cut = 2.0 ** -25 if self.out32 else 2.0 ** -17
+        # x A^T as bf16 numbers, 8 bits each: of a number in 1..2 less than 2^-7 is left of the first, half a step of that, 2^-16 at most, of two, 2^-24 of three
+        cut = 2.0 ** -24 if self.out32 else 2.0 ** -16
         for a in np.unique(self.index.cpu().numpy()).tolist():
             if not 0 <= a < self.n:
                 continue
