@@ -321,7 +321,8 @@ typedef struct {
 /* Pure host check of both, usable without a GPU; returns and `why` as for moe_ep_validate_config.  cfg as for moe_ep_linear, with weights in bf16. */
 int moe_ep_validate_linear_adapters(const moe_ep_linear_config *cfg, const moe_ep_adapter_config *adapters, const char **why);
 
-/* Bytes of workspace that a call of up to n_rows rows needs (0 if something is invalid, or without rows); never fewer for more rows. */
+/* Bytes of workspace that a call of up to n_rows rows needs (0 if something is invalid, or without rows); never fewer for more rows.  Of more than 512 rows
+ * whose length or distance is not a multiple of 8 elements, x's or weight's, room for a copy of them is among it. */
 size_t moe_ep_linear_adapters_workspace_bytes(const moe_ep_linear_config *cfg, const moe_ep_adapter_config *adapters, int32_t n_rows);
 
 /*

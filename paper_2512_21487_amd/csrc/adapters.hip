@@ -62,9 +62,31 @@ __device__ __forceinline__ void store_zeros(const AdapterArgs& x, long long row)
     *reinterpret_cast<u32x4_t*>(x.low + row * adapter_pitch(x.width) + x.width) = u32x4_t{0, 0, 0, 0};
 }
 
+// Rows on 16 bytes, zeros behind the last element: a wavefront has a row, 4 KB of it on their way.  `number`: of the launch's copying wavefronts
+__device__ __forceinline__ void align_rows(const AlignArgs& c, int number, int wavefronts, int lane)
+{
+    constexpr int STEP = 64 * 8, AHEAD = 4;
+    for (int at = number; at < c.x.rows + c.w.rows; at += wavefronts) {
+        const bool of_x = at < c.x.rows;
+        const AlignArgs::Rows& r = of_x ? c.x : c.w;
+        const size_t row = of_x ? at : at - c.x.rows;
+        const uint16_t* const from = r.from + row * r.ld;
+        uint16_t* const to = r.to + row * c.pitch;
+        int k = lane * 8;
+        for (; k + (AHEAD - 1) * STEP + 8 <= c.K; k += AHEAD * STEP) {
+            u32x4_t v[AHEAD];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) v[i] = *reinterpret_cast<const u32x4_any2*>(from + k + i * STEP);
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) *reinterpret_cast<u32x4_t*>(to + k + i * STEP) = v[i];
+        }
+        for (; k < c.pitch; k += STEP) *reinterpret_cast<u32x4_t*>(to + k) = load_part<8>(from + k, c.K - k, c.K);
+    }
+}
+
 // Many rows: a workgroup has MB * 16 of them and NB * 16 ranks, and of the rows' adapters each `groups`th.
 template <int MB, int NB, int WAVES, int DEPTH>
-__global__ __launch_bounds__(WAVES * 64) void adapters_down_tiles_kernel(LinearArgs a, AdapterArgs x, int list_tiles, int groups)
+__global__ __launch_bounds__(WAVES * 64) void adapters_down_tiles_kernel(LinearArgs a, AdapterArgs x, AlignArgs c, int list_tiles, int groups)
 {
     extern __shared__ uint4 lds4[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -77,7 +99,12 @@ __global__ __launch_bounds__(WAVES * 64) void adapters_down_tiles_kernel(LinearA
     const int blocks = (x.rank + NB * 16 - 1) / (NB * 16);
     const int r0 = (int)(b % blocks) * (NB * 16), group = (int)(b / blocks % groups);
     const long long m0 = b / blocks / groups * (MB * 16);
-    if (m0 >= a.R) return;
+    if (m0 >= a.R) {
+        // the copies are behind: these have a chain of K steps, those fill what they leave
+        const long long number = b - (((long long)a.R + MB * 16 - 1) / (MB * 16)) * blocks * groups;
+        if (number < c.workgroups) align_rows(c, (int)number * WAVES + wave, c.workgroups * WAVES, lane);
+        return;
+    }
     const bool mine = lane < MB * 16 && m0 + lane < a.R;
     if (r0 == 0 && group == 0 && wave == 0 && mine) store_zeros(x, m0 + lane);
     Distinct tile(mine ? adapter_of(x, (int)(m0 + lane)) : -1);
@@ -90,7 +117,7 @@ __global__ __launch_bounds__(WAVES * 64) void adapters_down_tiles_kernel(LinearA
 }
 
 template <int MB, int NB, int WAVES, int DEPTH>
-hipError_t launch_tiles(const LinearArgs& a, const AdapterArgs& x, int groups, hipStream_t s)
+hipError_t launch_tiles(const LinearArgs& a, const AdapterArgs& x, const AlignArgs& c, int groups, hipStream_t s)
 {
     constexpr int bytes = WAVES * SplitCfg<MB, NB, false>::BYTES;
     static_assert(bytes <= 160 * 1024, "LDS of a compute unit");
@@ -99,34 +126,59 @@ hipError_t launch_tiles(const LinearArgs& a, const AdapterArgs& x, int groups, h
     if (e != hipSuccess) return e;
     const long long list_tiles = ((long long)a.R + x.tile - 1) / x.tile;
     const long long tiles = ((long long)a.R + MB * 16 - 1) / (MB * 16), blocks = (x.rank + NB * 16 - 1) / (NB * 16);
-    const long long grid = (list_tiles + WAVES - 1) / WAVES + tiles * blocks * groups;
-    hipLaunchKernelGGL((adapters_down_tiles_kernel<MB, NB, WAVES, DEPTH>), grid_of(grid), dim3(WAVES * 64), bytes, s, a, x, (int)list_tiles, groups);
+    const long long grid = c.workgroups + (list_tiles + WAVES - 1) / WAVES + tiles * blocks * groups;
+    hipLaunchKernelGGL((adapters_down_tiles_kernel<MB, NB, WAVES, DEPTH>), grid_of(grid), dim3(WAVES * 64), bytes, s, a, x, c, (int)list_tiles, groups);
     return hipGetLastError();
 }
-
-}  // namespace
 
 // Tiles of few rows spread a few hundred of them over the compute units, tall ones read A less often.  16 rows x 16 ranks (a), two workgroups with 16 x 32 (b), two with 32 x 64 (c), 32 x
 // 64 (d), 64 x 64 (e): the whole call of R x 1024 x 4096, 16 prompts, us: rank 16, R 600 30 / 31 / 40 / - / -, 4096 49 / 56 / 55 / - / -, 16384 157 / - / 170 / 159 / 161; rank 64, 1024 34 / 32 /
 // 42 / - / -, 2048 51 / 51 / 47 / 50 / -, 4096 71 / - / 59 / 66 / -, 8192 - / - / 110 / 108 / 116, 16384 - / - / 186 / 170 / 167; rank 128, 4096 - / - / 77 / 71 / 85, 16384 - / - / 253 / 206 / 207; of
 // 16384 x 5120 x 5120, rank 64, (d) 718, (e) 692.  Tiles of 64 x 64 filled by direct loads into a ring took as long as (e) (693), and longer of fewer rows.
-hipError_t launch_adapters_down(const LinearArgs& a, const AdapterArgs& x, int n_cu, hipStream_t s)
+hipError_t launch_adapters_down(const LinearArgs& a, const AdapterArgs& x, const AlignArgs& c, int n_cu, hipStream_t s)
 {
-    if (x.rank <= 16) return launch_tiles<1, 1, 16, 2>(a, x, 1, s);
-    if (a.R < 2048) return launch_tiles<1, 2, 8, 4>(a, x, 2, s);
-    if (a.R < 8192) return launch_tiles<2, 4, 8, 2>(a, x, 2, s);
-    if (a.R < 64 * n_cu) return launch_tiles<2, 4, 8, 1>(a, x, 1, s);
-    return launch_tiles<4, 4, 8, 1>(a, x, 1, s);
+    if (x.rank <= 16) return launch_tiles<1, 1, 16, 2>(a, x, c, 1, s);
+    if (a.R < 2048) return launch_tiles<1, 2, 8, 4>(a, x, c, 2, s);
+    if (a.R < 8192) return launch_tiles<2, 4, 8, 2>(a, x, c, 2, s);
+    if (a.R < 64 * n_cu) return launch_tiles<2, 4, 8, 1>(a, x, c, 1, s);
+    return launch_tiles<4, 4, 8, 1>(a, x, c, 1, s);
 }
 
-hipError_t launch_linear_adapters(const LinearArgs& a, const AdapterArgs& x, int n_cu, hipStream_t s)
+}  // namespace
+
+hipError_t launch_linear_adapters(const LinearArgs& a, AdapterArgs x, uint16_t* aligned_x, uint16_t* aligned_w, int n_cu, hipStream_t s)
 {
     if (a.R <= 0) return hipSuccess;
     if (a.N < 1 || a.K < 1 || a.w32 || x.n < 1 || x.rank < 8 || x.rank > kRankMost || x.rank % 8) return hipErrorInvalidValue;
-    const int kernel = adapter_kernel(linear_kernel(a, n_cu));
-    if (x.tile != linear_tile_rows(kernel)) return hipErrorInvalidValue;
-    const hipError_t e = launch_adapters_down(a, x, n_cu, s);
-    return e == hipSuccess ? launch_chosen(kernel, a, x, n_cu, s) : e;
+    LinearArgs product = a;
+    AlignArgs c{};
+    c.K = a.K;
+    c.pitch = adapter_pitch_of(a.K);
+    if (aligned_x) {
+        c.x = {a.x, aligned_x, a.ldx, a.R};
+        product.x = aligned_x;
+        product.ldx = c.pitch;
+    }
+    if (aligned_w) {
+        c.w = {static_cast<const uint16_t*>(a.w), aligned_w, a.ldw, a.N};
+        product.w = aligned_w;
+        product.ldw = c.pitch;
+    }
+    product.K = c.pitch;
+    int kernel = adapter_kernel(linear_kernel(product, n_cu));
+    // only where the product is then one of tiles filled by direct loads
+    if (aligned_x || aligned_w) {
+        if (kernel >= kLinearTiled && kernel < kLinearStaged128x64) {
+            c.workgroups = (int)fmin(((double)c.x.rows + c.w.rows + 7) / 8, 4.0 * n_cu);   // a row for a wavefront, eight wavefronts or sixteen
+        } else {
+            product = a;
+            c = AlignArgs{};
+            kernel = adapter_kernel(linear_kernel(a, n_cu));
+        }
+    } else product.K = a.K;
+    x.tile = linear_tile_rows(kernel);
+    const hipError_t e = launch_adapters_down(a, x, c, n_cu, s);
+    return e == hipSuccess ? launch_chosen(kernel, product, x, n_cu, s) : e;
 }
 
 }  // namespace moe_ep

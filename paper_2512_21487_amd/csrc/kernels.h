@@ -276,8 +276,17 @@ inline int adapter_groups(int R, int n) { return R / 16 + (n + 1 < R ? n + 1 : R
 // The product's kernel with adapters: dot products have no reduction that could go on, and too few wavefronts to make x A^T beside them: rows / split, us: 8 x 1024 x 4096 21 / 12, 1 x
 // 160 x 5120 11.4 / 10.7, rank 16.
 constexpr int adapter_kernel(int linear) { return linear < kLinearTiled ? kLinearSplit16x16 : linear; }
-hipError_t launch_adapters_down(const LinearArgs& a, const AdapterArgs& x, int n_cu, hipStream_t s);
-hipError_t launch_linear_adapters(const LinearArgs& a, const AdapterArgs& x, int n_cu, hipStream_t s);
+// Rows of x or of W that are not on 16 bytes are copied in front of a product in tiles, each to `pitch` elements with zeros at the end, beside x A^T.  That moves them once more; tiles through registers take
+// twice as long as direct loads.  Without / with copies, rank 16, us: 700 x 1000 x 1001 29 / 22, 1531 x 1409 x 2049 53 / 43, 8000 x 777 x 2001 126 / 85, rows of x alone: 600 x 4096 x 1024 31 / 24,
+// 4096 x 4096 x 2048 164 / 80, 16384 x 2048 x 2048 344 / 178.
+struct AlignArgs {
+    struct Rows { const uint16_t* from; uint16_t* to; long long ld; int rows; } x, w;   // rows 0: as they are
+    int K, pitch, workgroups;
+};
+inline int adapter_pitch_of(int K) { return (K + 7) / 8 * 8; }
+inline bool rows_off_16(int K, long long ld) { return K % 8 != 0 || ld % 8 != 0; }   // whatever the first one's address
+// aligned_x, aligned_w: room for the copies, or NULL; x.tile and x.lists' contents are the launch's
+hipError_t launch_linear_adapters(const LinearArgs& a, AdapterArgs x, uint16_t* aligned_x, uint16_t* aligned_w, int n_cu, hipStream_t s);
 hipError_t launch_linear_grouped(const LinearArgs& a, const AdapterArgs& x, float* wide, int32_t* table, int n_cu, hipStream_t s);
 
 // ---- norms around a block (norm.hip): the public struct's fields as the kernels read them

@@ -117,19 +117,24 @@ struct Product {
 // bf16 numbers that stand for one of x A^T
 int parts_of(const moe_ep_linear_config& c) { return c.out_type == MOE_EP_F32 ? 3 : 2; }
 
-// What the workspace holds: x A^T of every row; behind it, of up to kGathered rows, x W^T in fp32 and the groups' table, of more the lists of the row tiles, of 16 to 256 rows: (R / t + 1)
+// What the workspace holds: x A^T of every row; behind it, of up to kGathered rows, x W^T in fp32 and the groups' table, of more the lists of the row tiles and, where rows are
+// not on 16 bytes, copies of x and of W that are.  A tile has 16 to 256 rows: (R / t + 1)
 // (1 + t (1 + t / 32)) numbers are at most those of t = 256 and one more for 16 rows.
 struct AdapterWorkspace {
-    size_t low, wide, table, lists;
+    size_t low, wide, table, lists, x, w;
     AdapterWorkspace(const moe_ep_linear_config& c, const moe_ep_adapter_config& ad, int32_t n_rows)
     {
         const int few = n_rows < kGathered ? n_rows : kGathered;
         low = (size_t)n_rows * adapter_pitch(adapter_width(ad.rank, parts_of(c))) * 2;
         wide = ((size_t)few * c.out_features * 4 + 15) / 16 * 16;
         table = (size_t)adapter_groups(few, ad.n_adapters) * kGroupEntry * 4;
-        lists = ((size_t)n_rows * 9 + n_rows / 16 + adapter_list(256) + 1) * 4;
+        lists = (((size_t)n_rows * 9 + n_rows / 16 + adapter_list(256) + 1) * 4 + 15) / 16 * 16;
+        const int K = c.in_features;
+        const size_t row = (size_t)adapter_pitch_of(K) * 2;
+        x = n_rows > kGathered && rows_off_16(K, c.x_stride ? c.x_stride : K) ? n_rows * row : 0;
+        w = n_rows > kGathered && rows_off_16(K, c.weight_stride ? c.weight_stride : K) ? c.out_features * row : 0;
     }
-    size_t bytes() const { return low + (wide + table > lists ? wide + table : lists); }   // of more rows not fewer: that holds of each
+    size_t bytes() const { return low + (wide + table > lists + x + w ? wide + table : lists + x + w); }   // of more rows not fewer: that holds of each
 };
 
 }  // namespace
@@ -282,8 +287,9 @@ int moe_ep_linear_adapters(const moe_ep_linear_config* c, const moe_ep_adapter_c
         e = launch_linear_grouped(p.args, a, reinterpret_cast<float*>(behind), reinterpret_cast<int32_t*>(behind + parts.wide), n_cu, static_cast<hipStream_t>(stream));
     else {
         a.lists = reinterpret_cast<int32_t*>(behind);
-        a.tile = linear_tile_rows(adapter_kernel(linear_kernel(p.args, n_cu)));
-        e = launch_linear_adapters(p.args, a, n_cu, static_cast<hipStream_t>(stream));
+        char* const copies = behind + parts.lists;
+        e = launch_linear_adapters(p.args, a, parts.x ? reinterpret_cast<uint16_t*>(copies) : nullptr, parts.w ? reinterpret_cast<uint16_t*>(copies + parts.x) : nullptr, n_cu,
+                                   static_cast<hipStream_t>(stream));
     }
     return e == hipSuccess ? MOE_EP_OK : hip_failed(why, "launch", e);
 }

@@ -112,6 +112,29 @@ def test_every_kernel(name, R, N, K, pattern):
         c.check()
 
 
+@pytest.mark.parametrize("name,R,N,K", [("staged 64x64", 1531, 1409, 136), ("staged 128x64", 3873, 2061, 72)])
+@pytest.mark.parametrize("pattern", ["runs", "some"])
+def test_operands_whose_first_row_alone_is_off_16_bytes(name, R, N, K, pattern):
+    """They are not copied, and go through registers."""
+    c = Adapted(R, N, K, 24, 9, pattern, bias=True, residual=True, name="silu", shifts=(1, 1, 0, 0))
+    if torch.cuda.get_device_properties(0).multi_processor_count == 256:
+        assert kernel_of(R, N, K, x=c.x.data_ptr(), w=c.w.data_ptr()) == name
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("R,N,K", [(600, 1100, 129), (1531, 1409, 203), (4100, 700, 65), (2000, 2500, 71)])
+@pytest.mark.parametrize("pads", [(0, 0, 0, 0), (3, 0, 0, 0), (0, 5, 0, 0), (7, 7, 3, 1)])
+@pytest.mark.parametrize("even", [False, True])
+def test_rows_that_are_copied(R, N, K, pads, even):
+    """Rows that are not on 16 bytes come into tiles from copies: x, W or both, with and without elements behind the last one."""
+    K = (K + 7) // 8 * 8 if even else K
+    for shifts in ((0, 0, 0, 0), (1, 3, 0, 0)):
+        c = Adapted(R, N, K, 16, 5, "runs", bias=True, residual=True, out32=even, pads=pads, shifts=shifts)
+        c.run()
+        c.check()
+
+
 # up to 512 rows are grouped, beside the product on each of its kernels
 GROUPED = {"rows 1x1": (5, 96, 200), "rows 4x2": (66, 16, 65), "split 16x16": (207, 151, 96), "split 32x16": (66, 707, 65), "split 64x16": (66, 1034, 65), "split 64x32": (65, 2051, 65),
            "split 64x32 by 4": (66, 8294, 65), "staged 128x64": (130, 32886, 65), "staged 64x64": (65, 12304, 65), "tiles 128x128": (67, 32395, 576),
