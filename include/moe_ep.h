@@ -321,13 +321,13 @@ typedef struct {
 /* Pure host check of both, usable without a GPU; returns and `why` as for moe_ep_validate_config.  cfg as for moe_ep_linear, with weights in bf16. */
 int moe_ep_validate_linear_adapters(const moe_ep_linear_config *cfg, const moe_ep_adapter_config *adapters, const char **why);
 
-/* Bytes of workspace that a call of up to n_rows rows needs (0 if something is invalid, or without rows); never fewer for more rows.  Of more than 512 rows
+/* Bytes of workspace that a call of up to n_rows rows needs (0 if something is invalid, or without rows); never fewer for more rows.  Of more than 768 rows
  * whose length or distance is not a multiple of 8 elements, x's or weight's, room for a copy of them is among it. */
 size_t moe_ep_linear_adapters_workspace_bytes(const moe_ep_linear_config *cfg, const moe_ep_adapter_config *adapters, int32_t n_rows);
 
 /*
  *   x, weight, bias, residual, out, n_rows   as for moe_ep_linear; weight_type MOE_EP_BF16
- *   index      int32 [n_rows], device memory: a row's adapter; any number outside 0..n_adapters - 1: no adapter.  Rows in any order.  Up to 512 rows are
+ *   index      int32 [n_rows], device memory: a row's adapter; any number outside 0..n_adapters - 1: no adapter.  Rows in any order.  Up to 768 rows are
  *              grouped by adapter; of more, those of one adapter that lie together (a prompt's, say) cost least: of up to 256 rows that share a tile, every adapter adds 64
  *              elements or more to K
  *   down, up   bf16 [n_adapters, rank, K] and [n_adapters, N, rank], A and B, without gaps; `up` on 16 bytes.  Of the adapters that `index` names they must

@@ -265,7 +265,9 @@ constexpr int kRankMost = 128;
 int linear_tile_rows(int kernel);       // of what linear_kernel chose; 0: no tiles
 // Few rows, of many adapters maybe: the product's launch leaves x W^T in fp32, and other workgroups of it make `low`, of groups of up to 16 rows of one adapter (or of none); another
 // launch adds the groups' low B_a^T and has the epilogue.
-constexpr int kGathered = 512, kGroupEntry = 1 + 16;
+// (tiles that the reduction goes on in / groups, us: rows in no order, 600, 768, 1024 x 4096 x 4096, rank 16 of 64, 119 / 63, 120 / 65, 129 / 86, 768 x 2048 x 2048, rank 64 of 256, 114 / 73; all of
+// their own, 768 x 4096 x 4096 173 / 198; prompts, 640 x 4096 x 4096 45 / 39, 640 x 5120 x 1536 28 / 35, 768 x 4096 x 4096 47 / 47, 768 x 2048 x 2048, rank 64, 27 / 31, 1024 x 4096 x 4096 48 / 57)
+constexpr int kGathered = 768, kGroupEntry = 1 + 16;
 struct GroupArgs {
     static constexpr bool on = false, beside = true;
     AdapterArgs adapters;

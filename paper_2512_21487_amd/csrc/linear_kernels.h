@@ -352,15 +352,17 @@ __device__ __forceinline__ void down_group(const LinearArgs& a, const GroupArgs&
     int* const all = reinterpret_cast<int*>(lds4);
     int* const in_front = all + kGathered;
     if (tid < 16) s_rows[tid] = -1;
-    // Every wavefront has all rows, 64 to a register, and counts for some 64 of them: of each adapter among these how many rows of the 64s in front have it.  (A thread that
-    // compares its row with all in front took 4 us for 512 rows.)
+    // Every wavefront has all rows, 64 to a register, and counts for some 64 of them: of each adapter among these how many rows of the 64s in front have it.  (Threads that
+    // compare their rows with all in front took 2 us longer for 500 rows.)
     constexpr int WORDS = kGathered / 64;
     int of[WORDS];
 #pragma unroll
     for (int i = 0; i < WORDS; ++i) of[i] = i * 64 + lane < a.R ? adapter_of(x, i * 64 + lane) : -2;
-    static_assert(WAVES >= WORDS / 2, "a wavefront counts for 64 rows, or for 64 from the beginning and 64 from the end");
 #pragma unroll 1
-    for (int own = wave; own < WORDS; own = WAVES < WORDS && own < WAVES ? WORDS - 1 - own : WORDS) {
+    for (int i = 0; i < WORDS; i += WAVES) {
+        // there and back, so that what all count together is as much
+        const int own = i / WAVES % 2 ? i + WAVES - 1 - wave : i + wave;
+        if (own * 64 >= a.R) continue;
         const int row = own * 64 + lane, mine = row < a.R ? adapter_of(x, row) : -2;
         int n = 0;
         unsigned long long left = __ballot(mine > -2);
@@ -385,8 +387,8 @@ __device__ __forceinline__ void down_group(const LinearArgs& a, const GroupArgs&
     }
     __syncthreads();
     int left = group, begin = -1;
-#pragma unroll
-    for (int w = 0; w < kGathered / 64; ++w) {
+#pragma unroll 1
+    for (int w = 0; w * 64 < a.R; ++w) {
         unsigned long long bits = s_begin[w];
         const int n = __popcll(bits);
         if (begin < 0 && left < n) {

@@ -123,7 +123,7 @@ def test_operands_whose_first_row_alone_is_off_16_bytes(name, R, N, K, pattern):
     c.check()
 
 
-@pytest.mark.parametrize("R,N,K", [(600, 1100, 129), (1531, 1409, 203), (4100, 700, 65), (2000, 2500, 71)])
+@pytest.mark.parametrize("R,N,K", [(600, 1100, 129), (800, 1100, 129), (1531, 1409, 203), (4100, 700, 65), (2000, 2500, 71)])
 @pytest.mark.parametrize("pads", [(0, 0, 0, 0), (3, 0, 0, 0), (0, 5, 0, 0), (7, 7, 3, 1)])
 @pytest.mark.parametrize("even", [False, True])
 def test_rows_that_are_copied(R, N, K, pads, even):
@@ -135,7 +135,7 @@ def test_rows_that_are_copied(R, N, K, pads, even):
         c.check()
 
 
-# up to 512 rows are grouped, beside the product on each of its kernels
+# up to 768 rows are grouped, beside the product on each of its kernels
 GROUPED = {"rows 1x1": (5, 96, 200), "rows 4x2": (66, 16, 65), "split 16x16": (207, 151, 96), "split 32x16": (66, 707, 65), "split 64x16": (66, 1034, 65), "split 64x32": (65, 2051, 65),
            "split 64x32 by 4": (66, 8294, 65), "staged 128x64": (130, 32886, 65), "staged 64x64": (65, 12304, 65), "tiles 128x128": (67, 32395, 576),
            "tiles 192x256": (66, 2100, 72), "tiles 256x192": (193, 33747, 72), "tiles 256x256": (512, 24719, 128), "tiles 64x64": (300, 2046, 256)}
@@ -153,7 +153,7 @@ def test_grouped_beside_every_kernel(name, pattern):
         c.check()
 
 
-@pytest.mark.parametrize("R", [1, 15, 16, 17, 31, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 400, 449, 511, 512, 513, 600])
+@pytest.mark.parametrize("R", [1, 15, 16, 17, 31, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 400, 449, 511, 512, 513, 600, 640, 703, 704, 767, 768, 769])
 @pytest.mark.parametrize("n", [1, 2, 20, 1000])
 def test_groups_of_every_number_of_rows(R, n):
     """Groups that are full, one row short or over, of rows in any order, on kernels of four, eight and sixteen wavefronts."""
@@ -165,14 +165,14 @@ def test_groups_of_every_number_of_rows(R, n):
 
 @pytest.mark.parametrize("rank", [8, 16, 24, 32, 40, 56, 64, 72, 96, 120, 128])
 @pytest.mark.parametrize("out32", [False, True])
-@pytest.mark.parametrize("R,N,K", [(3, 40, 130), (70, 520, 320), (300, 640, 192), (700, 513, 136)])
+@pytest.mark.parametrize("R,N,K", [(3, 40, 130), (70, 520, 320), (300, 640, 192), (700, 513, 136), (800, 513, 136)])
 def test_ranks(rank, out32, R, N, K):
     c = Adapted(R, N, K, rank, 6, "runs" if rank % 16 else "random", out32=out32, residual=True)
     c.run()
     c.check()
 
 
-@pytest.mark.parametrize("R", [513, 1100, 2048, 5000, 8200, 16384, 16500])
+@pytest.mark.parametrize("R", [769, 1100, 2048, 5000, 8200, 16384, 16500])
 @pytest.mark.parametrize("rank", [8, 16, 24, 64, 72, 128])
 @pytest.mark.parametrize("K", [63, 200])
 def test_every_tile_of_x_a(R, rank, K):
@@ -183,7 +183,7 @@ def test_every_tile_of_x_a(R, rank, K):
         c.check()
 
 
-@pytest.mark.parametrize("R", [256, 300, 1100])
+@pytest.mark.parametrize("R", [256, 300, 768, 1100])
 @pytest.mark.parametrize("N,K", [(2048, 512), (1544, 328)])
 def test_an_adapter_for_every_row(R, N, K):
     c = Adapted(R, N, K, 8, R, "own")
@@ -193,7 +193,7 @@ def test_an_adapter_for_every_row(R, N, K):
 
 @pytest.mark.parametrize("pads", [(8, 8, 8, 8), (1, 0, 0, 0), (0, 3, 0, 0), (0, 0, 5, 1), (4, 12, 20, 36)])
 @pytest.mark.parametrize("shifts", [(0, 0, 0, 0), (1, 1, 1, 1), (4, 2, 4, 2)])
-@pytest.mark.parametrize("R,N,K", [(7, 130, 192), (520, 520, 200), (520, 520, 203)])
+@pytest.mark.parametrize("R,N,K", [(7, 130, 192), (520, 520, 200), (520, 520, 203), (780, 520, 203)])
 @pytest.mark.parametrize("out32", [False, True])
 def test_strides_and_alignments(pads, shifts, R, N, K, out32):
     c = Adapted(R, N, K, 16, 4, "some", out32=out32, bias=True, residual=True, name="silu", pads=pads, shifts=shifts)

@@ -88,14 +88,14 @@ class Block:
         assert near(self.out, 0.5 * self.h32.double() + torch.sigmoid(self.close.double()) * self.y.double(), 1e-5)
 
 
-@pytest.mark.parametrize("T", [1, 4, 33, 200, 700])
+@pytest.mark.parametrize("T", [1, 4, 33, 200, 700, 900])
 def test_a_block(T):
     b = Block(T)
     b.run()
     b.check()
 
 
-@pytest.mark.parametrize("T", [1, 33, 700])
+@pytest.mark.parametrize("T", [1, 33, 900])
 def test_a_block_in_a_graph(T):
     b = Block(T)
     b.run()
