@@ -312,6 +312,53 @@ def test_offsets_beyond_32_bits():
     small.check()
 
 
+@pytest.mark.parametrize("R,N,K,name", [(800, 2048, 1024, "tiles"), (800, 2048, 1023, "copies"), (5000, 72, 4096, "shared reduction")])
+def test_offsets_beyond_32_bits_of_many_rows(R, N, K, name):
+    """The same where the product's reduction goes on, in tiles of each kind: the last of so many adapters that A, B or both begin behind 2^32 bytes."""
+    import paper_2512_21487_amd as pkg
+    rank, n = 128, 2 ** 32 // (256 * max(N, K)) + 3
+    small = Adapted(R, N, K, rank, 1, "one", out32=True)
+    down, up = (torch.zeros((n, *s), dtype=torch.bfloat16, device="cuda") for s in ((rank, K), (N, rank)))
+    down[n - 1], up[n - 1] = small.down[0], small.up[0]
+    scale = torch.ones(n, device="cuda")
+    scale[n - 1] = small.scale[0]
+    small.run()
+    out = torch.zeros_like(small.out)
+    adapters = pkg.AdapterConfig(n_adapters=n, rank=rank)
+    workspace = torch.empty(pkg.linear_adapters_workspace_bytes(small.cfg, adapters, R), dtype=torch.uint8, device="cuda")
+    pkg.linear_adapters(small.cfg, adapters, small.x, small.w, torch.full((R,), n - 1, dtype=torch.int32, device="cuda"), down, up, scale, out=out, workspace=workspace)
+    torch.cuda.synchronize()
+    assert torch.equal(out, small.out)
+    small.check()
+
+
+def test_rows_whose_products_lie_beyond_32_bits():
+    """So many rows that x, x A^T and the lists pass 2^32 bytes, or 2^30; the first, some in the middle and the last."""
+    import paper_2512_21487_amd as pkg
+    R, N, K, rank, n = 2 ** 25 + 77, 16, 72, 8, 3
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.empty((R, K), dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    w, down, up = (torch.empty(s, dtype=torch.bfloat16, device="cuda").normal_(0.0, 0.2, generator=gen) for s in ((N, K), (n, rank, K), (n, N, rank)))
+    index = torch.randint(-1, n, (R,), dtype=torch.int32, device="cuda", generator=gen)
+    cfg, adapters = pkg.LinearConfig(in_features=K, out_features=N), pkg.AdapterConfig(n_adapters=n, rank=rank)
+    workspace = torch.empty(pkg.linear_adapters_workspace_bytes(cfg, adapters, R), dtype=torch.uint8, device="cuda")
+    out = torch.full((R + 1, N), 9.0, dtype=torch.bfloat16, device="cuda")
+    pkg.linear_adapters(cfg, adapters, x, w, index, down, up, out=out, workspace=workspace, n_rows=R)
+    torch.cuda.synchronize()
+    for at in (0, R // 2, R - 2000):
+        rows = slice(at, at + 2000)
+        v, of = x[rows].double(), index[rows]
+        want, size = v @ w.double().t(), v.abs() @ w.double().abs().t()
+        for a in range(n):
+            mine = of == a
+            want[mine] += (v[mine] @ down[a].double().t()) @ up[a].double().t()
+            size[mine] += (v[mine].abs() @ down[a].double().abs().t()) @ up[a].double().abs().t()
+        # what the parts of x A^T leave, fp32 sums, and a rounding to bf16
+        bound = size * (2.0 ** -16 + (K + 24) * 2.0 ** -24)
+        assert bool(((out[rows].double() - want).abs() <= bound + 2.0 ** -8 * (want.abs() + bound)).all())
+    assert bool((out[R] == 9.0).all())
+
+
 def test_no_rows_and_refused_memory():
     import paper_2512_21487_amd as pkg
     c = Adapted(8, 32, 64, 16, 2, "own")
