@@ -344,6 +344,7 @@ def _current_stream(device: int) -> int:
 _I32, _BYTE = 2, 3             # kinds of elements beside BF16 and F32
 _SIZES = (2, 4, 4, 1)
 _kinds = (set(), set(), set(), set())   # what a torch tensor of a kind may be typed as; filled at the first one
+_usual = [None, None, None, None]       # and what it mostly is: told by identity in half the time
 
 
 def _check_type(x, name: str, kind: int) -> None:
@@ -354,6 +355,7 @@ def _check_type(x, name: str, kind: int) -> None:
         # bf16 may come as integers that hold its bits
         for have, types in zip(_kinds, ((torch.bfloat16, torch.int16, torch.uint16), (torch.float32,), (torch.int32,), (torch.uint8, torch.int8, torch.bool))):
             have.update(types)
+        _usual[:] = torch.bfloat16, torch.float32, torch.int32, torch.uint8
     if x.dtype not in _kinds[kind]:
         raise ValueError(f"{name} holds {x.dtype}, the call reads {('bfloat16', 'float32', 'int32', 'bytes')[kind]}")
 
@@ -377,7 +379,8 @@ def _rows(x, name: str, n_rows: int, cols: int, stride: int, kind: int, device: 
     except (AttributeError, TypeError):
         return _ptr(x)
     # the usual case, decided in half the time
-    if len(have) == 2 and have[0] >= n_rows and have[1] >= cols and apart[1] == 1 and apart[0] == stride and x.get_device() == device and x.dtype in _kinds[kind]:
+    if len(have) == 2 and have[0] >= n_rows and have[1] >= cols and apart[1] == 1 and apart[0] == stride and x.get_device() == device and (
+            x.dtype is _usual[kind] or x.dtype in _kinds[kind]):
         return x.data_ptr()
     _check_type(x, name, kind)
     _check_place(x, name, device)
@@ -397,7 +400,7 @@ def _vector(x, name: str, n: int, kind: int, device: int) -> Optional[int]:
     if x is None:
         return None
     try:
-        if x.numel() >= n and x.dtype in _kinds[kind] and x.is_contiguous() and x.get_device() == device:
+        if x.numel() >= n and (x.dtype is _usual[kind] or x.dtype in _kinds[kind]) and x.is_contiguous() and x.get_device() == device:
             return x.data_ptr()
         if x.numel() < n or x.element_size() != _SIZES[kind] or not x.is_contiguous():
             raise ValueError(f"{name} must be {n} contiguous elements of {_SIZES[kind]} bytes")

@@ -310,7 +310,8 @@ int norm_kernel_of(int R, int M, int n_cu);
 hipError_t launch_norm(const NormArgs& a, int n_cu, hipStream_t s);
 
 // What the kernels are about to read or write through a caller's pointer (moe_ep.hip): NULL where it is usable, else what is wrong.
-// device: the one that device memory has to be on, or -1
-const char* check_span(const void* p, size_t bytes, bool want_host, const void** dev_ptr, int device = -1);
+// device: the one that device memory has to be on, or -1.  found: receives the allocation, where it is device memory of a known extent
+struct Allocation { const char* base; size_t size; };
+const char* check_span(const void* p, size_t bytes, bool want_host, const void** dev_ptr, int device = -1, Allocation* found = nullptr);
 
 }  // namespace moe_ep

@@ -320,7 +320,7 @@ int fail(moe_ep_ctx* ctx, int code, const char* what, hipError_t e = hipSuccess)
 // pointer or an undersized buffer into an error before a kernel faults on it.  Returns nullptr when
 // the span is usable, else what is wrong with it.  `want_host`: pinned host memory is required
 // (the link stand-ins of MOE_EP_IO_PINNED_HOST); *dev_ptr receives the address kernels use.
-const char* moe_ep::check_span(const void* p, size_t bytes, bool want_host, const void** dev_ptr, int device)
+const char* moe_ep::check_span(const void* p, size_t bytes, bool want_host, const void** dev_ptr, int device, Allocation* found)
 {
     hipPointerAttribute_t attr;
     if (hipPointerGetAttributes(&attr, p) != hipSuccess) {
@@ -351,6 +351,7 @@ const char* moe_ep::check_span(const void* p, size_t bytes, bool want_host, cons
     const char* lo = static_cast<const char*>(base);
     const char* q = static_cast<const char*>(p);
     if (q < lo || (size_t)(lo + size - q) < bytes) return "points at an allocation smaller than the forward needs";
+    if (found && attr.type == hipMemoryTypeDevice) *found = Allocation{lo, size};
     return nullptr;
 }
 

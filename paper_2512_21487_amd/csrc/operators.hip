@@ -69,15 +69,26 @@ const char* overlap(const Span* sp, int n)
         }
     return nullptr;
 }
-// a buffer that the device cannot read or write, or NULL
+// A buffer that the device cannot read or write, or NULL.  Buffers often lie in one allocation: one that lies in an allocation that another of this call's was found in is not asked
+// about again (0.2 us each).
 const char* out_of_reach(const Span* sp, int n, int device)
 {
+    constexpr int kMost = 16;
+    Allocation known[kMost];
+    int count = 0;
     for (int i = 0; i < n && checks_pointers(); ++i) {
         if (!sp[i].p) continue;
-        if (const char* bad = check_span(sp[i].p, extent(sp[i]), false, nullptr, device)) {
+        const char* const p = static_cast<const char*>(sp[i].p);
+        const size_t bytes = extent(sp[i]);
+        bool in = false;
+        for (int k = 0; k < count && !in; ++k) in = p >= known[k].base && (size_t)(p - known[k].base) <= known[k].size && known[k].size - (size_t)(p - known[k].base) >= bytes;
+        if (in) continue;
+        Allocation found{nullptr, 0};
+        if (const char* bad = check_span(p, bytes, false, nullptr, device, &found)) {
             snprintf(t_text, sizeof t_text, "%s %s", sp[i].name, bad);
             return t_text;
         }
+        if (found.base && count < kMost) known[count++] = found;
     }
     return nullptr;
 }
