@@ -165,7 +165,7 @@ hipError_t launch_linear_adapters(const LinearArgs& a, AdapterArgs x, uint16_t* 
         product.ldw = c.pitch;
     }
     product.K = c.pitch;
-    int kernel = adapter_kernel(linear_kernel(product, n_cu));
+    int kernel = adapter_kernel(product, n_cu);
     // only where the product is then one of tiles filled by direct loads
     if (aligned_x || aligned_w) {
         if (kernel >= kLinearTiled && kernel < kLinearStaged128x64) {
@@ -173,7 +173,7 @@ hipError_t launch_linear_adapters(const LinearArgs& a, AdapterArgs x, uint16_t* 
         } else {
             product = a;
             c = AlignArgs{};
-            kernel = adapter_kernel(linear_kernel(a, n_cu));
+            kernel = adapter_kernel(a, n_cu);
         }
     } else product.K = a.K;
     x.tile = linear_tile_rows(kernel);

@@ -92,10 +92,13 @@ hipError_t launch_linear_grouped(const LinearArgs& a, const AdapterArgs& x, floa
     g.workgroups = (g.groups * g.shares + 7) / 8 * 8;
     // Of up to 32 rows the weights bound it, and what is on its way from memory: 32 columns a workgroup and two K steps ahead, eight wavefronts, so that compute units have two workgroups
     // or more, x A^T beside the product among them.  The product's own kernel / this, rank 16, us: 1, 12 x 5120 x 5120 20.8 / 18.1, 22.6 / 19.6, 2 x 4096 x 4096 17.0 / 14.0,
-    // 4 x 5120 x 1536 12.0 / 10.4, 17 x 4096 x 4096 21.0 / 16.9, 32 x 5120 x 5120 30 / 24; of few columns both are as fast, 1 x 160 x 5120 11.2 / 11.4.
-    const hipError_t e = a.R <= 16   ? launch_split<1, 2, 8, 2>(product, g, s)
-                         : a.R <= 32 ? launch_split<2, 2, 8, 2>(product, g, s)
-                                     : launch_chosen(adapter_kernel(linear_kernel(product, n_cu)), product, g, n_cu, s);
+    // 4 x 5120 x 1536 12.0 / 10.4, 17 x 4096 x 4096 21.0 / 16.9, 32 x 5120 x 5120 30 / 24; of few columns both are as fast, 1 x 160 x 5120 11.2 / 11.4.  Nor do workgroups of sixteen wavefronts, one a
+    // compute unit, go with many that make x A^T: 111 x 448 x 2240, rank 128 of 58, 30 / 22, 64 x 1536 x 2048, rank 64 of 64, 18 / 15; with few, 48 x 512 x 5120, rank 16 of 48, 14 / 16.
+    const int kernel = adapter_kernel(product, n_cu);
+    const bool sixteen = kernel == kLinearSplit16x16 || kernel == kLinearSplit32x16;
+    const hipError_t e = a.R <= 16                                                ? launch_split<1, 2, 8, 2>(product, g, s)
+                         : a.R <= 32 || (sixteen && 2 * g.workgroups > n_cu) ? launch_split<2, 2, 8, 2>(product, g, s)
+                                                                                  : launch_chosen(kernel, product, g, n_cu, s);
     return e == hipSuccess ? launch_up<2>(a, x, wide, table, g.groups, s) : e;
 }
 

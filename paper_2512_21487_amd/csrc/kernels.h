@@ -275,9 +275,11 @@ struct GroupArgs {
     int groups, shares, workgroups;     // groups there may be; workgroups that share one's ranks; of all, a multiple of the XCDs
 };
 inline int adapter_groups(int R, int n) { return R / 16 + (n + 1 < R ? n + 1 : R); }   // full ones, and one that is not for every adapter and for none
-// The product's kernel with adapters: dot products have no reduction that could go on, and too few wavefronts to make x A^T beside them: rows / split, us: 8 x 1024 x 4096 21 / 12, 1 x
-// 160 x 5120 11.4 / 10.7, rank 16.
-constexpr int adapter_kernel(int linear) { return linear < kLinearTiled ? kLinearSplit16x16 : linear; }
+// The product's kernel with adapters: linear_kernel's, but dot products have no reduction that could go on, and too few wavefronts to make x A^T beside them (rows / split, us: 8 x 1024 x
+// 4096 21 / 12, 1 x 160 x 5120 11.4 / 10.7, rank 16), and of a K of less than the four steps that the smaller tiles need, large tiles are often few: 192 x 256 tiles / shared reduction, us: 800 x
+// 448 x 128 22 / 10, 1016 x 256 x 192 24 / 10, 5692 x 128 x 192 24 / 14, 7933 x 299 x 130, 84 tiles, 53 / 27; 1000 x 5120 x 192, 120 tiles, 24 / 29, 4096 x 2048 x 128 26 / 36;
+// grouped 700 x 1024 x 192 18 / 14, 128 x 8192 x 128 18 / 12.
+int adapter_kernel(const LinearArgs& a, int n_cu);
 // Rows of x or of W that are not on 16 bytes are copied in front of a product in tiles, each to `pitch` elements with zeros at the end, beside x A^T.  That moves them once more; tiles through registers take
 // twice as long as direct loads.  Without / with copies, rank 16, us: 700 x 1000 x 1001 29 / 22, 1531 x 1409 x 2049 53 / 43, 8000 x 777 x 2001 126 / 85, rows of x alone: 600 x 4096 x 1024 31 / 24,
 // 4096 x 4096 x 2048 164 / 80, 16384 x 2048 x 2048 344 / 178.

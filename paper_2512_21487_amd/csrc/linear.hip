@@ -85,6 +85,14 @@ int linear_tile_rows(int kernel)
     }
 }
 
+int adapter_kernel(const LinearArgs& a, int n_cu)
+{
+    const int kernel = linear_kernel(a, n_cu);
+    if (kernel < kLinearTiled) return kLinearSplit16x16;
+    const double tiles = (double)((a.R + 191) / 192) * ((a.N + 255) / 256);
+    return a.K < 256 && kernel < kLinearTiled + 3 && 2.5 * tiles < n_cu ? kLinearSplit64x32by4 : kernel;
+}
+
 hipError_t launch_linear(const LinearArgs& a, int n_cu, hipStream_t s)
 {
     if (a.R <= 0) return hipSuccess;

@@ -532,7 +532,7 @@ __global__ __launch_bounds__(WAVES * 64) void linear_split_kernel(LinearArgs a, 
     const int mt = (a.R + MB * 16 - 1) / (MB * 16), nt = (a.N + NB * 16 - 1) / (NB * 16);
     if constexpr (X::beside)
         if (workgroup() < x.workgroups) {
-            down_group<WAVES, WAVES == 16 ? 2 : 4>(a, x, lds4, (int)workgroup());
+            down_group<WAVES, WAVES == 16 ? 2 : 3>(a, x, lds4, (int)workgroup());
             return;
         }
     const long long total = (long long)mt * nt, per = (total + 7) / 8, at = workgroup() - in_front_of(x), L = (at & 7) * per + (at >> 3);

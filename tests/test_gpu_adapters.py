@@ -163,6 +163,22 @@ def test_groups_of_every_number_of_rows(R, n):
         c.check()
 
 
+@pytest.mark.parametrize("R,N,K", [(800, 448, 128), (1016, 256, 192), (5692, 128, 192), (2000, 299, 130), (600, 300, 72), (770, 260, 65)])
+@pytest.mark.parametrize("pattern", ["runs", "some"])
+def test_short_reductions_of_few_columns(R, N, K, pattern):
+    c = Adapted(R, N, K, 16, 6, pattern, bias=True, residual=True, name="gelu")
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("R,N,K,rank,n", [(111, 448, 2240, 128, 58), (64, 1536, 320, 64, 64), (40, 100, 520, 128, 40), (200, 190, 130, 128, 150)])
+def test_many_groups_beside_a_small_product(R, N, K, rank, n):
+    for pattern in ("own", "some"):
+        c = Adapted(R, N, K, rank, n, pattern, residual=True)
+        c.run()
+        c.check()
+
+
 @pytest.mark.parametrize("rank", [8, 16, 24, 32, 40, 56, 64, 72, 96, 120, 128])
 @pytest.mark.parametrize("out32", [False, True])
 @pytest.mark.parametrize("R,N,K", [(3, 40, 130), (70, 520, 320), (300, 640, 192), (700, 513, 136), (800, 513, 136)])
