@@ -83,7 +83,8 @@ __device__ __forceinline__ float over_row(float v, float* lds, int& turn, Op op)
 
 // x <- (x - mean) / sqrt(mean((x - mean)^2) + eps); RMS: without the mean.  The mean is taken out before the squares are summed, so that nothing cancels.
 // Where squares or sums leave fp32 while the row's numbers do not, its largest is between 2^56 (its square times 32768 is 2^127) and 2^128: times 2^-72 neither
-// they nor anything that counts beside them is lost, and eps, which does not count there, goes with it.  Such a row costs two or three reductions more.
+// they nor anything that counts beside them is lost, and eps, which does not count there, goes with it, but to no less than a normal number: numbers that are all the
+// mean have nothing else below the square root.  Such a row costs two or three reductions more.
 template <int WAVES, int V>
 __device__ __forceinline__ void normalise(float (&x)[V][8], const int (&left)[V], int cols, int kind, float eps, float* lds, int& turn)
 {
@@ -121,7 +122,7 @@ __device__ __forceinline__ void normalise(float (&x)[V][8], const int (&left)[V]
                 for (int v = 0; v < V; ++v)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) x[v][i] *= s;
-                eps = eps * s * s;
+                eps = fmaxf(eps * s * s, __FLT_MIN__);
                 continue;
             }
         }

@@ -248,6 +248,22 @@ def test_rows_beyond_fp32_in_their_squares(M, kind):
     assert bool(torch.isfinite(out).all())
 
 
+@pytest.mark.parametrize("M", [8, 64, 512, 1024, 2048, 4096, 8192, 16384, 32768])
+def test_equal_numbers_beyond_fp32_in_their_sum(M):
+    """Powers of two, whose sums and mean are exact in any order: nothing is left of them, and the bias is the result."""
+    import paper_2512_21487_amd as pkg
+    for rows in (3, 300):
+        x = torch.full((rows, M), 2.0 ** 127, device="cuda")
+        x[1] = -2.0 ** 120
+        bias = torch.arange(M, device="cuda", dtype=torch.float32) - 3.0
+        for eps in (1e-20, 1e-6, 1.0):
+            out, total = torch.empty_like(x), torch.empty_like(x)
+            pkg.norm(pkg.NormConfig(features=M, norm_before=pkg.NORM_LAYER, block_type=1, out_type=1, weight_type=1, eps=eps), x, before_bias=bias, out=out)
+            pkg.norm(pkg.NormConfig(features=M, norm_after=pkg.NORM_LAYER, block_type=1, stream_type=1, weight_type=1, eps=eps), x, after_bias=bias, sum=total)
+            torch.cuda.synchronize()
+            assert torch.equal(out, bias.expand_as(out)) and torch.equal(total, bias.expand_as(out))
+
+
 def test_numbers_that_are_none_stay_in_their_rows():
     import paper_2512_21487_amd as pkg
     inf, nan = float("inf"), float("nan")
