@@ -335,7 +335,7 @@ size_t moe_ep_linear_adapters_workspace_bytes(const moe_ep_linear_config *cfg, c
  *   scale      fp32 [n_adapters], or NULL (1)
  *   workspace  workspace_bytes bytes of device memory on 16 bytes, the call's own until `stream` has passed it: nothing in it has to be set, nothing is kept in it, and
  *              two calls that may overlap (on two streams, or in two graphs) need one each
- * x A^T is summed in fp32 and keeps 16 bits of mantissa on its way to B, 24 where out is fp32 (a row of x that is not finite may give NaN where the formula gives an infinity); the rest as for moe_ep_linear.  out and
+ * x A^T is summed in fp32 and keeps 24 bits of mantissa on its way to B (a row of x that is not finite may give NaN where the formula gives an infinity); the rest as for moe_ep_linear.  out and
  * workspace must not overlap anything else, but out the residual in place.  The call enqueues two kernels.  A row without an adapter has the product's formula; its bits may differ from
  * moe_ep_linear's, which may choose another kernel.
  */

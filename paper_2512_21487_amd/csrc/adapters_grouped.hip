@@ -6,7 +6,7 @@ namespace moe_ep {
 
 namespace {
 
-// A wavefront has a group of up to 16 rows and NB * 16 columns: x W^T of them, as the product left it, and the product of their x A^T (as `parts` bf16 numbers) with B, straight
+// A wavefront has a group of up to 16 rows and NB * 16 columns: x W^T of them, as the product left it, and the product of their x A^T (as kParts bf16 numbers) with B, straight
 // from memory in the order that the matrix instruction wants: 64 bytes of a row, 16 rows at a time.
 template <int NB>
 __global__ __launch_bounds__(256) void adapters_up_kernel(LinearArgs a, AdapterArgs x, const float* wide, const int32_t* table, int slices)
@@ -37,24 +37,22 @@ __global__ __launch_bounds__(256) void adapters_up_kernel(LinearArgs a, AdapterA
 #pragma unroll 4
         for (int k = kh * 8; k - kh * 8 < x.rank; k += 32) {
             const bool in = k < x.rank;
-            u32x4_t u[NB], l[3];
+            u32x4_t u[NB], l[kParts];
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 u[b] = u32x4_t{0, 0, 0, 0};
                 if (in) u[b] = *reinterpret_cast<const u32x4_t*>(up + (size_t)min(n0 + b * 16 + row, a.N - 1) * x.rank + k);
             }
 #pragma unroll
-            for (int p = 0; p < 3; ++p) {
+            for (int p = 0; p < kParts; ++p) {
                 l[p] = u32x4_t{0, 0, 0, 0};
-                if (in && there && p < x.parts) l[p] = *reinterpret_cast<const u32x4_t*>(low + p * x.rank + k);
+                if (in && there) l[p] = *reinterpret_cast<const u32x4_t*>(low + p * x.rank + k);
             }
 #pragma unroll
-            for (int p = 2; p >= 0; --p) {
-                if (p >= x.parts) continue;
+            for (int p = kParts - 1; p >= 0; --p)
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
                     v[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, u[b]), __builtin_bit_cast(bf16x8_t, l[p]), v[b], 0, 0, 0);
-            }
         }
     }
     e.store(m, there, v, res);

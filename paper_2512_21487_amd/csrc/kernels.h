@@ -252,13 +252,16 @@ struct AdapterArgs {
     const int32_t* index;               // of every row; one that is not in 0..n-1: none
     const uint16_t *down, *up;          // A [n, rank, K], B [n, N, rank]
     const float* scale;                 // [n] or NULL
-    uint16_t* low;                      // workspace [R, adapter_pitch(width)]: scale_a x A_a^T as `parts` bf16 numbers that add up to it, [parts, rank], of rows with an adapter; behind
+    uint16_t* low;                      // workspace [R, adapter_pitch(width)]: scale_a x A_a^T as three bf16 numbers that add up to it, [kParts, rank], of rows with an adapter; behind
                                         // `width` elements of every row 8 zeros
     int32_t* lists;                     // workspace: of every tile of `tile` rows, adapter_list(tile) numbers: how many adapters its rows have, each one's number and a bit for every row
-    int n, rank, parts, width, tile;
+    int n, rank, width, tile;
 };
-// reduction steps of 64 that an adapter adds to a tile
-inline int adapter_width(int rank, int parts) { return (rank * parts + 63) / 64 * 64; }
+// What x A^T is on its way to the matrix instruction: two bf16 numbers would leave 2^-16 of it, three leave what fp32 does.  Two / three, us: 1 x 5120 x 5120, rank 16, 14.6 / 14.7, 256 x
+// 4096 x 4096, rank 64, 27.6 / 28.0, 1531 x 1409 x 2049, rank 24, 43.4 / 45.3, 4096 x 5632 x 2048, rank 32, 112 / 119, 16384 x 5120 x 5120, rank 64, 723 / 737.
+constexpr int kParts = 3;
+// elements that an adapter adds to a tile's reduction, in steps of 64
+inline int adapter_width(int rank) { return (rank * kParts + 63) / 64 * 64; }
 __host__ __device__ constexpr int adapter_pitch(int width) { return width + 8; }
 __host__ __device__ constexpr int adapter_list(int tile) { return 1 + tile * (1 + (tile + 31) / 32); }
 constexpr int kRankMost = 128;

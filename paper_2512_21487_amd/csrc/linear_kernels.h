@@ -42,7 +42,7 @@ struct TileAdapters {
 __device__ __forceinline__ int rank_of_chunk(const AdapterArgs& x, int c)
 {
     const int per = x.rank >> 3;
-    return c < per * x.parts ? (c - per * (c / per)) * 8 : -1;
+    return c < per * kParts ? (c - per * (c / per)) * 8 : -1;
 }
 
 // 0.5 z (1 + erf(z / sqrt 2)).  1 - erf(x) for x >= 0 is a polynomial in 1 / (1 + p x) times exp(-x^2) to 1.5e-7 (Abramowitz and Stegun,
@@ -230,15 +230,15 @@ struct SplitCfg {
 // the upper halves of two words, of `a` in the low half
 __device__ __forceinline__ uint32_t upper_halves(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
 
-// A wavefront's 16 rows x 16 ranks of sums: a lane has 4 consecutive ranks of its row, r the first.  They are written as `parts` bf16 numbers each, 8 bits cut off the top at a
-// time and the last rounded.  Of a sum in 1..2 the first leaves less than 2^-7, what rounds that to 8 bits half a step, 2^-16 at most: 2^-8 of what rounding the result to bf16
-// leaves.  With one cut more 2^-24 are left (results in fp32).
+// A wavefront's 16 rows x 16 ranks of sums: a lane has 4 consecutive ranks of its row, r the first.  They are written as kParts bf16 numbers each, 8 bits cut off the top at a
+// time and the last rounded.  Of a sum in 1..2 the first leaves less than 2^-7, the second less than 2^-15, what rounds that to 8 bits half a step, 2^-24 at most: as much as fp32 itself.
 __device__ __forceinline__ void store_low(const AdapterArgs& x, long long row, int r, f32x4_t v)
 {
     uint16_t* const to = x.low + row * adapter_pitch(x.width) + r;
-    for (int p = 0; p < x.parts; ++p) {
+#pragma unroll
+    for (int p = 0; p < kParts; ++p) {
         u32x2_t u;
-        if (p + 1 == x.parts) u = u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+        if (p + 1 == kParts) u = u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
         else {
             u = u32x2_t{upper_halves(v[0], v[1]), upper_halves(v[2], v[3])};
 #pragma unroll

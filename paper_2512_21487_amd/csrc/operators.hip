@@ -125,9 +125,6 @@ struct Product {
     }
 };
 
-// bf16 numbers that stand for one of x A^T
-int parts_of(const moe_ep_linear_config& c) { return c.out_type == MOE_EP_F32 ? 3 : 2; }
-
 // What the workspace holds: x A^T of every row; behind it, of up to kGathered rows, x W^T in fp32 and the groups' table, of more the lists of the row tiles and, where rows are
 // not on 16 bytes, copies of x and of W that are.  A tile has 16 to 256 rows: (R / t + 1)
 // (1 + t (1 + t / 32)) numbers are at most those of t = 256 and one more for 16 rows.
@@ -136,7 +133,7 @@ struct AdapterWorkspace {
     AdapterWorkspace(const moe_ep_linear_config& c, const moe_ep_adapter_config& ad, int32_t n_rows)
     {
         const int few = n_rows < kGathered ? n_rows : kGathered;
-        low = (size_t)n_rows * adapter_pitch(adapter_width(ad.rank, parts_of(c))) * 2;
+        low = (size_t)n_rows * adapter_pitch(adapter_width(ad.rank)) * 2;
         wide = ((size_t)few * c.out_features * 4 + 15) / 16 * 16;
         table = (size_t)adapter_groups(few, ad.n_adapters) * kGroupEntry * 4;
         lists = (((size_t)n_rows * 9 + n_rows / 16 + adapter_list(256) + 1) * 4 + 15) / 16 * 16;
@@ -291,7 +288,7 @@ int moe_ep_linear_adapters(const moe_ep_linear_config* c, const moe_ep_adapter_c
     AdapterArgs a{};
     a.index = index; a.down = static_cast<const uint16_t*>(down); a.up = static_cast<const uint16_t*>(up); a.scale = scale;
     a.low = static_cast<uint16_t*>(workspace);
-    a.n = ad->n_adapters; a.rank = ad->rank; a.parts = parts_of(*c); a.width = adapter_width(a.rank, a.parts);
+    a.n = ad->n_adapters; a.rank = ad->rank; a.width = adapter_width(a.rank);
     const AdapterWorkspace parts(*c, *ad, n_rows);
     char* const behind = static_cast<char*>(workspace) + parts.low;
     if (n_rows <= kGathered)
