@@ -388,7 +388,8 @@ int moe_ep_validate_norm(const moe_ep_norm_config *cfg, const char **why);
  *   n_rows     0..2^30
  * sum and out must not overlap anything else, nor each other (rows of the same distance may lie side by side).  Everything is computed in fp32 from h as it
  * is, not as `sum` holds it, and each result is rounded once.  A row with a number that is not finite gives what the formula gives in fp32; in a
- * norm, squares and sums beyond fp32 do no harm.  Rows do not depend on each other; the same call gives the same bits.
+ * norm, squares and sums beyond fp32 do no harm, and a mean that is large beside the spread is taken out until it is not: a layer norm of fp32 numbers is off by (M / 64 + 24) 2^-24 of 1 and of its
+ * result at most, and of a row of equal numbers leaves the bias and a quarter of that.  Rows do not depend on each other; the same call gives the same bits.
  * Alignment, what lies between rows, streams, graphs, devices, checks, `why` and n_rows == 0 as for moe_ep_linear.
  */
 int moe_ep_norm(const moe_ep_norm_config *cfg, const void *block, const void *residual, const void *gate, const void *after_weight,

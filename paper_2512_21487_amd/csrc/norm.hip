@@ -62,77 +62,118 @@ __device__ __forceinline__ void store8(char* row, int col, bool wide, int left, 
 struct Add { __device__ float operator()(float a, float b) const { return a + b; } };
 struct Larger { __device__ float operator()(float a, float b) const { return fmaxf(a, b); } };   // of two numbers where one is NaN, the other
 
-// over the WAVES wavefronts of a row, the same bits in every lane
-template <int WAVES, class Op>
-__device__ __forceinline__ float over_row(float v, float* lds, int& turn, Op op)
+// N numbers over the WAVES wavefronts of a row, the same bits in every lane
+constexpr int kOverRow = 2;
+template <int WAVES, int N, class Op>
+__device__ __forceinline__ void over_row(float (&v)[N], float* lds, int& turn, Op op)
 {
+    static_assert(N <= kOverRow, "norm_kernel's LDS");
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v = op(v, __shfl_xor(v, d, 64));
+    for (int d = 1; d < 64; d <<= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = op(v[i], __shfl_xor(v[i], d, 64));
     if constexpr (WAVES > 1) {
         // two places in turn: who is at the next reduction has left this one's barrier, which everybody reaches behind reading the last one's
-        float* const at = lds + (turn & 1) * WAVES;
+        float* const at = lds + (turn & 1) * (kOverRow * WAVES);
         ++turn;
-        if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = at[0];
+        if ((threadIdx.x & 63) == 0)
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) v = op(v, at[w]);
+            for (int i = 0; i < N; ++i) at[i * WAVES + (threadIdx.x >> 6)] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = at[i * WAVES];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) v[i] = op(v[i], at[i * WAVES + w]);
+        }
     }
-    return v;
+}
+
+template <int WAVES, int V>
+__device__ __forceinline__ float mean_of(const float (&x)[V][8], float each, float* lds, int& turn)
+{
+    float s[1] = {0.f};
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[0] += x[v][i];
+    over_row<WAVES>(s, lds, turn, Add());
+    return s[0] * each;
 }
 
 // x <- (x - mean) / sqrt(mean((x - mean)^2) + eps); RMS: without the mean.  The mean is taken out before the squares are summed, so that nothing cancels.
+// What the mean is off by, a few steps of it, is all that is left of a row of equal numbers: the sum of what is left comes with that of its squares and is taken out too, from
+// the row once more if it is a quarter of the result's unit or more.  So results are off by steps of their own, M / 64 + 20 at most, however large the mean is beside the spread.
 // Where squares or sums leave fp32 while the row's numbers do not, its largest is between 2^56 (its square times 32768 is 2^127) and 2^128: times 2^-72 neither
 // they nor anything that counts beside them is lost, and eps, which does not count there, goes with it, but to no less than a normal number: numbers that are all the
 // mean have nothing else below the square root.  Such a row costs two or three reductions more.
-template <int WAVES, int V>
-__device__ __forceinline__ void normalise(float (&x)[V][8], const int (&left)[V], int cols, int kind, float eps, float* lds, int& turn)
+// (Without / with the sum of what is left, us: 1531 x 1409, fp32 stream, layer norms on both sides, 11.4 / 12.1.)
+template <bool LAYER, int WAVES, int V>
+__device__ __forceinline__ void normalise_as(float (&x)[V][8], const int (&left)[V], int cols, float eps, float* lds, int& turn)
 {
+#pragma clang fp contract(off)   // the same differences from the mean everywhere
     const float each = 1.0f / (float)cols;
-    for (int scaled = 0;; ++scaled) {
-        float mean = 0.f;
-        if (kind == kNormLayer) {
-            float s = 0.f;
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) s += x[v][i];
-            mean = over_row<WAVES>(s, lds, turn, Add()) * each;
-        }
-        float q = 0.f;
+    float mean = 0.f, rest = 0.f, power = 0.f;
+    if constexpr (LAYER) mean = mean_of<WAVES, V>(x, each, lds, turn);
+    bool scaled = false;
+    // a pass leaves 2^-15 of a mean or less, and 2^128 is 2^201 from the root of the least eps
+    for (int pass = 0; pass < 16; ++pass) {
+        float s[LAYER ? 2 : 1] = {};
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float d = i < left[v] ? x[v][i] - mean : 0.f;
-                q = fmaf(d, d, q);
+                s[0] = fmaf(d, d, s[0]);
+                if constexpr (LAYER) s[1] += d;
             }
-        const float power = over_row<WAVES>(q, lds, turn, Add()) * each;
-        if (scaled == 0 && !(power <= __FLT_MAX__)) {
-            float top = 0.f;
+        over_row<WAVES>(s, lds, turn, Add());
+        power = s[0] * each;
+        if (!scaled && !(power <= __FLT_MAX__)) {
+            float top[1] = {0.f};
 #pragma unroll
             for (int v = 0; v < V; ++v)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[v][i]));
-            top = over_row<WAVES>(top, lds, turn, Larger());
+                for (int i = 0; i < 8; ++i) top[0] = fmaxf(top[0], fabsf(x[v][i]));
+            over_row<WAVES>(top, lds, turn, Larger());
             // a number that is none, or infinite: as the formula has it
-            if (top <= __FLT_MAX__) {
-                constexpr float s = 0x1p-72f;
+            if (top[0] <= __FLT_MAX__) {
+                constexpr float by = 0x1p-72f;
 #pragma unroll
                 for (int v = 0; v < V; ++v)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) x[v][i] *= s;
-                eps = fmaxf(eps * s * s, __FLT_MIN__);
+                    for (int i = 0; i < 8; ++i) x[v][i] *= by;
+                eps = fmaxf(eps * by * by, __FLT_MIN__);
+                scaled = true;
+                if constexpr (LAYER) mean = mean_of<WAVES, V>(x, each, lds, turn);
                 continue;
             }
         }
-        const float r = __builtin_amdgcn_rsqf(power + eps);
+        if constexpr (!LAYER) break;
+        else {
+            rest = s[1] * each;
+            const float spread = fmaf(-rest, rest, power);
+            power = spread < 0.f ? 0.f : spread;
+            if (!(rest * rest > 0.0625f * (power + eps))) break;
 #pragma unroll
-        for (int v = 0; v < V; ++v)
+            for (int v = 0; v < V; ++v)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[v][i] = (x[v][i] - mean) * r;
-        return;
+                for (int i = 0; i < 8; ++i) x[v][i] -= mean;
+            mean = rest;
+        }
     }
+    const float r = __builtin_amdgcn_rsqf(power + eps);
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[v][i] = (LAYER ? x[v][i] - mean - rest : x[v][i]) * r;
+}
+
+template <int WAVES, int V>
+__device__ __forceinline__ void normalise(float (&x)[V][8], const int (&left)[V], int cols, int kind, float eps, float* lds, int& turn)
+{
+    if (kind == kNormLayer) normalise_as<true, WAVES, V>(x, left, cols, eps, lds, turn);
+    else normalise_as<false, WAVES, V>(x, left, cols, eps, lds, turn);
 }
 
 // A weight and a bias of 8 features
@@ -169,13 +210,13 @@ __device__ __forceinline__ float gate_of(float g, int form)
 
 // WAVES wavefronts have a row, a lane 8 elements of it in each of V turns.  WIDE: the block, the stream or the gate is fp32.  EARLY: weights and biases are asked for
 // with the row, not behind the sums in front of them.
-// Of many rows memory bounds it: 16384 x 5120, bf16, residual and norm in front, 123 us for 671 MB, 5.5 TB/s (a copy of 1 GiB: 5.1); of few the chain of load, sum
+// Of many rows memory bounds it: 16384 x 5120, bf16, residual and norm in front, 125 us for 671 MB, 5.4 TB/s (a copy of 1 GiB: 5.1); of few the chain of load, sum
 // over wavefronts, square root, store: 1 x 5120 3.8 us, 5.0 with norms on both sides and nothing in L2.
 template <int WAVES, int V, bool WIDE, bool EARLY>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(NormArgs a)
 {
     constexpr int ROWS = WAVES == 1 ? 4 : 1;
-    __shared__ float lds[2 * WAVES];
+    __shared__ float lds[2 * kOverRow * WAVES];
     int turn = 0;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
     const long long m = workgroup() * ROWS + (WAVES == 1 ? wave : 0);
