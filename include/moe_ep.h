@@ -330,8 +330,8 @@ size_t moe_ep_linear_adapters_workspace_bytes(const moe_ep_linear_config *cfg, c
  *   index      int32 [n_rows], device memory: a row's adapter; any number outside 0..n_adapters - 1: no adapter.  Rows in any order.  Up to 768 rows are
  *              grouped by adapter; of more, those of one adapter that lie together (a prompt's, say) cost least: of up to 256 rows that share a tile, every adapter adds 64
  *              elements or more to K
- *   down, up   bf16 [n_adapters, rank, K] and [n_adapters, N, rank], A and B, without gaps; `up` on 16 bytes.  Of the adapters that `index` names they must
- *              be finite: one that is not may give NaN in rows of others too
+ *   down, up   bf16 [n_adapters, rank, K] and [n_adapters, N, rank], A and B, without gaps; `up` on 16 bytes.  A number of an adapter's that is not
+ *              finite reaches rows of that adapter alone, where it gives NaN or what the formula gives
  *   scale      fp32 [n_adapters], or NULL (1)
  *   workspace  workspace_bytes bytes of device memory on 16 bytes, the call's own until `stream` has passed it: nothing in it has to be set, nothing is kept in it, and
  *              two calls that may overlap (on two streams, or in two graphs) need one each

@@ -8,21 +8,6 @@ namespace moe_ep {
 
 namespace {
 
-// The adapters of up to 64 rows, one a lane, in the order of their first rows: next() gives one after the other, and which lanes have it.
-struct Distinct {
-    int mine;
-    unsigned long long left;
-    __device__ __forceinline__ explicit Distinct(int adapter) : mine(adapter), left(__ballot(adapter >= 0)) {}
-    __device__ __forceinline__ bool next(int& adapter, unsigned long long& who)
-    {
-        if (!left) return false;
-        adapter = __builtin_amdgcn_readlane(mine, __builtin_ctzll(left));
-        who = __ballot(mine == adapter);
-        left &= ~who;
-        return true;
-    }
-};
-
 // the list of a tile of up to 256 rows, by one wavefront
 __device__ __forceinline__ void make_list(const LinearArgs& a, const AdapterArgs& x, long long tile, int lane)
 {

@@ -255,6 +255,7 @@ struct AdapterArgs {
     uint16_t* low;                      // workspace [R, adapter_pitch(width)]: scale_a x A_a^T as three bf16 numbers that add up to it, [kParts, rank], of rows with an adapter; behind
                                         // `width` elements of every row 8 zeros
     int32_t* lists;                     // workspace: of every tile of `tile` rows, adapter_list(tile) numbers: how many adapters its rows have, each one's number and a bit for every row
+    uint16_t* none;                     // workspace: a bit for every row of a tile whose results are made again: ceil(R / 16) x ceil(N / 32) numbers of 16 bits
     int n, rank, width, tile;
 };
 // What x A^T is on its way to the matrix instruction: two bf16 numbers would leave 2^-16 of it, three leave what fp32 does.  Two / three, us: 1 x 5120 x 5120, rank 16, 14.6 / 14.7, 256 x

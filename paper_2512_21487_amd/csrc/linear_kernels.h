@@ -416,6 +416,72 @@ __device__ __forceinline__ void down_group(const LinearArgs& a, const GroupArgs&
 constexpr int group_lds(int waves) { return waves * SplitCfg<1, 1, false>::BYTES + 16 * 4 + kGathered / 64 * 8; }
 static_assert(2 * kGathered * 4 <= 4 * SplitCfg<1, 1, false>::BYTES, "the rows' adapters and counts are where down()'s operands come");
 
+// The adapters of up to 64 rows, one a lane, in the order of their first rows: next() gives one after the other, and which lanes have it.
+struct Distinct {
+    int mine;
+    unsigned long long left;
+    __device__ __forceinline__ explicit Distinct(int adapter) : mine(adapter), left(__ballot(adapter >= 0)) {}
+    __device__ __forceinline__ bool next(int& adapter, unsigned long long& who)
+    {
+        if (!left) return false;
+        adapter = __builtin_amdgcn_readlane(mine, __builtin_ctzll(left));
+        who = __ballot(mine == adapter);
+        left &= ~who;
+        return true;
+    }
+};
+
+// ---- adapters that hold a number that is none
+
+// 16 rows x 16 columns by themselves, straight from memory: x W^T, and x A^T B^T of each row's own adapter alone.  A lane has what a matrix instruction gives it.
+__device__ __forceinline__ f32x4_t block_alone(const LinearArgs& a, const AdapterArgs& x, int lane, int m0, int n0)
+{
+    const int row = lane & 15, kh = lane >> 4, m = min(m0 + row, a.R - 1), n = min(n0 + row, a.N - 1);
+    const uint16_t *const xp = a.x + (size_t)m * a.ldx, *const wp = static_cast<const uint16_t*>(a.w) + (size_t)n * a.ldw;
+    f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int k = kh * 8; k - kh * 8 < a.K; k += 32)
+        v = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, load_part<8>(wp + k, a.K - k, a.K)), __builtin_bit_cast(bf16x8_t, load_part<8>(xp + k, a.K - k, a.K)), v, 0, 0, 0);
+    Distinct own(adapter_of(x, m));
+    int adapter;
+    unsigned long long who;
+    while (own.next(adapter, who)) {
+        const bool its = own.mine == adapter;
+        const uint16_t *const low = x.low + (size_t)m * adapter_pitch(x.width), *const up = x.up + ((size_t)adapter * a.N + n) * x.rank;
+        f32x4_t t = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+        for (int k = kh * 8; k - kh * 8 < x.rank; k += 32)
+#pragma unroll 1
+            for (int p = 0; p < kParts; ++p) {
+                u32x4_t u = {0, 0, 0, 0}, l = {0, 0, 0, 0};
+                if (k < x.rank) u = *reinterpret_cast<const u32x4_t*>(up + k);
+                if (k < x.rank && its) l = *reinterpret_cast<const u32x4_t*>(low + p * x.rank + k);
+                t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, u), __builtin_bit_cast(bf16x8_t, l), t, 0, 0, 0);
+            }
+        if (its) v += t;   // of the others' rows t is 0 times B, which is none where B is
+    }
+    return v;
+}
+
+// B of every adapter that a tile has is multiplied with rows of all, zeros in those that have another: a number of it that is none would leave none in their results.  Rows with results
+// that are none are made again, without the others (rows in which all are numbers keep their bits).  Looking at the sums costs 1531 x 1409 x 2049 45 -> 46 us, 4096 x 5632 x 2048 116.5 -> 119.6, 16384 x
+// 5120 x 5120 735 -> 738 (all of a tile's before its first are stored, in place of a row of blocks at a time: 45, 120 and 830, spilled).  Which of 16 rows have such a result in NB blocks of
+// columns, a bit each:
+template <int NB>
+__device__ __forceinline__ uint32_t rows_with_none(const f32x4_t (&v)[NB])
+{
+    // (of two numbers one of which is NaN, maximum gives that)
+    float most[2] = {0.f, 0.f};
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) most[i] = __builtin_elementwise_maximum(__builtin_elementwise_maximum(most[i], __builtin_fabsf(v[b][2 * i])), __builtin_fabsf(v[b][2 * i + 1]));
+    const unsigned long long lanes = __ballot(!(__builtin_elementwise_maximum(most[0], most[1]) <= __FLT_MAX__));
+    return (uint32_t)(lanes | lanes >> 16 | lanes >> 32 | lanes >> 48) & 0xffffu;
+}
+// The bits of the blocks from row m and column n on, as a tile leaves them in the workspace
+__device__ __forceinline__ uint16_t* none_at(const LinearArgs& a, const AdapterArgs& x, int m, int n) { return x.none + (size_t)(m >> 4) * ((a.N + 31) >> 5) + (n >> 5); }
+
 // how many workgroups of a launch are in front of the product's
 template <class X>
 __host__ __device__ __forceinline__ int in_front_of(const X& x)
@@ -676,6 +742,15 @@ __global__ __launch_bounds__(WAVES * 64) void linear_split_kernel(LinearArgs a, 
 #pragma unroll
             for (int w = 1; w < WAVES; ++w) v[j] += at[w * (C::BYTES / 16)];
         }
+        if constexpr (X::on)
+            if (tile.count && rows_with_none<NB>(v))
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    const f32x4_t alone = block_alone(a, x, lane, m0 + i * 16, n0 + j * 16);
+                    const f32x4_t sum = v[j];
+                    const bool none = sum[0] * 0.f + sum[1] * 0.f + sum[2] * 0.f + sum[3] * 0.f != 0.f;
+                    v[j] = none ? alone : sum;
+                }
         e.store(m, m < a.R, v, res);
     }
 }
@@ -789,8 +864,10 @@ struct TileEpilogue {
             if (a.out32) r.v[p][1] = *reinterpret_cast<const u32x4_any2*>(at + 16);
         }
     }
-    __device__ __forceinline__ void store(int mb, f32x4_t (&v)[NB], const Residual& res) const
+    // without: a bit for each of the 16 rows that is not stored
+    __device__ __forceinline__ void store(int mb, f32x4_t (&v)[NB], const Residual& res, uint32_t without) const
     {
+        const auto stored = [&](int p) { return there(mb, p) && !(without >> (p * ROWS + r0) & 1); };
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             v[b] += bias[b];
@@ -802,7 +879,7 @@ struct TileEpilogue {
         for (int p = 0; p < PASSES; ++p) {
             const uint32_t from = (read ^ (p * ROWS & 7) * 16) + p * ROWS * COLS * 4;
             f32x4_t lo = *reinterpret_cast<const f32x4_t*>(sums + from), hi = *reinterpret_cast<const f32x4_t*>(sums + (from ^ 16u));
-            if (!there(mb, p) || left < 8) continue;
+            if (!stored(p) || left < 8) continue;
             if (a.residual) {
                 const u32x4_t r = res.v[p][0];
                 if (a.out32) {
@@ -822,7 +899,7 @@ struct TileEpilogue {
         if (left > 0 && left < 8) {   // the last columns, one by one
 #pragma unroll 1
             for (int p = 0; p < PASSES; ++p) {
-                if (!there(mb, p)) break;
+                if (!stored(p)) continue;
                 const uint32_t from = (read ^ (p * ROWS & 7) * 16) + p * ROWS * COLS * 4, row = mb * 16 + p * ROWS;
                 const char* const r = res_at + (res_off + row * (uint32_t)a.ldr * (a.out32 ? 4u : 2u));
                 char* const to = out_at + (out_off + row * (uint32_t)a.ldo * (a.out32 ? 4u : 2u));
@@ -902,7 +979,7 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a, X 
         }
     };
     // Step ks, behind K, is one of an adapter's: the loads go on as they are, from other places.  Rows of another adapter or none, and what is beyond the last part, read the
-    // zeros behind a row of `low`; what they are multiplied with, B's rows and columns that are there, is finite.
+    // zeros behind a row of `low`, which are multiplied with B's rows and columns that are there (rows_with_none() is for those that are no numbers).
     const auto aim_adapter = [&](int ks) __attribute__((always_inline)) {
         if constexpr (X::on) {
             static_assert(C::NW == 4, "a wavefront's regions are 32 rows apart, all even or all odd");
@@ -974,6 +1051,8 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a, X 
     int ring = 0, ki = 0, next_m0 = m0, next_n0 = n0;   // ki: the K step whose loads start at the next hand-over
     bool more = true;                                    // there is a tile behind the one that is multiplied
     int tile_steps = steps;                              // of the tile that is multiplied
+    uint32_t some_none = 0, rows_none = 0;               // rows of this wavefront's were not stored; of the tile, a lane has those of its row of blocks
+    int first_none = -1;                                 // the first tile with such
     const auto advance = [&]() __attribute__((always_inline)) {
         if (ki == steps) {
             more = tile_at(it + 1, next_m0, next_n0);
@@ -1046,8 +1125,23 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a, X 
             if (a.residual && mb + 1 < MB) e.fetch(mb + 1, ahead);
             f32x4_t v[NB];
             row_of_blocks<0, MB, NB>(mb, acc, v);
-            e.store(mb, v, res);
+            uint32_t none = 0;
+            if constexpr (X::on) {
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) asm volatile("" : "+v"(v[nb]));   // or the compiler looks at every row of blocks in a branch of its own
+                none = tile_steps > KT ? rows_with_none<NB>(v) : 0u;
+                some_none |= none;
+                rows_none = lane == mb ? none : rows_none;
+            }
+            e.store(mb, v, res, none);
         }
+        if constexpr (X::on)
+            if (__builtin_expect(some_none != 0, 0)) {
+                // of this tile, and of all behind the first that has any
+                const int m = m0 + wm * C::WTM + lane * 16, n = n0 + wn * C::WTN;
+                if (lane < MB && m < a.R && n < a.N) *none_at(a, x, m, n) = (uint16_t)rows_none;
+                if (first_none < 0) first_none = it;
+            }
         if (!more) break;
         m0 = next_m0;
         n0 = next_n0;
@@ -1055,6 +1149,31 @@ __global__ __launch_bounds__(256, OCC) void linear_tiled_kernel(LinearArgs a, X 
         ++it;
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);   // no load may land in LDS that is another workgroup's by then
+    if constexpr (X::on) {
+        // rows that were not stored, now that no accumulator is held (where they are found, 256 x 256 tiles would spill 62 to 101 registers instead of 11 to 25)
+        if (__builtin_expect(first_none < 0, 1)) return;
+        for (it = first_none; tile_at(it, m0, n0); ++it) {
+            tile.aim(x, m0 / BM);
+            const int m = m0 + wm * C::WTM, n = n0 + wn * C::WTN;
+            if (!tile.count || n >= a.N) continue;
+            const TileEpilogue<MB, C::WTN, ACT> e(a, lds + SLOTS * C::SLOT_BYTES + wave * C::SUM_BYTES, lane, m, n);
+#pragma unroll 1
+            for (int mb = 0; mb < MB && m + mb * 16 < a.R; ++mb) {
+                const uint32_t none = __builtin_amdgcn_readfirstlane((int)*static_cast<volatile const uint16_t*>(none_at(a, x, m + mb * 16, n)));
+                if (!none) continue;
+                typename TileEpilogue<MB, C::WTN, ACT>::Residual res;
+                if (a.residual) e.fetch(mb, res);
+                f32x4_t v[NB];
+#pragma unroll 1
+                for (int b = 0; b < NB; ++b) {
+                    const f32x4_t u = block_alone(a, x, lane, m + mb * 16, n + b * 16);
+#pragma unroll
+                    for (int c = 0; c < NB; ++c) v[c] = c == b ? u : v[c];
+                }
+                e.store(mb, v, res, ~none);
+            }
+        }
+    }
 }
 
 template <int BM, int BN, int SLOTS, int OCC, bool RAGGED, bool ACT, bool STAGED, class X>

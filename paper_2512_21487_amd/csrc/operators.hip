@@ -125,11 +125,11 @@ struct Product {
     }
 };
 
-// What the workspace holds: x A^T of every row; behind it, of up to kGathered rows, x W^T in fp32 and the groups' table, of more the lists of the row tiles and, where rows are
+// What the workspace holds: x A^T of every row; behind it, of up to kGathered rows, x W^T in fp32 and the groups' table, of more the lists of the row tiles, a bit for every row of a tile and, where rows are
 // not on 16 bytes, copies of x and of W that are.  A tile has 16 to 256 rows: (R / t + 1)
 // (1 + t (1 + t / 32)) numbers are at most those of t = 256 and one more for 16 rows.
 struct AdapterWorkspace {
-    size_t low, wide, table, lists, x, w;
+    size_t low, wide, table, lists, none, x, w;
     AdapterWorkspace(const moe_ep_linear_config& c, const moe_ep_adapter_config& ad, int32_t n_rows)
     {
         const int few = n_rows < kGathered ? n_rows : kGathered;
@@ -137,12 +137,13 @@ struct AdapterWorkspace {
         wide = ((size_t)few * c.out_features * 4 + 15) / 16 * 16;
         table = (size_t)adapter_groups(few, ad.n_adapters) * kGroupEntry * 4;
         lists = (((size_t)n_rows * 9 + n_rows / 16 + adapter_list(256) + 1) * 4 + 15) / 16 * 16;
+        none = n_rows > kGathered ? (((size_t)n_rows + 15) / 16 * (((size_t)c.out_features + 31) / 32) * 2 + 15) / 16 * 16 : 0;
         const int K = c.in_features;
         const size_t row = (size_t)adapter_pitch_of(K) * 2;
         x = n_rows > kGathered && rows_off_16(K, c.x_stride ? c.x_stride : K) ? n_rows * row : 0;
         w = n_rows > kGathered && rows_off_16(K, c.weight_stride ? c.weight_stride : K) ? c.out_features * row : 0;
     }
-    size_t bytes() const { return low + (wide + table > lists + x + w ? wide + table : lists + x + w); }   // of more rows not fewer: that holds of each
+    size_t bytes() const { return low + (wide + table > lists + none + x + w ? wide + table : lists + none + x + w); }   // of more rows not fewer: that holds of each
 };
 
 }  // namespace
@@ -295,7 +296,8 @@ int moe_ep_linear_adapters(const moe_ep_linear_config* c, const moe_ep_adapter_c
         e = launch_linear_grouped(p.args, a, reinterpret_cast<float*>(behind), reinterpret_cast<int32_t*>(behind + parts.wide), n_cu, static_cast<hipStream_t>(stream));
     else {
         a.lists = reinterpret_cast<int32_t*>(behind);
-        char* const copies = behind + parts.lists;
+        a.none = reinterpret_cast<uint16_t*>(behind + parts.lists);
+        char* const copies = behind + parts.lists + parts.none;
         e = launch_linear_adapters(p.args, a, parts.x ? reinterpret_cast<uint16_t*>(copies) : nullptr, parts.w ? reinterpret_cast<uint16_t*>(copies + parts.x) : nullptr, n_cu,
                                    static_cast<hipStream_t>(stream));
     }
