@@ -478,11 +478,25 @@ def linear_adapters_workspace_bytes(cfg: LinearConfig, adapters: AdapterConfig, 
     return int(load_library().moe_ep_linear_adapters_workspace_bytes(ctypes.byref(cfg), ctypes.byref(adapters), n_rows))
 
 
+def _matrices(x, name: str, n: int, rows: int, cols: int, device: int) -> Optional[int]:
+    """Address of n bf16 matrices without gaps: [n, rows, cols], its rows one behind another [n rows, cols], or flat."""
+    if x is not None:
+        try:
+            have = x.shape
+        except AttributeError:
+            return _ptr(x)
+        fits = (have[0] >= n and have[1] == rows and have[2] == cols if len(have) == 3 else have[0] >= n * rows and have[1] == cols if len(have) == 2
+                else len(have) == 1)
+        if not fits:
+            raise ValueError(f"{name} must be [{n}, {rows}, {cols}], got {tuple(have)}")
+    return _vector(x, name, n * rows * cols, BF16, device)
+
+
 def linear_adapters(cfg: LinearConfig, adapters: AdapterConfig, x, weight, index, down, up, scale=None, bias=None, residual=None, out=None, workspace=None,
                     n_rows: Optional[int] = None, workspace_bytes: Optional[int] = None, stream: Optional[int] = None) -> int:
     """moe_ep_linear_adapters: out = act(x weight^T + bias + scale[a] (x down[a]^T) up[a]^T) + residual, a = index[row].
 
-    ``workspace`` is a contiguous tensor of at least ``linear_adapters_workspace_bytes`` bytes (a raw address comes with ``workspace_bytes``)."""
+    ``down`` is [n_adapters, rank, K], ``up`` [n_adapters, N, rank]; ``workspace`` is a contiguous tensor of at least ``linear_adapters_workspace_bytes`` bytes (a raw address comes with ``workspace_bytes``)."""
     if n_rows is None:
         n_rows = int(x.shape[0])
     if not 0 <= n_rows <= _MOST_ROWS:
@@ -506,7 +520,7 @@ def linear_adapters(cfg: LinearConfig, adapters: AdapterConfig, x, weight, index
         ctypes.byref(cfg), ctypes.byref(adapters), _rows(x, "x", n_rows, K, cfg.x_stride or K, BF16, at),
         _rows(weight, "weight", N, K, cfg.weight_stride or K, F32 if cfg.weight_type else BF16, at), _vector(bias, "bias", N, F32, at),
         _rows(residual, "residual", n_rows, N, cfg.residual_stride or N, result, at), _vector(index, "index", n_rows, _I32, at),
-        _vector(down, "down", n * rank * K, BF16, at), _vector(up, "up", n * rank * N, BF16, at), _vector(scale, "scale", n, F32, at), n_rows,
+        _matrices(down, "down", n, rank, K, at), _matrices(up, "up", n, N, rank, at), _vector(scale, "scale", n, F32, at), n_rows,
         _rows(out, "out", n_rows, N, cfg.out_stride or N, result, at), _ptr(workspace), workspace_bytes or 0, stream, ctypes.byref(why))
     if rc != 0:
         raise MoeEpError(rc, (why.value or b"").decode())

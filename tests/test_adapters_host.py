@@ -100,3 +100,18 @@ def test_tensors_that_are_refused():
             call(kw)
     with pytest.raises(ValueError, match="workspace_bytes"):
         call(dict(workspace_bytes=None))
+
+
+@pytest.mark.parametrize("name,shape,fits", [
+    ("down", (4, 16, 64), True), ("down", (5, 16, 64), True), ("down", (64, 64), True), ("down", (4 * 16 * 64,), True), ("down", (4, 64, 16), False), ("down", (4, 32, 64), False),
+    ("down", (16, 4, 64), False), ("down", (4, 16, 128), False), ("down", (3, 16, 64), False), ("down", (4, 1024), False), ("down", (1, 4, 16, 64), False),
+    ("up", (4, 32, 16), True), ("up", (6, 32, 16), True), ("up", (128, 16), True), ("up", (4, 16, 32), False), ("up", (16, 128), False), ("up", (4, 64, 16), False),
+    ("up", (4, 32, 32), False), ("up", (3, 32, 16), False)])
+def test_adapters_whose_shape_is_another(name, shape, fits):
+    """As many elements in another order would give other numbers."""
+    torch = pytest.importorskip("torch")
+    both = dict(down=D, up=E)
+    both[name] = torch.zeros(shape, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match=name) as ei:   # one that fits is refused for being on the host
+        call(both)
+    assert ("must be [" in str(ei.value)) == (not fits)
