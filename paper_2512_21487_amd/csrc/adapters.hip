@@ -131,36 +131,46 @@ hipError_t launch_adapters_down(const LinearArgs& a, const AdapterArgs& x, const
 
 }  // namespace
 
+int adapter_plan(const LinearArgs& a, int n_cu, bool* copies)
+{
+    const bool of_x = rows_off_16(a.K, a.ldx), of_w = rows_off_16(a.K, a.ldw);
+    LinearArgs copied = a;
+    if (of_x || of_w) copied.K = adapter_pitch_of(a.K);
+    if (of_x) { copied.x = nullptr; copied.ldx = copied.K; }   // on 16 bytes, wherever
+    if (of_w) { copied.w = nullptr; copied.ldw = copied.K; }
+    const int kernel = adapter_kernel(copied, n_cu);
+    // Only where the product is then one of tiles filled by direct loads.  Else the operands are taken as they are, by what is chosen for such.  (Of a short K the shared reduction
+    // in tiles of 64 x 32, which copies would have led to, takes them as well, but is no better where there are many tiles.  That choice / that reduction, us: 1531 x 1409 x 131 19 / 26, 4100 x 700 x 65 21 / 27,
+    // 7933 x 299 x 131 23 / 31, 2000 x 2048 x 192, rows 195 apart, 22 / 26; of few 800 x 1100 x 129 19 / 14, 5692 x 128 x 131 22 / 17, 2000 x 299 x 130 18 / 14.)
+    *copies = (of_x || of_w) && kernel >= kLinearTiled && kernel < kLinearStaged128x64;
+    return *copies || !(of_x || of_w) ? kernel : adapter_kernel(a, n_cu);
+}
+
 hipError_t launch_linear_adapters(const LinearArgs& a, AdapterArgs x, uint16_t* aligned_x, uint16_t* aligned_w, int n_cu, hipStream_t s)
 {
     if (a.R <= 0) return hipSuccess;
     if (a.N < 1 || a.K < 1 || a.w32 || x.n < 1 || x.rank < 8 || x.rank > kRankMost || x.rank % 8) return hipErrorInvalidValue;
+    if ((aligned_x != nullptr) != rows_off_16(a.K, a.ldx) || (aligned_w != nullptr) != rows_off_16(a.K, a.ldw)) return hipErrorInvalidValue;
     LinearArgs product = a;
     AlignArgs c{};
-    c.K = a.K;
-    c.pitch = adapter_pitch_of(a.K);
-    if (aligned_x) {
-        c.x = {a.x, aligned_x, a.ldx, a.R};
-        product.x = aligned_x;
-        product.ldx = c.pitch;
-    }
-    if (aligned_w) {
-        c.w = {static_cast<const uint16_t*>(a.w), aligned_w, a.ldw, a.N};
-        product.w = aligned_w;
-        product.ldw = c.pitch;
-    }
-    product.K = c.pitch;
-    int kernel = adapter_kernel(product, n_cu);
-    // only where the product is then one of tiles filled by direct loads
-    if (aligned_x || aligned_w) {
-        if (kernel >= kLinearTiled && kernel < kLinearStaged128x64) {
-            c.workgroups = (int)fmin(((double)c.x.rows + c.w.rows + 7) / 8, 4.0 * n_cu);   // a row for a wavefront, eight wavefronts or sixteen
-        } else {
-            product = a;
-            c = AlignArgs{};
-            kernel = adapter_kernel(a, n_cu);
+    bool copies;
+    const int kernel = adapter_plan(a, n_cu, &copies);
+    if (copies) {
+        c.K = a.K;
+        c.pitch = adapter_pitch_of(a.K);
+        product.K = c.pitch;
+        if (aligned_x) {
+            c.x = {a.x, aligned_x, a.ldx, a.R};
+            product.x = aligned_x;
+            product.ldx = c.pitch;
         }
-    } else product.K = a.K;
+        if (aligned_w) {
+            c.w = {static_cast<const uint16_t*>(a.w), aligned_w, a.ldw, a.N};
+            product.w = aligned_w;
+            product.ldw = c.pitch;
+        }
+        c.workgroups = (int)fmin(((double)c.x.rows + c.w.rows + 7) / 8, 4.0 * n_cu);   // a row for a wavefront, eight wavefronts or sixteen
+    }
     x.tile = linear_tile_rows(kernel);
     const hipError_t e = launch_adapters_down(a, x, c, n_cu, s);
     return e == hipSuccess ? launch_chosen(kernel, product, x, n_cu, s) : e;

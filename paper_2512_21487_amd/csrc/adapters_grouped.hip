@@ -67,12 +67,9 @@ hipError_t launch_up(const LinearArgs& a, const AdapterArgs& x, const float* wid
     return hipGetLastError();
 }
 
-}  // namespace
-
-hipError_t launch_linear_grouped(const LinearArgs& a, const AdapterArgs& x, float* wide, int32_t* table, int n_cu, hipStream_t s)
+// the product that leaves x W^T in fp32
+LinearArgs product_of(const LinearArgs& a, float* wide)
 {
-    if (a.R <= 0) return hipSuccess;
-    if (a.R > kGathered || a.N < 1 || a.K < 1 || a.w32 || x.n < 1 || x.rank < 8 || x.rank > kRankMost || x.rank % 8) return hipErrorInvalidValue;
     LinearArgs product = a;
     product.out = wide;
     product.ldo = a.N;
@@ -80,23 +77,46 @@ hipError_t launch_linear_grouped(const LinearArgs& a, const AdapterArgs& x, floa
     product.bias = nullptr;
     product.residual = nullptr;
     product.act = kActNone;
-    GroupArgs g{};
-    g.adapters = x;
-    g.table = table;
-    g.groups = adapter_groups(a.R, x.n);
-    const int blocks = (x.rank + 15) / 16;
+    return product;
+}
+
+// groups, shares, workgroups
+void share_groups(GroupArgs& g, int R, int n, int rank, int n_cu)
+{
+    g.groups = adapter_groups(R, n);
+    const int blocks = (rank + 15) / 16;
     // two workgroups for a compute unit, beside the product's own (512 x 4096 x 4096, 400 adapters of rank 32, one / two / four 84 / 90 / 91 us, of rank 128 169 / 187 / 161)
     g.shares = g.groups * blocks <= 2 * n_cu ? blocks : 2 * n_cu / g.groups > 1 ? 2 * n_cu / g.groups : 1;
     g.workgroups = (g.groups * g.shares + 7) / 8 * 8;
-    // Of up to 32 rows the weights bound it, and what is on its way from memory: 32 columns a workgroup and two K steps ahead, eight wavefronts, so that compute units have two workgroups
-    // or more, x A^T beside the product among them.  The product's own kernel / this, rank 16, us: 1, 12 x 5120 x 5120 20.8 / 18.1, 22.6 / 19.6, 2 x 4096 x 4096 17.0 / 14.0,
-    // 4 x 5120 x 1536 12.0 / 10.4, 17 x 4096 x 4096 21.0 / 16.9, 32 x 5120 x 5120 30 / 24; of few columns both are as fast, 1 x 160 x 5120 11.2 / 11.4.  Nor do workgroups of sixteen wavefronts, one a
-    // compute unit, go with many that make x A^T: 111 x 448 x 2240, rank 128 of 58, 30 / 22, 64 x 1536 x 2048, rank 64 of 64, 18 / 15; with few, 48 x 512 x 5120, rank 16 of 48, 14 / 16.
-    const int kernel = adapter_kernel(product, n_cu);
+}
+
+}  // namespace
+
+// Of up to 32 rows the weights bound it, and what is on its way from memory: 32 columns a workgroup and two K steps ahead, eight wavefronts, so that compute units have two workgroups
+// or more, x A^T beside the product among them.  The product's own kernel / this, rank 16, us: 1, 12 x 5120 x 5120 20.8 / 18.1, 22.6 / 19.6, 2 x 4096 x 4096 17.0 / 14.0,
+// 4 x 5120 x 1536 12.0 / 10.4, 17 x 4096 x 4096 21.0 / 16.9, 32 x 5120 x 5120 30 / 24; of few columns both are as fast, 1 x 160 x 5120 11.2 / 11.4.  Nor do workgroups of sixteen wavefronts, one a
+// compute unit, go with many that make x A^T: 111 x 448 x 2240, rank 128 of 58, 30 / 22, 64 x 1536 x 2048, rank 64 of 64, 18 / 15; with few, 48 x 512 x 5120, rank 16 of 48, 14 / 16.
+int grouped_plan(const LinearArgs& a, int n, int rank, int n_cu)
+{
+    GroupArgs g{};
+    share_groups(g, a.R, n, rank, n_cu);
+    const int kernel = adapter_kernel(product_of(a, nullptr), n_cu);
     const bool sixteen = kernel == kLinearSplit16x16 || kernel == kLinearSplit32x16;
-    const hipError_t e = a.R <= 16                                                ? launch_split<1, 2, 8, 2>(product, g, s)
-                         : a.R <= 32 || (sixteen && 2 * g.workgroups > n_cu) ? launch_split<2, 2, 8, 2>(product, g, s)
-                                                                                  : launch_chosen(kernel, product, g, n_cu, s);
+    return a.R <= 16 ? kGroupedRows16 : a.R <= 32 || (sixteen && 2 * g.workgroups > n_cu) ? kGroupedRows32 : kernel;
+}
+
+hipError_t launch_linear_grouped(const LinearArgs& a, const AdapterArgs& x, float* wide, int32_t* table, int n_cu, hipStream_t s)
+{
+    if (a.R <= 0) return hipSuccess;
+    if (a.R > kGathered || a.N < 1 || a.K < 1 || a.w32 || x.n < 1 || x.rank < 8 || x.rank > kRankMost || x.rank % 8) return hipErrorInvalidValue;
+    const LinearArgs product = product_of(a, wide);
+    GroupArgs g{};
+    g.adapters = x;
+    g.table = table;
+    share_groups(g, a.R, x.n, x.rank, n_cu);
+    const int kernel = grouped_plan(a, x.n, x.rank, n_cu);
+    const hipError_t e = kernel == kGroupedRows16 ? launch_split<1, 2, 8, 2>(product, g, s) : kernel == kGroupedRows32 ? launch_split<2, 2, 8, 2>(product, g, s)
+                                                                                          : launch_chosen(kernel, product, g, n_cu, s);
     return e == hipSuccess ? launch_up<2>(a, x, wide, table, g.groups, s) : e;
 }
 

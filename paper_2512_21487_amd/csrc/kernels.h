@@ -293,7 +293,12 @@ struct AlignArgs {
 };
 inline int adapter_pitch_of(int K) { return (K + 7) / 8 * 8; }
 inline bool rows_off_16(int K, long long ld) { return K % 8 != 0 || ld % 8 != 0; }   // whatever the first one's address
-// aligned_x, aligned_w: room for the copies, or NULL; x.tile and x.lists' contents are the launch's
+// What launch_linear_adapters runs the product on (tests ask too); copies: whether rows that are not on 16 bytes are copied in front of it
+int adapter_plan(const LinearArgs& a, int n_cu, bool* copies);
+// and launch_linear_grouped, the number of its adapters and their rank beside the call's sizes: linear_kernel's, or one of two that only groups have
+enum { kGroupedRows16 = 100, kGroupedRows32 };
+int grouped_plan(const LinearArgs& a, int n, int rank, int n_cu);
+// aligned_x, aligned_w: room for the copies of rows that are not on 16 bytes, else NULL; x.tile and x.lists' contents are the launch's
 hipError_t launch_linear_adapters(const LinearArgs& a, AdapterArgs x, uint16_t* aligned_x, uint16_t* aligned_w, int n_cu, hipStream_t s);
 hipError_t launch_linear_grouped(const LinearArgs& a, const AdapterArgs& x, float* wide, int32_t* table, int n_cu, hipStream_t s);
 

@@ -337,8 +337,8 @@ __device__ __forceinline__ void down(const LinearArgs& a, const AdapterArgs& x, 
     __syncthreads();
 }
 
-// Up to kGathered rows in any order, in groups: an adapter's rows, and those without one, are taken 16 at a time.  Of every row a thread counts those in front of it with the same
-// adapter; each row whose count is a multiple of 16 begins a group, and a workgroup has the group of its number and some of its ranks.  So A is read once for 16 of its rows, and
+// Up to kGathered rows in any order, in groups: an adapter's rows, and those without one, are taken 16 at a time.  Of every row those in front of it with the same adapter are counted, by
+// ballots of wavefronts that have all rows; each row whose count is a multiple of 16 begins a group, and a workgroup has the group of its number and some of its ranks.  So A is read once for 16 of its rows, and
 // however many rows have the same adapter, no workgroup has more to do than another.  The workgroup of a group's first ranks writes down its rows.
 template <int WAVES, int DEPTH>
 __device__ __forceinline__ void down_group(const LinearArgs& a, const GroupArgs& g, uint4* lds4, int number)
