@@ -117,9 +117,9 @@ hipError_t launch_tiles(const LinearArgs& a, const AdapterArgs& x, const AlignAr
 }
 
 // Tiles of few rows spread a few hundred of them over the compute units, tall ones read A less often.  16 rows x 16 ranks (a), two workgroups with 16 x 32 (b), two with 32 x 64 (c), 32 x
-// 64 (d), 64 x 64 (e): the whole call of R x 1024 x 4096, 16 prompts, us: rank 16, R 600 30 / 31 / 40 / - / -, 4096 49 / 56 / 55 / - / -, 16384 157 / - / 170 / 159 / 161; rank 64, 1024 34 / 32 /
-// 42 / - / -, 2048 51 / 51 / 47 / 50 / -, 4096 71 / - / 59 / 66 / -, 8192 - / - / 110 / 108 / 116, 16384 - / - / 186 / 170 / 167; rank 128, 4096 - / - / 77 / 71 / 85, 16384 - / - / 253 / 206 / 207; of
-// 16384 x 5120 x 5120, rank 64, (d) 718, (e) 692.  Tiles of 64 x 64 filled by direct loads into a ring took as long as (e) (693), and longer of fewer rows.
+// 64 (d), 64 x 64 (e): the whole call of R x 1024 x 4096, 16 prompts, us: rank 16, R 600 31 / 30 / 40 / 47 / 75, 4096 52 / 57 / 56 / 62 / 76, 16384 159 / 192 / 174 / 166 / 164; rank 64, 1024 35 /
+// 34 / 44 / 50 / 70, 2048 54 / 53 / 50 / 57 / 76, 4096 77 / 78 / 63 / 68 / 81, 8192 142 / 155 / 116 / 116 / 123, 16384 245 / 280 / 196 / 182 / 175; rank 128, 4096 108 / 119 / 84 / 79 / 93, 16384 366 /
+// 442 / 271 / 221 / 232; of 16384 x 5120 x 5120, rank 64, (d) 742, (e) 729.  Tiles of 64 x 64 filled by direct loads into a ring took as long as (e), and longer of fewer rows.
 hipError_t launch_adapters_down(const LinearArgs& a, const AdapterArgs& x, const AlignArgs& c, int n_cu, hipStream_t s)
 {
     if (x.rank <= 16) return launch_tiles<1, 1, 16, 2>(a, x, c, 1, s);

@@ -85,7 +85,7 @@ void share_groups(GroupArgs& g, int R, int n, int rank, int n_cu)
 {
     g.groups = adapter_groups(R, n);
     const int blocks = (rank + 15) / 16;
-    // two workgroups for a compute unit, beside the product's own (512 x 4096 x 4096, 400 adapters of rank 32, one / two / four 84 / 90 / 91 us, of rank 128 169 / 187 / 161)
+    // two workgroups for a compute unit, beside the product's own (512 x 4096 x 4096, 400 adapters of rank 32, one / two / four 92 / 92 / 111 us, of rank 128 166 / 165 / 167)
     g.shares = g.groups * blocks <= 2 * n_cu ? blocks : 2 * n_cu / g.groups > 1 ? 2 * n_cu / g.groups : 1;
     g.workgroups = (g.groups * g.shares + 7) / 8 * 8;
 }
@@ -93,9 +93,9 @@ void share_groups(GroupArgs& g, int R, int n, int rank, int n_cu)
 }  // namespace
 
 // Of up to 32 rows the weights bound it, and what is on its way from memory: 32 columns a workgroup and two K steps ahead, eight wavefronts, so that compute units have two workgroups
-// or more, x A^T beside the product among them.  The product's own kernel / this, rank 16, us: 1, 12 x 5120 x 5120 20.8 / 18.1, 22.6 / 19.6, 2 x 4096 x 4096 17.0 / 14.0,
-// 4 x 5120 x 1536 12.0 / 10.4, 17 x 4096 x 4096 21.0 / 16.9, 32 x 5120 x 5120 30 / 24; of few columns both are as fast, 1 x 160 x 5120 11.2 / 11.4.  Nor do workgroups of sixteen wavefronts, one a
-// compute unit, go with many that make x A^T: 111 x 448 x 2240, rank 128 of 58, 30 / 22, 64 x 1536 x 2048, rank 64 of 64, 18 / 15; with few, 48 x 512 x 5120, rank 16 of 48, 14 / 16.
+// or more, x A^T beside the product among them.  The product's own kernel / this, rank 16, us: 1, 12 x 5120 x 5120 17.5 / 15.0, 18.0 / 15.4, 2 x 4096 x 4096 15.8 / 13.3,
+// 17 x 4096 x 4096 18.2 / 14.8, 32 x 5120 x 5120 22 / 17; of few columns both are as fast, 1 x 160 x 5120 12.5 / 12.4.  Nor do workgroups of sixteen wavefronts, one a
+// compute unit, go with many that make x A^T: 111 x 448 x 2240, rank 128 of 58, 32 / 23, 64 x 1536 x 2048, rank 64 of 64, 17 / 15; with few, 48 x 512 x 5120, rank 16 of 48, 14 / 14.
 int grouped_plan(const LinearArgs& a, int n, int rank, int n_cu)
 {
     GroupArgs g{};

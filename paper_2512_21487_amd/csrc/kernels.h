@@ -269,8 +269,8 @@ constexpr int kRankMost = 128;
 int linear_tile_rows(int kernel);       // of what linear_kernel chose; 0: no tiles
 // Few rows, of many adapters maybe: the product's launch leaves x W^T in fp32, and other workgroups of it make `low`, of groups of up to 16 rows of one adapter (or of none); another
 // launch adds the groups' low B_a^T and has the epilogue.
-// (tiles that the reduction goes on in / groups, us: rows in no order, 600, 768, 1024 x 4096 x 4096, rank 16 of 64, 119 / 63, 120 / 65, 129 / 86, 768 x 2048 x 2048, rank 64 of 256, 114 / 73; all of
-// their own, 768 x 4096 x 4096 173 / 198; prompts, 640 x 4096 x 4096 45 / 39, 640 x 5120 x 1536 28 / 35, 768 x 4096 x 4096 47 / 47, 768 x 2048 x 2048, rank 64, 27 / 31, 1024 x 4096 x 4096 48 / 57)
+// (tiles that the reduction goes on in / groups, us: rows in no order, 600, 768, 1024 x 4096 x 4096, rank 16 of 64, 121 / 60, 121 / 63, 132 / 84, 768 x 2048 x 2048, rank 64 of 256, 143 / 80; as many
+// adapters as rows, 768 x 4096 x 4096 171 / 209; prompts, 640 x 4096 x 4096 44 / 36, 640 x 5120 x 1536 27 / 34, 768 x 4096 x 4096 44 / 43, 768 x 2048 x 2048, rank 64, 28 / 29, 1024 x 4096 x 4096 48 / 57)
 constexpr int kGathered = 768, kGroupEntry = 1 + 16;
 struct GroupArgs {
     static constexpr bool on = false, beside = true;
@@ -281,12 +281,12 @@ struct GroupArgs {
 inline int adapter_groups(int R, int n) { return R / 16 + (n + 1 < R ? n + 1 : R); }   // full ones, and one that is not for every adapter and for none
 // The product's kernel with adapters: linear_kernel's, but dot products have no reduction that could go on, and too few wavefronts to make x A^T beside them (rows / split, us: 8 x 1024 x
 // 4096 21 / 12, 1 x 160 x 5120 11.4 / 10.7, rank 16), and of a K of less than the four steps that the smaller tiles need, large tiles are often few: 192 x 256 tiles / shared reduction, us: 800 x
-// 448 x 128 22 / 10, 1016 x 256 x 192 24 / 10, 5692 x 128 x 192 24 / 14, 7933 x 299 x 130, 84 tiles, 53 / 27; 1000 x 5120 x 192, 120 tiles, 24 / 29, 4096 x 2048 x 128 26 / 36;
-// grouped 700 x 1024 x 192 18 / 14, 128 x 8192 x 128 18 / 12.
+// 448 x 128 24 / 13, 1016 x 256 x 192 25 / 13, 5692 x 128 x 192 26 / 15, 7933 x 299 x 130, 84 tiles, 42 / 21; 1000 x 5120 x 192, 120 tiles, 24 / 29, 4096 x 2048 x 128 26 / 36;
+// grouped 700 x 1024 x 192 19 / 19, 128 x 8192 x 128 18 / 14.
 int adapter_kernel(const LinearArgs& a, int n_cu);
 // Rows of x or of W that are not on 16 bytes are copied in front of a product in tiles, each to `pitch` elements with zeros at the end, beside x A^T.  That moves them once more; tiles through registers take
-// twice as long as direct loads.  Without / with copies, rank 16, us: 700 x 1000 x 1001 29 / 22, 1531 x 1409 x 2049 53 / 43, 8000 x 777 x 2001 126 / 85, rows of x alone: 600 x 4096 x 1024 31 / 24,
-// 4096 x 4096 x 2048 164 / 80, 16384 x 2048 x 2048 344 / 178.
+// twice as long as direct loads.  Without / with copies, rank 16, us: 700 x 1000 x 1001 28 / 21, 1531 x 1409 x 2049 50 / 42, 8000 x 777 x 2001 119 / 80, rows of x alone: 600 x 4096 x 1024 30 / 24,
+// 4096 x 4096 x 2048 157 / 79, 16384 x 2048 x 2048 319 / 176.
 struct AlignArgs {
     struct Rows { const uint16_t* from; uint16_t* to; long long ld; int rows; } x, w;   // rows 0: as they are
     int K, pitch, workgroups;

@@ -1,6 +1,9 @@
 // Norms behind and in front of a block, with the block's gate and the residual stream between them:
 //   h = residual_scale residual + block_scale f(gate) N_after(block);   sum = h,  out = N_before(h)
-// All of it is fp32 in registers, a row at a time: each operand is read once, each result rounded once and written once.
+// All of it is fp32 in registers, a row at a time: each operand is read once, each result rounded once and written once.  (Rows of more than 16384 elements with an operand in fp32
+// have up to 105 registers a lane more than there are, in scratch memory: 1024 x 32768, block and stream in fp32, 138 us, 3.4 TB/s; in bf16, without, 63 us, 4.2 TB/s.)
+#include <type_traits>
+
 #include "rows.h"
 
 namespace moe_ep {
@@ -62,6 +65,22 @@ __device__ __forceinline__ void store8(char* row, int col, bool wide, int left, 
 struct Add { __device__ float operator()(float a, float b) const { return a + b; } };
 struct Larger { __device__ float operator()(float a, float b) const { return fmaxf(a, b); } };   // of two numbers where one is NaN, the other
 
+// over a wavefront's lanes, the same bits in every lane: as by exchanges of lanes 1, 2, 4, .. 32 apart, the mirrored ones of which hold what those would.  Without LDS (exchanges
+// through it, us: 1531 x 1409, layer norms on both sides, 12.4 / 12.0, 4096 x 4096 38.6 / 34.6; RMS, 16384 x 5120, 120.8 / 119.1)
+template <class Op>
+__device__ __forceinline__ float over_wave(float v, Op op)
+{
+    const auto from = [&](auto control) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), decltype(control)::value, 0xf, 0xf, true)); };
+    v = op(v, from(std::integral_constant<int, 0xb1>()));    // quad_perm 1 0 3 2
+    v = op(v, from(std::integral_constant<int, 0x4e>()));    // quad_perm 2 3 0 1
+    v = op(v, from(std::integral_constant<int, 0x141>()));   // row_half_mirror
+    v = op(v, from(std::integral_constant<int, 0x140>()));   // row_mirror
+    const auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = op(__uint_as_float(rows[0]), __uint_as_float(rows[1]));
+    const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return op(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
+}
+
 // N numbers over the WAVES wavefronts of a row, the same bits in every lane
 constexpr int kOverRow = 2;
 template <int WAVES, int N, class Op>
@@ -69,9 +88,7 @@ __device__ __forceinline__ void over_row(float (&v)[N], float* lds, int& turn, O
 {
     static_assert(N <= kOverRow, "norm_kernel's LDS");
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1)
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = op(v[i], __shfl_xor(v[i], d, 64));
+    for (int i = 0; i < N; ++i) v[i] = over_wave(v[i], op);
     if constexpr (WAVES > 1) {
         // two places in turn: who is at the next reduction has left this one's barrier, which everybody reaches behind reading the last one's
         float* const at = lds + (turn & 1) * (kOverRow * WAVES);
@@ -85,95 +102,122 @@ __device__ __forceinline__ void over_row(float (&v)[N], float* lds, int& turn, O
             v[i] = at[i * WAVES];
 #pragma unroll
             for (int w = 1; w < WAVES; ++w) v[i] = op(v[i], at[i * WAVES + w]);
+            if (N > 1) __builtin_amdgcn_sched_barrier(0);   // one number's sums after the other's: all at once are 2 WAVES registers
         }
     }
 }
 
-template <int WAVES, int V>
-__device__ __forceinline__ float mean_of(const float (&x)[V][8], float each, float* lds, int& turn)
-{
-    float s[1] = {0.f};
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s[0] += x[v][i];
-    over_row<WAVES>(s, lds, turn, Add());
-    return s[0] * each;
-}
-
 // x <- (x - mean) / sqrt(mean((x - mean)^2) + eps); RMS: without the mean.  The mean is taken out before the squares are summed, so that nothing cancels.
-// What the mean is off by, a few steps of it, is all that is left of a row of equal numbers: the sum of what is left comes with that of its squares and is taken out too, from
-// the row once more if it is a quarter of the result's unit or more.  So results are off by steps of their own, M / 64 + 20 at most, however large the mean is beside the spread.
+// What the mean is off by, a few steps of it, is all that is left of a row of equal numbers: the sum of what is left comes with that of its squares and is taken out too, and
+// what the squares are of once more if it is a quarter of the result's unit or more.  So results are off by steps of their own, M / 64 + 20 at most, however large the mean is beside the spread.
 // Where squares or sums leave fp32 while the row's numbers do not, its largest is between 2^56 (its square times 32768 is 2^127) and 2^128: times 2^-72 neither
 // they nor anything that counts beside them is lost, and eps, which does not count there, goes with it, but to no less than a normal number: numbers that are all the
 // mean have nothing else below the square root.  Such a row costs two or three reductions more.
-// (Without / with the sum of what is left, us: 1531 x 1409, fp32 stream, layer norms on both sides, 11.4 / 12.1.)
-template <bool LAYER, int WAVES, int V>
-__device__ __forceinline__ void normalise_as(float (&x)[V][8], const int (&left)[V], int cols, float eps, float* lds, int& turn)
+constexpr float kScaled = 0x1p-72f;
+__device__ __forceinline__ float scaled_eps(float eps) { return fmaxf(eps * kScaled * kScaled, __FLT_MIN__); }
+template <int WAVES, int V>
+__device__ __forceinline__ float largest(const float (&x)[V][8], float* lds, int& turn)
 {
-#pragma clang fp contract(off)   // the same differences from the mean everywhere
+    float top[1] = {0.f};
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top[0] = fmaxf(top[0], fabsf(x[v][i]));
+    over_row<WAVES>(top, lds, turn, Larger());
+    return top[0];
+}
+
+template <int WAVES, int V>
+__device__ __forceinline__ void normalise_rms(float (&x)[V][8], const int (&left)[V], int cols, float eps, float* lds, int& turn)
+{
     const float each = 1.0f / (float)cols;
-    float mean = 0.f, rest = 0.f, power = 0.f;
-    if constexpr (LAYER) mean = mean_of<WAVES, V>(x, each, lds, turn);
-    bool scaled = false;
-    // a pass leaves 2^-15 of a mean or less, and 2^128 is 2^201 from the root of the least eps
-    for (int pass = 0; pass < 16; ++pass) {
-        float s[LAYER ? 2 : 1] = {};
+    for (int scaled = 0;; ++scaled) {
+        float q[1] = {0.f};
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float d = i < left[v] ? x[v][i] - mean : 0.f;
+                const float d = i < left[v] ? x[v][i] : 0.f;
+                q[0] = fmaf(d, d, q[0]);
+            }
+        over_row<WAVES>(q, lds, turn, Add());
+        const float power = q[0] * each;
+        // (a number that is none, or infinite: as the formula has it)
+        if (scaled == 0 && !(power <= __FLT_MAX__) && largest<WAVES, V>(x, lds, turn) <= __FLT_MAX__) {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[v][i] *= kScaled;
+            eps = scaled_eps(eps);
+            continue;
+        }
+        const float r = __builtin_amdgcn_rsqf(power + eps);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[v][i] *= r;
+        return;
+    }
+}
+
+// Either kind.  The row stays as it is until the end: what a pass found out is in three numbers beside it.  (1531 x 1409, layer norms on both sides, without the sum of what is left /
+// with it, us: 11.4 / 12.0.)
+template <int WAVES, int V>
+__device__ __forceinline__ void normalise_any(float (&x)[V][8], const int (&left)[V], int cols, bool layer, float eps, float* lds, int& turn)
+{
+#pragma clang fp contract(off)   // the same differences from the mean everywhere
+    const float each = 1.0f / (float)cols;
+    const auto mean_of = [&](float by) {
+        float s[1] = {0.f};
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[0] = fmaf(x[v][i], by, s[0]);
+        over_row<WAVES>(s, lds, turn, Add());
+        return s[0] * each;
+    };
+    float by = 1.f, mean = layer ? mean_of(1.f) : 0.f, rest = 0.f, last = 0.f, power = 0.f;
+    const auto differ = [&](int v, int i) { return fmaf(x[v][i], by, -mean) - rest; };
+    // a pass leaves 2^-15 of a mean or less: of 2^128 the ninth leaves less than a quarter of the root of the least eps
+#pragma unroll 1
+    for (int pass = 0; pass < 16; ++pass) {
+        float s[2] = {0.f, 0.f};
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float d = i < left[v] ? differ(v, i) : 0.f;
                 s[0] = fmaf(d, d, s[0]);
-                if constexpr (LAYER) s[1] += d;
+                s[1] += d;
             }
         over_row<WAVES>(s, lds, turn, Add());
         power = s[0] * each;
-        if (!scaled && !(power <= __FLT_MAX__)) {
-            float top[1] = {0.f};
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) top[0] = fmaxf(top[0], fabsf(x[v][i]));
-            over_row<WAVES>(top, lds, turn, Larger());
-            // a number that is none, or infinite: as the formula has it
-            if (top[0] <= __FLT_MAX__) {
-                constexpr float by = 0x1p-72f;
-#pragma unroll
-                for (int v = 0; v < V; ++v)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[v][i] *= by;
-                eps = fmaxf(eps * by * by, __FLT_MIN__);
-                scaled = true;
-                if constexpr (LAYER) mean = mean_of<WAVES, V>(x, each, lds, turn);
-                continue;
-            }
+        if (by == 1.f && !(power <= __FLT_MAX__) && largest<WAVES, V>(x, lds, turn) <= __FLT_MAX__) {
+            by = kScaled;
+            eps = scaled_eps(eps);
+            if (layer) mean = mean_of(by);
+            continue;
         }
-        if constexpr (!LAYER) break;
-        else {
-            rest = s[1] * each;
-            const float spread = fmaf(-rest, rest, power);
-            power = spread < 0.f ? 0.f : spread;
-            if (!(rest * rest > 0.0625f * (power + eps))) break;
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[v][i] -= mean;
-            mean = rest;
-        }
+        if (!layer) break;
+        last = s[1] * each;
+        const float spread = fmaf(-last, last, power);
+        power = spread < 0.f ? 0.f : spread;
+        if (!(last * last > 0.0625f * (power + eps))) break;
+        rest += last;
     }
     const float r = __builtin_amdgcn_rsqf(power + eps);
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[v][i] = (LAYER ? x[v][i] - mean - rest : x[v][i]) * r;
+        for (int i = 0; i < 8; ++i) x[v][i] = (differ(v, i) - last) * r;
 }
 
-template <int WAVES, int V>
+// LAYERS: it may be a layer norm
+template <bool LAYERS, int WAVES, int V>
 __device__ __forceinline__ void normalise(float (&x)[V][8], const int (&left)[V], int cols, int kind, float eps, float* lds, int& turn)
 {
-    if (kind == kNormLayer) normalise_as<true, WAVES, V>(x, left, cols, eps, lds, turn);
-    else normalise_as<false, WAVES, V>(x, left, cols, eps, lds, turn);
+    if constexpr (LAYERS) normalise_any<WAVES, V>(x, left, cols, kind == kNormLayer, eps, lds, turn);
+    else normalise_rms<WAVES, V>(x, left, cols, eps, lds, turn);
 }
 
 // A weight and a bias of 8 features
@@ -209,10 +253,11 @@ __device__ __forceinline__ float gate_of(float g, int form)
 }
 
 // WAVES wavefronts have a row, a lane 8 elements of it in each of V turns.  WIDE: the block, the stream or the gate is fp32.  EARLY: weights and biases are asked for
-// with the row, not behind the sums in front of them.
-// Of many rows memory bounds it: 16384 x 5120, bf16, residual and norm in front, 125 us for 671 MB, 5.4 TB/s (a copy of 1 GiB: 5.1); of few the chain of load, sum
-// over wavefronts, square root, store: 1 x 5120 3.8 us, 5.0 with norms on both sides and nothing in L2.
-template <int WAVES, int V, bool WIDE, bool EARLY>
+// with the row, not behind the sums in front of them.  LAYERS: some norm is a layer norm, whose code costs others registers (RMS with it / without, us:
+// 16384 x 5120 123 / 117, 4096 x 4096, norms on both sides, 32.5 / 30.2, 4096 x 32768 222 / 212).
+// Of many rows memory bounds it: 16384 x 5120, bf16, residual and norm in front, 119 us for 671 MB, 5.6 TB/s (a copy of 1 GiB: 5.1); of few the chain of load, sum
+// over wavefronts, square root, store: 1 x 5120 3.7 us, 4.5 with norms on both sides and nothing in L2.
+template <int WAVES, int V, bool WIDE, bool EARLY, bool LAYERS>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(NormArgs a)
 {
     constexpr int ROWS = WAVES == 1 ? 4 : 1;
@@ -255,7 +300,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(Nor
     float x[V][8];
 #pragma unroll
     for (int v = 0; v < V; ++v) to_float(b[v], a.block32, x[v]);
-    if (a.after != kNormNone) normalise<WAVES, V>(x, left, a.M, a.after, a.eps, lds, turn);
+    if (a.after != kNormNone) normalise<LAYERS, WAVES, V>(x, left, a.M, a.after, a.eps, lds, turn);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         if constexpr (!EARLY) after[v] = load_weights(a, a.after_weight, a.after_bias, col[v], left[v]);
@@ -287,7 +332,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_kernel(Nor
     for (int v = 0; v < V; ++v)
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[v][i] = i < left[v] ? x[v][i] : 0.f;
-    normalise<WAVES, V>(x, left, a.M, a.before, a.eps, lds, turn);
+    normalise<LAYERS, WAVES, V>(x, left, a.M, a.before, a.eps, lds, turn);
     char* const out = static_cast<char*>(a.out) + (size_t)m * a.ldo * (a.out32 ? 4 : 2);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -302,8 +347,12 @@ hipError_t launch_as(const NormArgs& a, hipStream_t s)
 {
     const long long groups = WAVES == 1 ? ((long long)a.R + 3) / 4 : a.R;
     const dim3 threads(WAVES == 1 ? 256 : WAVES * 64);
-    if (a.block32 || a.stream32 || (a.gate32 && !a.gate_per_row)) hipLaunchKernelGGL((norm_kernel<WAVES, V, true, EARLY>), grid_of(groups), threads, 0, s, a);
-    else hipLaunchKernelGGL((norm_kernel<WAVES, V, false, EARLY>), grid_of(groups), threads, 0, s, a);
+    const bool wide = a.block32 || a.stream32 || (a.gate32 && !a.gate_per_row);
+    const auto launch = [&](auto layers) {
+        if (wide) hipLaunchKernelGGL((norm_kernel<WAVES, V, true, EARLY, decltype(layers)::value>), grid_of(groups), threads, 0, s, a);
+        else hipLaunchKernelGGL((norm_kernel<WAVES, V, false, EARLY, decltype(layers)::value>), grid_of(groups), threads, 0, s, a);
+    };
+    if (a.after == kNormLayer || a.before == kNormLayer) launch(std::true_type{}); else launch(std::false_type{});
     return hipGetLastError();
 }
 
@@ -312,10 +361,10 @@ hipError_t launch_when(bool early, const NormArgs& a, hipStream_t s) { return ea
 
 }  // namespace
 
-// The least that holds a row, in one turn up to 4096 elements.  Residual and norm of bf16 rows, turns x wavefronts, us: 1 / 1024 / 16384 x 2048 1 x 4 3.0 / 6.1 /
-// 47, 2 x 2 3.6 / 6.5 / 48, 4 x 1 5.0 / 8.2 / 53; x 4096 1 x 8 3.3 / 9.9 / 96, 2 x 4 3.7 / 9.8 / 94, 4 x 2 5.2 / 12 / 99.  Beyond 4096 the turns are two where compute units have
-// several rows: 1 x 16 / 2 x 8, of norms on both sides, operands not in L2, 1, 33, 256, 512 x 5120 5.0 / 5.3, 5.7 / 6.2, 7.0 / 7.5, 12 / 10, 256 x 8192 8.4 / 8.5; of one norm, 1024, 16384
-// x 5120 17 / 14, 183 / 123.
+// The least that holds a row, in one turn up to 4096 elements.  Residual and norm of bf16 rows, turns x wavefronts, us: 1 / 1024 / 16384 x 2048 1 x 4 2.9 / 6.0 /
+// 48, 2 x 2 3.3 / 6.2 / 47, 4 x 1 5.5 / 8.4 / 52; x 4096 1 x 8 3.1 / 9.0 / 98, 2 x 4 3.4 / 8.9 / 96, 4 x 2 5.3 / 11 / 99.  Beyond 4096 the turns are two where compute units have
+// several rows: 1 x 16 / 2 x 8, of norms on both sides, operands not in L2, 1, 33, 256, 512 x 5120 4.5 / 4.6, 5.2 / 5.6, 6.4 / 6.9, 11 / 10, 256 x 8192 7.8 / 7.8; of one norm, 1024, 16384
+// x 5120 14 / 11, 170 / 119.
 int norm_kernel_of(int R, int M, int n_cu)
 {
     if (M > 4096 && M <= 8192) return R <= n_cu ? kNorm16x1 : kNorm8x2;
@@ -327,9 +376,10 @@ hipError_t launch_norm(const NormArgs& a, int n_cu, hipStream_t s)
     if (a.R <= 0) return hipSuccess;
     if (a.M < 1 || a.M > kNormMost) return hipErrorInvalidValue;
     // With a row for every compute unit, or fewer, nothing but the row's own loads hides those of the weights.  Weights asked for behind the sums / with the row, norms on
-    // both sides, operands not in L2, us: 1, 33, 256, 512 x 2048 4.1 / 3.6, 4.9 / 4.2, 5.6 / 4.8, 6.1 / 5.7; x 4096 4.5 / 4.0, 5.6 / 4.7, 6.5 / 5.8, 8.0 / 8.3; with more
-    // rows their registers cost wavefronts: 16384 x 2048 47 / 51, x 4096 96 / 101 (one norm).
-    const bool early = a.R <= n_cu;
+    // both sides, operands not in L2, us: 1, 33, 256, 512 x 2048 3.6 / 3.1, 4.1 / 3.5, 5.1 / 4.3, 5.7 / 5.3; x 4096 4.0 / 3.4, 5.2 / 4.3, 6.0 / 5.3, 7.7 / 7.4.  With more rows the registers
+    // that they take are wavefronts less: of an RMS norm in front that costs least (16384 x 2048, 4096 50 / 48, 101 / 94, norms on both sides 55 / 56, 125 / 107, a gate an element 66 / 68,
+    // 149 / 127), of layer norms it is as often worse (49 / 52, 104 / 103, on both sides 73 / 73, 161 / 147, 4096 rows 24 / 24, 43 / 43), without a norm in front it is (38 / 39, 69 / 71).
+    const bool early = a.R <= n_cu || (a.before == kNormRms && a.after != kNormLayer);
     switch (norm_kernel_of(a.R, a.M, n_cu)) {
     case kNorm1x1: return launch_when<1, 1>(early, a, s);
     case kNorm2x1: return launch_when<2, 1>(early, a, s);
