@@ -79,3 +79,24 @@ def test_rows_that_are_copied(name, R, N, K, pads):
             on(name, c, pads=pads[:2])
         c.run()
         c.check()
+
+
+@pytest.mark.parametrize("name,R,N,K", [(name, *MANY[name][-1]) for name in MANY] + [("off: " + name, *OFF[name]) for name in sorted(OFF)])
+@pytest.mark.parametrize("out32", [False, True])
+def test_a_broken_adapter_on_every_kernel(name, R, N, K, out32):
+    """B of one adapter is NaN in the first and the last column, A of another in one number; rows of others have what their formula gives, the broken ones' NaN where it does, residual in place."""
+    off = name.startswith("off: ")
+    c = Adapted(R, N, K, 16, 5, "own", out32=out32, bias=True, residual=True, name="gelu", shifts=(1, 0, 0, 0) if off else (0, 0, 0, 0))
+    on(name[5:] if off else name, c)
+    want, bound = c.want()
+    c.up[1, 0], c.up[1, N - 1], c.down[3, 15, 0] = float("nan"), float("nan"), float("nan")
+    none = torch.zeros((R, N), dtype=torch.bool, device="cuda")
+    none[c.index == 1, 0] = none[c.index == 1, N - 1] = True
+    none[c.index == 3] = True
+    c.out.copy_(c.r)
+    c.r = c.out
+    c.run()
+    torch.cuda.synchronize()
+    got = c.out.double()
+    assert torch.equal(torch.isnan(got), none)
+    assert bool((((got - want).abs() / bound)[~none] <= 1.0).all())
