@@ -505,16 +505,19 @@ def linear_adapters(cfg: LinearConfig, adapters: AdapterConfig, x, weight, index
         stream = _current_stream(cfg.device)
     K, N, at, n, rank = cfg.in_features, cfg.out_features, cfg.device, adapters.n_adapters, adapters.rank
     result = F32 if cfg.out_type else BF16
-    if workspace is not None and workspace_bytes is None:
-        try:
-            workspace_bytes = workspace.numel() * workspace.element_size()
-        except AttributeError:
-            raise ValueError("workspace_bytes must be given with an address") from None
+    if hasattr(workspace, "numel"):
+        have = workspace.numel() * workspace.element_size()
+        if workspace_bytes is None:
+            workspace_bytes = have
+        elif workspace_bytes > have:
+            raise ValueError(f"workspace has {have} bytes, not workspace_bytes ({workspace_bytes})")
         if not workspace.is_contiguous():
             raise ValueError("workspace must be contiguous")
         if workspace.get_device() != at:
             _check_place(workspace, "workspace", at)
         workspace = workspace.data_ptr()
+    elif workspace is not None and workspace_bytes is None:
+        raise ValueError("workspace_bytes must be given with an address")
     why = ctypes.c_char_p()
     rc = (_lib or load_library()).moe_ep_linear_adapters(
         ctypes.byref(cfg), ctypes.byref(adapters), _rows(x, "x", n_rows, K, cfg.x_stride or K, BF16, at),

@@ -115,3 +115,15 @@ def test_adapters_whose_shape_is_another(name, shape, fits):
     with pytest.raises(ValueError, match=name) as ei:   # one that fits is refused for being on the host
         call(both)
     assert ("must be [" in str(ei.value)) == (not fits)
+
+
+def test_more_workspace_than_the_tensor_has():
+    """A number of bytes beside a tensor is no licence to write behind it."""
+    torch = pytest.importorskip("torch")
+    small = torch.zeros(1 << 10, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="workspace has 1024 bytes"):
+        call(dict(workspace=small, workspace_bytes=1 << 20))
+    with pytest.raises(ValueError, match="contiguous"):
+        call(dict(workspace=torch.zeros((8, 64), dtype=torch.uint8)[:, :32], workspace_bytes=64))
+    with pytest.raises(ValueError, match="workspace"):   # one that fits is refused for being on the host
+        call(dict(workspace=small, workspace_bytes=1 << 10))
